@@ -1,0 +1,388 @@
+"""The feed-forward sub-block's operators as timed cases: the residual's
+addition with the RMS norm (16-bit or 8-bit output) and its gradient, the gated
+feed-forward block forward and as a training step, and the projection shared by
+requests that bring low-rank adapters of their own.
+
+Token counts are those of the templates in workloads/ (4096 and 17,776 tokens,
+two long videos of 28,612), prompts of odd lengths and single tokens; widths are
+the long-video template's 4096 and 16384 and generic ones down to 256.  draw()
+spreads over the same ranges.
+"""
+import math
+
+import torch
+
+own = False     # whether run() calls the library, or computes the plain form
+
+DEV = "cuda:0"
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32, "e4m3": torch.float8_e4m3fn}
+CODES = {"bf16": 0, "f16": 1, "f32": 2, "e4m3": 3}     # xema_dtype
+ACTS = {"silu": 0, "gelu": 1}
+EPS = 1e-6
+
+
+def _norm(name, rows, dim, x, resid, out):
+    return {"name": name, "kind": "norm", "rows": rows, "dim": dim, "x": x, "resid": resid, "out": out}
+
+
+def _gated(name, kind, rows, dim, hidden, dtype, act, bias):
+    return {"name": name, "kind": kind, "rows": rows, "dim": dim, "hidden": hidden, "type": dtype, "act": act, "bias": bias}
+
+
+def _lora(name, requests, tokens, dim, out, rank, adapters, dtype, bias, padding=0):
+    return {"name": name, "kind": "lora", "requests": requests, "tokens": tokens, "dim": dim, "out_dim": out, "rank": rank,
+            "adapters": adapters, "type": dtype, "bias": bias, "padding": padding}
+
+
+def listed():
+    return [
+        # the next token of four requests, handed to 8-bit projections: latency
+        _norm("norm_tokens_8bit", 4, 4096, "bf16", "bf16", "e4m3"),
+        # a prompt of odd length beside an fp32 residual stream, 16-bit output
+        _norm("norm_prompt", 1539, 2568, "f16", "f32", "f16"),
+        # two long videos, the residual stream in fp32, 8-bit output: the largest
+        _norm("norm_long_8bit", 57224, 4096, "bf16", "f32", "e4m3"),
+        # the gradient of a training batch of eight sequences
+        {"name": "norm_gradient", "kind": "norm_bwd", "rows": 16384, "dim": 4096, "type": "bf16"},
+        # one token of one request through a wide layer: the weights are read once
+        _gated("gated_token", "gated", 1, 4096, 16384, "bf16", "silu", False),
+        # a ragged prompt through a narrow layer, widths that no tile divides
+        _gated("gated_prompt", "gated", 777, 1544, 4104, "f16", "gelu", True),
+        # the 17,776 tokens of a video in 8 bits
+        _gated("gated_video_8bit", "gated", 17776, 4096, 16384, "e4m3", "silu", False),
+        # a training step of a small layer on a short ragged batch
+        _gated("gated_train_small", "gated_train", 333, 512, 1368, "f16", "gelu", True),
+        # a training step of a large layer: the largest case
+        _gated("gated_train_large", "gated_train", 8192, 4096, 11008, "bf16", "silu", False),
+        # the next tokens of 48 requests with 20 adapters among them
+        _lora("lora_tokens", 48, 1, 4096, 4096, 16, 20, "bf16", True),
+        # prompts of seven requests in a padded batch, each with its own adapter
+        _lora("lora_prompts", 7, 431, 1544, 4104, 64, 7, "f16", False, 187),
+        # four image sequences of 4608 tokens, an adapter each
+        _lora("lora_images", 4, 4608, 4096, 4096, 32, 4, "bf16", True),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _width(rng, lo, hi, unit=8):
+    """A multiple of 8 (of 16 for 8-bit rows): half of the draws a multiple of 256."""
+    w = _log(rng, lo, hi)
+    return w // 256 * 256 if w >= 512 and rng.random() < 0.5 else (w + unit - 1) // unit * unit
+
+
+def draw(rng):
+    most = 0.8 * 12 * 8192 * 4096 * 11008
+    kind = rng.choice(("norm", "norm", "norm_bwd", "gated", "gated", "gated_train", "lora", "lora"))
+    while True:
+        if kind == "norm":
+            c = _norm("", _log(rng, 1, 57000), _width(rng, 256, 8192, 16), rng.choice(("bf16", "f16", "f32")),
+                      rng.choice(("none", "bf16", "f16", "f32")), rng.choice(("bf16", "f16", "e4m3", "e4m3")))
+            fits = c["rows"] * c["dim"] <= 57224 * 4096
+        elif kind == "norm_bwd":
+            c = {"name": "", "kind": kind, "rows": _log(rng, 1, 40000), "dim": _width(rng, 256, 8192),
+                 "type": rng.choice(("bf16", "f16"))}
+            fits = c["rows"] * c["dim"] <= 16384 * 4096
+        elif kind in ("gated", "gated_train"):
+            dtype = rng.choice(("bf16", "f16", "e4m3") if kind == "gated" else ("bf16", "f16"))
+            unit = 16 if dtype == "e4m3" else 8
+            c = _gated("", kind, _log(rng, 1, 20000), _width(rng, 256, 6144, unit), _width(rng, 512, 16384, unit), dtype,
+                       rng.choice(("silu", "gelu")), rng.choice((False, True)))
+            fits = work(c)["flops"] <= most
+        else:
+            tokens = rng.choice((1, 1, _log(rng, 2, 4608)))
+            requests = _log(rng, 1, 128) if tokens == 1 else rng.randint(1, 8)
+            c = _lora("", requests, tokens, _width(rng, 256, 6144), _width(rng, 256, 8192), 8 * rng.choice((1, 2, 4, 8, 16)),
+                      rng.randint(1, 24), rng.choice(("bf16", "f16")), rng.choice((False, True)),
+                      rng.choice((0, rng.randint(0, 200))))
+            fits = work(c)["flops"] <= most
+        if fits:
+            del c["name"]
+            return c
+
+
+# -- inputs ------------------------------------------------------------------------------------------------------
+
+
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def _normal(g, shape, std=1.0, dtype=torch.bfloat16, mean=0.0):
+    return torch.randn(shape, generator=g, device=DEV, dtype=torch.float32).mul_(std).add_(mean).to(dtype)
+
+
+def _eight_bit(t):
+    """Rows as e4m3 codes and one scale a row."""
+    scale = t.abs().amax(1).clamp_min(1e-12) / 448
+    return (t / scale[:, None]).to(torch.float8_e4m3fn), scale
+
+
+def _norm_inputs(c, seed):
+    g, shape = _gen(seed), (c["rows"], c["dim"])
+    # tokens of unlike sizes, as a residual stream holds them, and a few large channels
+    size = torch.exp(torch.randn((c["rows"], 1), generator=g, device=DEV))
+    big = 1 + 7 * (torch.rand((1, c["dim"]), generator=g, device=DEV) < 0.01)
+    d = {"x": (_normal(g, shape, dtype=torch.float32) * big).to(TYPES[c["x"]]), "gamma": _normal(g, (c["dim"],), 0.1, mean=1.0)}
+    if c["resid"] != "none":
+        d["resid"] = (_normal(g, shape, dtype=torch.float32) * size).to(TYPES[c["resid"]])
+    return d
+
+
+def _norm_bwd_inputs(c, seed):
+    g, shape, t = _gen(seed), (c["rows"], c["dim"]), TYPES[c["type"]]
+    return {"x": _normal(g, shape, 2.0, t), "dy": _normal(g, shape, 1e-2, t), "dsum": _normal(g, shape, 1e-2, t),
+            "gamma": _normal(g, (c["dim"],), 0.1, mean=1.0)}
+
+
+def _gated_inputs(c, seed):
+    g, D, F = _gen(seed), c["dim"], c["hidden"]
+    t = TYPES[c["type"]]
+    d = {}
+    for name, shape, std in (("x", (c["rows"], D), 1.0), ("gate_w", (F, D), D ** -0.5), ("up_w", (F, D), D ** -0.5)):
+        v = _normal(g, shape, std, torch.float32)
+        if c["type"] == "e4m3":
+            d[name], d[name.split("_")[0] + "_scale"] = _eight_bit(v)
+        else:
+            d[name] = v.to(t)
+    if c["bias"]:
+        d["gate_b"], d["up_b"] = _normal(g, (F,), D ** -0.5), _normal(g, (F,), D ** -0.5)
+    if c["kind"] == "gated_train":
+        d["dy"] = _normal(g, (c["rows"], F), 0.05, t)
+    return d
+
+
+def _lora_inputs(c, seed):
+    g, t = _gen(seed), TYPES[c["type"]]
+    D, N, R, n = c["dim"], c["out_dim"], c["rank"], c["adapters"]
+    requests, rows = c["requests"], c["requests"] * c["tokens"]
+    # every eighth request or so has no adapter; the rows behind the last request are padding
+    ids = torch.randint(0, n, (requests,), generator=g, device=DEV, dtype=torch.int32)
+    ids[torch.rand((requests,), generator=g, device=DEV) < 0.125] = -1
+    pad = torch.full((c["padding"],), -2, dtype=torch.int32, device=DEV)
+    return {"x": _normal(g, (rows + c["padding"], D), dtype=t), "w": _normal(g, (N, D), D ** -0.5, t),
+            "bias": _normal(g, (N,), D ** -0.5) if c["bias"] else None,
+            "a": _normal(g, (n, R, D), D ** -0.5, t), "b": _normal(g, (n, N, R), 0.5 * R ** -0.5, t),
+            "scale": torch.rand((n,), generator=g, device=DEV) + 0.5,
+            "ids": torch.cat((ids.repeat_interleave(c["tokens"]), pad))}
+
+
+INPUTS = {"norm": _norm_inputs, "norm_bwd": _norm_bwd_inputs, "gated": _gated_inputs, "gated_train": _gated_inputs,
+          "lora": _lora_inputs}
+
+
+def prepare(case, seed):
+    """The inputs and the buffers that a program allocates once."""
+    c = case
+    st = dict(INPUTS[c["kind"]](c, seed), case=c)
+    if c["kind"] == "norm":
+        shape = (c["rows"], c["dim"])
+        st["y"] = torch.empty(shape, dtype=TYPES[c["out"]], device=DEV)
+        if c["resid"] != "none":
+            st["sum"] = torch.empty(shape, dtype=TYPES[c["resid"]], device=DEV)
+        if c["out"] == "e4m3":
+            st["y_scale"] = torch.empty(c["rows"], dtype=torch.float32, device=DEV)
+    elif c["kind"] == "norm_bwd":
+        st["dx"], st["dgamma"] = torch.empty_like(st["x"]), torch.empty(c["dim"], dtype=torch.float32, device=DEV)
+    elif c["kind"] in ("gated", "gated_train"):
+        t = torch.bfloat16 if c["type"] == "e4m3" else TYPES[c["type"]]
+        st["y"] = torch.empty((c["rows"], c["hidden"]), dtype=t, device=DEV)
+        if c["kind"] == "gated_train":
+            st["pre"] = torch.empty((c["rows"], 2 * c["hidden"]), dtype=t, device=DEV)
+            for n in ("x", "gate_w", "up_w") + (("gate_b", "up_b") if c["bias"] else ()):
+                st["d" + n] = torch.empty_like(st[n])
+    else:
+        st["y"] = torch.zeros((st["x"].shape[0], c["out_dim"]), dtype=TYPES[c["type"]], device=DEV)
+    return st
+
+
+# -- the calls ---------------------------------------------------------------------------------------------------
+
+
+def _workspace(st, nbytes):
+    if "ws" not in st:
+        st["ws"] = torch.empty(nbytes, dtype=torch.uint8, device=DEV)
+    return st["ws"]
+
+
+def _own(st):
+    import paper_2607_11136_amd as X
+    c = st["case"]
+    if c["kind"] == "norm":
+        X.xema_op_rmsnorm(X.rmsnorm_args(st["x"], CODES[c["x"]], c["rows"], c["dim"], st["gamma"], EPS, st["y"], CODES[c["out"]],
+                                         y_scale=st.get("y_scale"), resid=st.get("resid"), resid_dtype=CODES.get(c["resid"], 0),
+                                         sum=st.get("sum"), sum_dtype=CODES.get(c["resid"], 0)))
+        y = st["y"]
+        if c["out"] == "e4m3":
+            y = _values(y, st["y_scale"])
+        return {k: v for k, v in (("y", y), ("scale", st.get("y_scale")), ("sum", st.get("sum"))) if v is not None}
+    if c["kind"] == "norm_bwd":
+        ws = _workspace(st, X.xema_rmsnorm_bwd_workspace_bytes(c["rows"], c["dim"]))
+        t = CODES[c["type"]]
+        X.xema_op_rmsnorm_bwd(X.rmsnorm_bwd_args(st["x"], t, c["rows"], c["dim"], st["gamma"], EPS, st["dy"], t, st["dx"], t,
+                                                 st["dgamma"], ws, ws.numel(), dsum=st["dsum"], dsum_dtype=t))
+        return {"dx": st["dx"], "dgamma": st["dgamma"]}
+    if c["kind"] == "lora":
+        ws = _workspace(st, X.xema_lora_workspace_bytes(st["x"].shape[0], c["rank"]))
+        t = CODES[c["type"]]
+        X.xema_op_lora_linear(X.lora_args(t, st["x"], st["x"].shape[0], c["dim"], st["w"], c["out_dim"], st["bias"], st["a"], st["b"],
+                                          st["scale"], c["rank"], c["adapters"], st["ids"], st["y"], t, ws, ws.numel()))
+        return st["y"]
+    train, t = c["kind"] == "gated_train", CODES[c["type"]]
+    X.xema_op_gated_ffn(X.gated_ffn_args(t, ACTS[c["act"]], st["x"], c["rows"], c["dim"], st["gate_w"], st["up_w"], c["hidden"],
+                                         st["y"], 0 if c["type"] == "e4m3" else t, gate_b=st.get("gate_b"), up_b=st.get("up_b"),
+                                         x_scale=st.get("x_scale"), gate_scale=st.get("gate_scale"), up_scale=st.get("up_scale"),
+                                         pre=st.get("pre")))
+    if not train:
+        return st["y"]
+    ws = _workspace(st, X.xema_gated_ffn_bwd_workspace_bytes(c["rows"], c["dim"], c["hidden"]))
+    X.xema_op_gated_ffn_bwd(X.gated_ffn_bwd_args(t, ACTS[c["act"]], st["x"], c["rows"], c["dim"], st["gate_w"], st["up_w"],
+                                                 c["hidden"], st["pre"], st["dy"], st["dx"], st["dgate_w"], st["dup_w"], ws, ws.numel(),
+                                                 dgate_b=st.get("dgate_b"), dup_b=st.get("dup_b")))
+    return {n: st[n] for n in ("y", "dx", "dgate_w", "dup_w", "dgate_b", "dup_b") if n in st}
+
+
+def _values(codes, scale):
+    """What 8-bit rows stand for; the scales are powers of two, so bfloat16 holds every value."""
+    return (codes.float() * scale[:, None]).bfloat16()
+
+
+def _act(g, name):
+    """(act(g), act'(g))"""
+    if name == "silu":
+        s = torch.sigmoid(g)
+        return g * s, s * (1 + g * (1 - s))
+    a = math.sqrt(2 / math.pi)
+    th = torch.tanh(a * (g + 0.044715 * g * g * g))
+    return 0.5 * g * (1 + th), 0.5 * (1 + th) + 0.5 * g * (1 - th * th) * a * (1 + 3 * 0.044715 * g * g)
+
+
+def _plain(st):
+    c = st["case"]
+    if c["kind"] == "norm":
+        s = st["x"].float()
+        if "resid" in st:
+            s = s + st["resid"].float()
+        y = s * torch.rsqrt((s * s).mean(1, keepdim=True) + EPS) * st["gamma"].float()
+        out = {"sum": s.to(TYPES[c["resid"]])} if "resid" in st else {}
+        if c["out"] != "e4m3":
+            return {"y": y.to(TYPES[c["out"]]), **out}
+        # the smallest power of two 2^k with 448 * 2^k at least the row's largest magnitude
+        m, e = torch.frexp(y.abs().amax(1))
+        scale = torch.ldexp(torch.ones_like(m), torch.clamp_min(e - 9 + (m > 0.875), -126))
+        return {"y": _values((y / scale[:, None]).to(torch.float8_e4m3fn), scale), "scale": scale, **out}
+    if c["kind"] == "norm_bwd":
+        x, dy = st["x"].float(), st["dy"].float()
+        r = torch.rsqrt((x * x).mean(1, keepdim=True) + EPS)
+        n, g = x * r, dy * st["gamma"].float()
+        return {"dx": (r * (g - n * (g * n).mean(1, keepdim=True)) + st["dsum"].float()).to(st["dx"].dtype),
+                "dgamma": (dy * n).sum(0)}
+    if c["kind"] == "lora":
+        x, ids, n = st["x"].float(), st["ids"], c["adapters"]
+        y = x @ st["w"].float().t()
+        if st["bias"] is not None:
+            y = y + st["bias"].float()
+        # every adapter's reduced rows, those of the row's own kept
+        mine = (ids[:, None] == torch.arange(n, device=DEV)[None]) * st["scale"]
+        t = (x @ st["a"].float().flatten(0, 1).t()).view(-1, n, c["rank"]) * mine[:, :, None]
+        y = y + t.flatten(1) @ st["b"].float().transpose(1, 2).flatten(0, 1)
+        return torch.where((ids >= -1)[:, None], y, 0.0).to(st["y"].dtype)
+    x, wg, wu = st["x"].float(), st["gate_w"].float(), st["up_w"].float()
+    if c["type"] == "e4m3":
+        x, wg, wu = x * st["x_scale"][:, None], wg * st["gate_scale"][:, None], wu * st["up_scale"][:, None]
+    g, u = x @ wg.t(), x @ wu.t()
+    if c["bias"]:
+        g, u = g + st["gate_b"].float(), u + st["up_b"].float()
+    a, da = _act(g, c["act"])
+    y = (a * u).to(st["y"].dtype)
+    if c["kind"] == "gated":
+        return y
+    dy, t = st["dy"].float(), st["y"].dtype
+    dg, du = dy * u * da, dy * a
+    out = {"y": y, "dx": (dg @ wg + du @ wu).to(t), "dgate_w": (dg.t() @ x).to(t), "dup_w": (du.t() @ x).to(t)}
+    return {**out, "dgate_b": dg.sum(0).bfloat16(), "dup_b": du.sum(0).bfloat16()} if c["bias"] else out
+
+
+def run(state):
+    return _own(state) if own else _plain(state)
+
+
+def work(case):
+    c = case
+    size = {"bf16": 2, "f16": 2, "f32": 4, "e4m3": 1, "none": 0}
+    if c["kind"] == "norm":
+        n = c["rows"] * c["dim"]
+        return {"bytes": n * (size[c["x"]] + 2 * size[c["resid"]] + size[c["out"]]) + 2 * c["dim"], "flops": 6 * n}
+    if c["kind"] == "norm_bwd":
+        n = c["rows"] * c["dim"]
+        return {"bytes": 8 * n + 6 * c["dim"], "flops": 12 * n}
+    if c["kind"] == "lora":
+        M, D, N, R = c["requests"] * c["tokens"], c["dim"], c["out_dim"], c["rank"]
+        used = min(c["adapters"], c["requests"])
+        return {"bytes": 2 * (M * (D + N) + N * D + used * R * (D + N)), "flops": 2 * M * (N * D + R * (D + N))}
+    M, D, F = c["rows"], c["dim"], c["hidden"]
+    if c["kind"] == "gated":
+        return {"bytes": size[c["type"]] * (M * D + 2 * F * D) + 2 * M * F, "flops": 4 * M * D * F}
+    return {"bytes": 2 * (2 * M * D + 2 * M * F + 4 * F * D), "flops": 12 * M * D * F}
+
+
+# -- the same in 64 bits -----------------------------------------------------------------------------------------
+
+
+def exact(case, seed):
+    c = case
+    d = INPUTS[c["kind"]](c, seed)
+    z = {k: v.double() for k, v in d.items() if v is not None and k != "ids"}
+    if c["kind"] == "norm":
+        s = z["x"] + z["resid"] if "resid" in z else z["x"]
+        y = s / torch.sqrt(s.pow(2).sum(1, keepdim=True) / c["dim"] + EPS) * z["gamma"]
+        out = {"sum": s} if "resid" in z else {}
+        if c["out"] != "e4m3":
+            return {"y": y, **out}
+        top = y.abs().max(1).values
+        scale = torch.exp2(torch.ceil(torch.log2(top / 448)).clamp(min=-126))
+        # e4m3: three bits behind the leading one, steps of 2^-9 below 2^-6
+        v = y / scale[:, None]
+        step = torch.exp2(torch.floor(torch.log2(v.abs().clamp(min=2.0 ** -6))) - 3)
+        return {"y": torch.round(v / step) * step * scale[:, None], "scale": scale, **out}
+    if c["kind"] == "norm_bwd":
+        # y_i = gamma_i x_i / q with q^2 = mean(x^2) + eps: dy_i / dx_j = gamma_i (delta_ij / q - x_i x_j / (dim q^3))
+        q = torch.sqrt(z["x"].pow(2).sum(1, keepdim=True) / c["dim"] + EPS)
+        along = (z["dy"] * z["gamma"] * z["x"]).sum(1, keepdim=True)
+        return {"dx": z["dy"] * z["gamma"] / q - z["x"] * along / (c["dim"] * q ** 3) + z["dsum"],
+                "dgamma": (z["dy"] * z["x"] / q).sum(0)}
+    if c["kind"] == "lora":
+        y = torch.zeros((d["x"].shape[0], c["out_dim"]), dtype=torch.float64, device=DEV)
+        for i in range(-1, c["adapters"]):
+            rows = torch.nonzero(d["ids"] == i)[:, 0]
+            if not len(rows):
+                continue
+            x = z["x"][rows]
+            part = x @ z["w"].t()
+            if i >= 0:
+                part += z["scale"][i] * (x @ z["a"][i].t()) @ z["b"][i].t()
+            if "bias" in z:
+                part += z["bias"]
+            y[rows] = part
+        return y
+    for n in ("x", "gate", "up"):
+        if n + "_scale" in z:
+            z["x" if n == "x" else n + "_w"] *= z[n + "_scale"][:, None]
+    gate = torch.nn.functional.linear(z["x"], z["gate_w"], z.get("gate_b"))
+    up = torch.nn.functional.linear(z["x"], z["up_w"], z.get("up_b"))
+    if c["act"] == "silu":
+        e = torch.exp(-gate)
+        act, slope = gate / (1 + e), (1 + e + gate * e) / (1 + e) ** 2
+        slope = torch.where(gate < -300, 0.0, slope)
+    else:
+        k = math.sqrt(8 / math.pi)     # (1 + tanh(z)) / 2 = 1 / (1 + exp(-2 z))
+        p = 1 / (1 + torch.exp(-k * (gate + 0.044715 * gate ** 3)))
+        act, slope = gate * p, p + gate * p * (1 - p) * k * (1 + 0.134145 * gate ** 2)
+    if c["kind"] == "gated":
+        return act * up
+    dgate, dup = z["dy"] * up * slope, z["dy"] * act
+    out = {"y": act * up, "dx": torch.cat((dgate, dup), 1) @ torch.cat((z["gate_w"], z["up_w"])),
+           "dgate_w": dgate.t().contiguous() @ z["x"], "dup_w": dup.t().contiguous() @ z["x"]}
+    return {**out, "dgate_b": dgate.sum(0), "dup_b": dup.sum(0)} if c["bias"] else out
