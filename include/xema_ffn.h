@@ -1,0 +1,198 @@
+/*
+ * xema_ffn.h -- the operators of a pre-norm gated feed-forward sub-block
+ * (gfx950): RMS norm with the residual's addition, gated feed-forward, and a
+ * projection shared by requests that bring low-rank adapters of their own.
+ *
+ * The block of xema.h has LayerNorm and a GELU MLP.  Denoisers of the same
+ * family, and the text encoders in front of them, use an RMS norm and a gated
+ * feed-forward layer in their place, 8-bit projections where they are served,
+ * and adapters that differ from request to request.  A sub-block is
+ *   xema_op_rmsnorm       h = RMSNorm(x + resid), in 16 bits or in 8 with scales
+ *   xema_op_gated_ffn     g = act(h W_gate^T) * (h W_up^T)
+ *   xema_op_lora_linear   y = g W_down^T + the adapter of each row's request
+ * and xema_op_gated_ffn_bwd and xema_op_rmsnorm_bwd are the gradients of the
+ * first two.
+ *
+ * Conventions are those of xema.h and xema_ops.h: status return, host-side
+ * validation before any launch, caller-owned device buffers, no allocation,
+ * no state between calls, asynchronous on `stream` (a hipStream_t of the
+ * current device, NULL = default stream; XEMA_ERR_INVALID_ARG for a stream of
+ * another device), 16-byte aligned pointers unless stated.  Every entry point
+ * can be captured into a graph; workspaces are scratch memory whose contents
+ * on entry are ignored, and calls that may overlap need one each.  Matrices
+ * are row-major with a leading dimension ("ld", in elements) of at least
+ * their width, below 2^21, whose bytes are a multiple of 16 (so rows start
+ * 16-byte aligned); widths are multiples of 8 (of 16 for XEMA_E4M3 rows) and
+ * at most 131072; row counts are any from 0 (nothing is launched) to
+ * 2^31 - 1024.  Outputs must not overlap inputs, workspaces or each other,
+ * except where an entry point allows it.
+ *
+ * Sums and statistics are fp32 (MFMA accumulators, row sums), each in one
+ * fixed order, with no atomics: the same call gives the same bytes.
+ *
+ * 8-bit values are OCP e4m3 (XEMA_E4M3: largest magnitude 448, no infinity),
+ * with fp32 scales: a row r of a matrix X stands for scale[r] * X[r].
+ */
+#ifndef XEMA_FFN_H_
+#define XEMA_FFN_H_
+
+#include <stdint.h>
+
+#include "xema.h"
+#include "xema_ops.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* RMS norm of x, or of the sum of x and the residual stream:
+ *   s[r] = x[r] + resid[r]                       (resid NULL: s = x)
+ *   y[r][i] = s[r][i] / sqrt(mean_j s[r][j]^2 + eps) * gamma[i]
+ * s is the fp32 sum: `sum` (may be NULL) receives it in sum_dtype, and y
+ * comes from the fp32 value, not from the stored one.
+ * x, resid and sum are each XEMA_BF16, XEMA_F16 or XEMA_F32 [rows, dim];
+ * gamma is bf16 [dim] (NULL: ones); `sum` may be x or resid itself (the same
+ * pointer, type and ld): an update of the residual stream in place.
+ * y is XEMA_BF16 or XEMA_F16, or XEMA_E4M3 with y_scale[rows]:
+ *   y_scale[r] = 2^k, the smallest with |y[r][i]| <= 448 * 2^k for all i and
+ *   k >= -126; the code of y[r][i] is y[r][i] / 2^k rounded to nearest even.
+ * A power of two makes that division exact and costs an e4m3 code no
+ * precision, being itself a floating-point value.  A row that holds a NaN or
+ * an infinity (in s or y) gets NaN as its scale, and NaN codes.  In 16 bits
+ * such a row's values are those of the formula.
+ * dim is a multiple of 8 (of 16 with XEMA_E4M3), at most 16384.             */
+typedef struct {
+  int64_t rows; int32_t dim;
+  const void* x; int32_t x_dtype; int64_t ldx;
+  const void* resid; int32_t resid_dtype; int64_t ld_resid;
+  void* sum; int32_t sum_dtype; int64_t ld_sum;
+  const void* gamma;
+  float eps;
+  void* y; int32_t y_dtype; int64_t ldy;
+  float* y_scale;
+} xema_rmsnorm_args;
+
+XEMA_API int xema_op_rmsnorm(const xema_rmsnorm_args* args, void* stream);
+
+/* Gradient of xema_op_rmsnorm with 16-bit output, for s the norm's input (x,
+ * or the stored sum) and dy the gradient that reaches y:
+ *   q = 1 / sqrt(mean_j s_j^2 + eps),  n = s q,  g = dy * gamma
+ *   dx[r][i] = q (g_i - n_i mean_j(g_j n_j)) + dsum[r][i]
+ *   dgamma[i] = sum over rows of dy[r][i] n[r][i]
+ * dsum (may be NULL) is the gradient that reaches s by itself, through the
+ * residual stream; dx is then the gradient of both x and resid.
+ * s, dy, dsum and dx are each XEMA_BF16, XEMA_F16 or XEMA_F32 [rows, dim];
+ * dgamma fp32 [dim] (may be NULL), zeros where rows is 0; gamma as above.
+ * dx may be dy, dsum or s itself (the same pointer, type and ld).
+ * The workspace (16-byte aligned) has at least
+ * xema_rmsnorm_bwd_workspace_bytes(rows, dim) bytes; without dgamma it may
+ * be NULL.                                                                  */
+typedef struct {
+  int64_t rows; int32_t dim;
+  const void* s; int32_t s_dtype; int64_t ld_s;
+  const void* dy; int32_t dy_dtype; int64_t ld_dy;
+  const void* dsum; int32_t dsum_dtype; int64_t ld_dsum;
+  const void* gamma;
+  float eps;
+  void* dx; int32_t dx_dtype; int64_t ld_dx;
+  float* dgamma;
+  void* workspace; int64_t workspace_bytes;
+} xema_rmsnorm_bwd_args;
+
+XEMA_API int xema_rmsnorm_bwd_workspace_bytes(int64_t rows, int32_t dim, int64_t* bytes);
+XEMA_API int xema_op_rmsnorm_bwd(const xema_rmsnorm_bwd_args* args, void* stream);
+
+typedef enum { XEMA_ACT_SILU = 0, XEMA_ACT_GELU_TANH = 1 } xema_act;
+
+/* Gated feed-forward, both projections, the activation and the product in
+ * one kernel:
+ *   g = x gate_w^T + gate_b,  u = x up_w^T + up_b,  y = act(g) * u
+ * with act(g) = g / (1 + e^-g) or GELU's tanh form.  x [rows, dim]; gate_w
+ * and up_w [hidden, dim] contiguous (one [2 hidden, dim] tensor is two
+ * pointers into it); gate_b, up_b bf16 [hidden], each may be NULL.
+ * dtype XEMA_BF16 or XEMA_F16: x and the weights have that type, and y too
+ * (y_dtype = dtype).  dtype XEMA_E4M3: x and the weights are e4m3 with scales
+ * x_scale [rows], gate_scale and up_scale [hidden] (fp32, 4-byte aligned), and
+ * y is XEMA_BF16 or XEMA_F16.  The products are summed in fp32 and nothing is
+ * rounded before y.  pre (may be NULL; 16-bit dtypes only) receives what the
+ * gradient needs: [rows, 2 hidden] contiguous in `dtype`, a row g then u.  */
+typedef struct {
+  int32_t dtype, act;
+  int64_t rows; int32_t dim, hidden;
+  const void* x; int64_t ldx; const float* x_scale;
+  const void *gate_w, *up_w; const float *gate_scale, *up_scale;
+  const void *gate_b, *up_b;
+  void* y; int32_t y_dtype; int64_t ldy;
+  void* pre;
+} xema_gated_ffn_args;
+
+XEMA_API int xema_op_gated_ffn(const xema_gated_ffn_args* args, void* stream);
+
+/* Gradient of xema_op_gated_ffn (dtype XEMA_BF16 or XEMA_F16) for dy, the
+ * gradient that reaches y:
+ *   dg = dy * u * act'(g),  du = dy * act(g)       (g, u from pre)
+ *   dx = dg gate_w + du up_w                        [rows, dim]
+ *   dgate_w = dg^T x,  dup_w = du^T x               [hidden, dim] contiguous
+ *   dgate_b, dup_b = column sums of dg, du          bf16 [hidden]
+ * x, dy, dx, pre, the weights and their gradients have type `dtype`.  Each of
+ * dx, the pair dgate_w and dup_w, and the pair dgate_b and dup_b may be NULL
+ * (not all).  dg and du are formed in fp32 and rounded to `dtype` once, for
+ * the products; the column sums take the fp32 values.  Where rows is 0 the
+ * gradients of weights and biases are zeros.  The workspace (256-byte
+ * aligned) has at least xema_gated_ffn_bwd_workspace_bytes(rows, dim, hidden)
+ * bytes.                                                                    */
+typedef struct {
+  int32_t dtype, act;
+  int64_t rows; int32_t dim, hidden;
+  const void* x; int64_t ldx;
+  const void *gate_w, *up_w;
+  const void* pre;
+  const void* dy; int64_t ld_dy;
+  void* dx; int64_t ld_dx;
+  void *dgate_w, *dup_w;
+  void *dgate_b, *dup_b;
+  void* workspace; int64_t workspace_bytes;
+} xema_gated_ffn_bwd_args;
+
+XEMA_API int xema_gated_ffn_bwd_workspace_bytes(int64_t rows, int32_t dim, int32_t hidden, int64_t* bytes);
+XEMA_API int xema_op_gated_ffn_bwd(const xema_gated_ffn_bwd_args* args, void* stream);
+
+/* A projection shared by all requests, with a low-rank adapter per row:
+ *   y[r] = x[r] w^T + bias + scale[i] (x[r] a[i]^T) b[i]^T,   i = row_adapter[r]
+ * x [rows, dim]; w [out_dim, dim], a [n_adapters, rank, dim] and
+ * b [n_adapters, out_dim, rank] contiguous, all of type `dtype` (XEMA_BF16 or
+ * XEMA_F16); bias bf16 [out_dim] (may be NULL); scale fp32 [n_adapters]
+ * (4-byte aligned); y [rows, out_dim] of type y_dtype (XEMA_BF16 or XEMA_F16).
+ * row_adapter int32 [rows] (4-byte aligned), on the device: the rows of a
+ * prompt name the same adapter, those of a batch of single tokens one each,
+ * in any order.  An id of
+ *   0 .. n_adapters - 1   selects that adapter,
+ *   -1                    none: the shared projection alone,
+ *   below -1              a padding row: its y stays as it was,
+ *   n_adapters or more    is a mistake: its y becomes NaN.
+ * rank is a multiple of 8 up to 128 (smaller ranks are padded with zeros, in
+ * a or in b); n_adapters may be 0 (a, b and scale are then not read).
+ * x[r] a[i]^T is summed in fp32, scaled, and carried as two values of `dtype`,
+ * its rounding and the rounding of what that leaves (16 significant bits in
+ * bf16), through the workspace (256-byte aligned, at least
+ * xema_lora_workspace_bytes(rows, rank) bytes).                              */
+typedef struct {
+  int32_t dtype;
+  int64_t rows; int32_t dim, out_dim;
+  const void* x; int64_t ldx;
+  const void* w; const void* bias;
+  const void *a, *b; const float* scale;
+  int32_t rank, n_adapters;
+  const int32_t* row_adapter;
+  void* y; int32_t y_dtype; int64_t ldy;
+  void* workspace; int64_t workspace_bytes;
+} xema_lora_args;
+
+XEMA_API int xema_lora_workspace_bytes(int64_t rows, int32_t rank, int64_t* bytes);
+XEMA_API int xema_op_lora_linear(const xema_lora_args* args, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* XEMA_FFN_H_ */

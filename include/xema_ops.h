@@ -26,7 +26,8 @@
 extern "C" {
 #endif
 
-typedef enum { XEMA_BF16 = 0, XEMA_F16 = 1, XEMA_F32 = 2 } xema_dtype;
+/* (XEMA_E4M3: the operators of xema_ffn.h alone) */
+typedef enum { XEMA_BF16 = 0, XEMA_F16 = 1, XEMA_F32 = 2, XEMA_E4M3 = 3 } xema_dtype;
 
 /* Row map used for chunked access to [B, L, ...] tensors: GEMM/LN row r
  * (0 <= r < rows) belongs to batch element b = r / rows_per_batch and maps to

@@ -33,7 +33,7 @@ XEMA_MAX_SLOTS = 16
 XEMA_CHUNK_GRANULE = 256
 XEMA_SEQ_PAD = 128
 
-XEMA_BF16, XEMA_F16, XEMA_F32 = 0, 1, 2
+XEMA_BF16, XEMA_F16, XEMA_F32, XEMA_E4M3 = 0, 1, 2, 3
 XEMA_EPI_BIAS, XEMA_EPI_BIAS_GELU, XEMA_EPI_GATED_RESIDUAL = 0, 1, 2
 
 SLOT_NAMES = ("mod", "rope", "q", "k", "vt", "ln1", "qkv", "wo16", "wup16", "wdown16",
@@ -126,6 +126,47 @@ class StepPlan(ctypes.Structure):
 
 _P = ctypes.c_void_p
 _I32, _I64, _F32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+
+
+class RmsnormArgs(ctypes.Structure):
+    _fields_ = [("rows", _I64), ("dim", _I32), ("x", _P), ("x_dtype", _I32), ("ldx", _I64),
+                ("resid", _P), ("resid_dtype", _I32), ("ld_resid", _I64),
+                ("sum", _P), ("sum_dtype", _I32), ("ld_sum", _I64), ("gamma", _P), ("eps", _F32),
+                ("y", _P), ("y_dtype", _I32), ("ldy", _I64), ("y_scale", _P)]
+
+
+class RmsnormBwdArgs(ctypes.Structure):
+    _fields_ = [("rows", _I64), ("dim", _I32), ("s", _P), ("s_dtype", _I32), ("ld_s", _I64),
+                ("dy", _P), ("dy_dtype", _I32), ("ld_dy", _I64),
+                ("dsum", _P), ("dsum_dtype", _I32), ("ld_dsum", _I64), ("gamma", _P), ("eps", _F32),
+                ("dx", _P), ("dx_dtype", _I32), ("ld_dx", _I64), ("dgamma", _P),
+                ("workspace", _P), ("workspace_bytes", _I64)]
+
+
+XEMA_ACT_SILU, XEMA_ACT_GELU_TANH = 0, 1
+
+
+class GatedFfnArgs(ctypes.Structure):
+    _fields_ = [("dtype", _I32), ("act", _I32), ("rows", _I64), ("dim", _I32), ("hidden", _I32),
+                ("x", _P), ("ldx", _I64), ("x_scale", _P), ("gate_w", _P), ("up_w", _P),
+                ("gate_scale", _P), ("up_scale", _P), ("gate_b", _P), ("up_b", _P),
+                ("y", _P), ("y_dtype", _I32), ("ldy", _I64), ("pre", _P)]
+
+
+class GatedFfnBwdArgs(ctypes.Structure):
+    _fields_ = [("dtype", _I32), ("act", _I32), ("rows", _I64), ("dim", _I32), ("hidden", _I32),
+                ("x", _P), ("ldx", _I64), ("gate_w", _P), ("up_w", _P), ("pre", _P),
+                ("dy", _P), ("ld_dy", _I64), ("dx", _P), ("ld_dx", _I64), ("dgate_w", _P), ("dup_w", _P),
+                ("dgate_b", _P), ("dup_b", _P), ("workspace", _P), ("workspace_bytes", _I64)]
+
+
+class LoraArgs(ctypes.Structure):
+    _fields_ = [("dtype", _I32), ("rows", _I64), ("dim", _I32), ("out_dim", _I32), ("x", _P), ("ldx", _I64),
+                ("w", _P), ("bias", _P), ("a", _P), ("b", _P), ("scale", _P), ("rank", _I32), ("n_adapters", _I32),
+                ("row_adapter", _P), ("y", _P), ("y_dtype", _I32), ("ldy", _I64),
+                ("workspace", _P), ("workspace_bytes", _I64)]
+
+
 _SIGNATURES = {
     "xema_status_str": (ctypes.c_char_p, [ctypes.c_int]),
     "xema_request_from_template": (ctypes.c_int, [ctypes.POINTER(BlockCfg), _I32, _I32, _I32, _I32,
@@ -181,6 +222,19 @@ _SIGNATURES = {
 }
 EXPORTED = tuple(_SIGNATURES)
 
+# the feed-forward sub-block's operators (include/xema_ffn.h)
+_FFN_SIGNATURES = {
+    "xema_op_rmsnorm": (ctypes.c_int, [ctypes.POINTER(RmsnormArgs), _P]),
+    "xema_rmsnorm_bwd_workspace_bytes": (ctypes.c_int, [_I64, _I32, ctypes.POINTER(_I64)]),
+    "xema_op_rmsnorm_bwd": (ctypes.c_int, [ctypes.POINTER(RmsnormBwdArgs), _P]),
+    "xema_op_gated_ffn": (ctypes.c_int, [ctypes.POINTER(GatedFfnArgs), _P]),
+    "xema_gated_ffn_bwd_workspace_bytes": (ctypes.c_int, [_I64, _I32, _I32, ctypes.POINTER(_I64)]),
+    "xema_op_gated_ffn_bwd": (ctypes.c_int, [ctypes.POINTER(GatedFfnBwdArgs), _P]),
+    "xema_lora_workspace_bytes": (ctypes.c_int, [_I64, _I32, ctypes.POINTER(_I64)]),
+    "xema_op_lora_linear": (ctypes.c_int, [ctypes.POINTER(LoraArgs), _P]),
+}
+EXPORTED_FFN = tuple(_FFN_SIGNATURES)
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -192,7 +246,7 @@ def lib() -> ctypes.CDLL:
             raise RuntimeError(f"{LIB_PATH} is missing: build it with "
                                "`python -m paper_2607_11136_amd.build` (needs hipcc)")
         l = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in _SIGNATURES.items():
+        for name, (res, args) in {**_SIGNATURES, **_FFN_SIGNATURES}.items():
             f = getattr(l, name)
             f.restype = res
             f.argtypes = args
@@ -531,3 +585,83 @@ def xema_vae_upconv(x, n: int, h: int, w: int, ci: int, wp, bias, co: int, row_b
                     row_count: int, y, stream=None) -> None:
     _check(lib().xema_vae_upconv(_ptr(x), n, h, w, ci, _ptr(wp), _ptr(bias), co, row_begin, row_count,
                                  _ptr(y), _stream(stream)), "xema_vae_upconv")
+
+
+# -- the feed-forward sub-block's operators (include/xema_ffn.h) ----------------------------------
+
+
+def rmsnorm_args(x, x_dtype: int, rows: int, dim: int, gamma, eps: float, y, y_dtype: int, y_scale=None, resid=None,
+                 resid_dtype: int = XEMA_BF16, sum=None, sum_dtype: int = XEMA_BF16, ldx: int = 0, ld_resid: int = 0,
+                 ld_sum: int = 0, ldy: int = 0) -> RmsnormArgs:
+    """Leading dimensions of 0 stand for dim."""
+    return RmsnormArgs(rows, dim, _ptr(x), x_dtype, ldx or dim, _ptr(resid), resid_dtype, ld_resid or dim, _ptr(sum), sum_dtype,
+                       ld_sum or dim, _ptr(gamma), eps, _ptr(y), y_dtype, ldy or dim, _ptr(y_scale))
+
+
+def xema_op_rmsnorm(args: RmsnormArgs, stream=None) -> None:
+    _check(lib().xema_op_rmsnorm(ctypes.byref(args), _stream(stream)), "xema_op_rmsnorm")
+
+
+def rmsnorm_bwd_args(s, s_dtype: int, rows: int, dim: int, gamma, eps: float, dy, dy_dtype: int, dx, dx_dtype: int, dgamma=None,
+                     workspace=None, workspace_bytes: int = 0, dsum=None, dsum_dtype: int = XEMA_BF16, ld_s: int = 0,
+                     ld_dy: int = 0, ld_dsum: int = 0, ld_dx: int = 0) -> RmsnormBwdArgs:
+    """Leading dimensions of 0 stand for dim."""
+    return RmsnormBwdArgs(rows, dim, _ptr(s), s_dtype, ld_s or dim, _ptr(dy), dy_dtype, ld_dy or dim, _ptr(dsum), dsum_dtype,
+                          ld_dsum or dim, _ptr(gamma), eps, _ptr(dx), dx_dtype, ld_dx or dim, _ptr(dgamma), _ptr(workspace),
+                          int(workspace_bytes))
+
+
+def xema_rmsnorm_bwd_workspace_bytes(rows: int, dim: int) -> int:
+    n = _I64()
+    _check(lib().xema_rmsnorm_bwd_workspace_bytes(rows, dim, ctypes.byref(n)), "xema_rmsnorm_bwd_workspace_bytes")
+    return n.value
+
+
+def xema_op_rmsnorm_bwd(args: RmsnormBwdArgs, stream=None) -> None:
+    _check(lib().xema_op_rmsnorm_bwd(ctypes.byref(args), _stream(stream)), "xema_op_rmsnorm_bwd")
+
+
+def gated_ffn_args(dtype: int, act: int, x, rows: int, dim: int, gate_w, up_w, hidden: int, y, y_dtype: int, gate_b=None, up_b=None,
+                   x_scale=None, gate_scale=None, up_scale=None, pre=None, ldx: int = 0, ldy: int = 0) -> GatedFfnArgs:
+    """Leading dimensions of 0 stand for the width."""
+    return GatedFfnArgs(dtype, act, rows, dim, hidden, _ptr(x), ldx or dim, _ptr(x_scale), _ptr(gate_w), _ptr(up_w), _ptr(gate_scale),
+                        _ptr(up_scale), _ptr(gate_b), _ptr(up_b), _ptr(y), y_dtype, ldy or hidden, _ptr(pre))
+
+
+def xema_op_gated_ffn(args: GatedFfnArgs, stream=None) -> None:
+    _check(lib().xema_op_gated_ffn(ctypes.byref(args), _stream(stream)), "xema_op_gated_ffn")
+
+
+def gated_ffn_bwd_args(dtype: int, act: int, x, rows: int, dim: int, gate_w, up_w, hidden: int, pre, dy, dx, dgate_w, dup_w, workspace,
+                       workspace_bytes: int, dgate_b=None, dup_b=None, ldx: int = 0, ld_dy: int = 0, ld_dx: int = 0) -> GatedFfnBwdArgs:
+    """Leading dimensions of 0 stand for the width."""
+    return GatedFfnBwdArgs(dtype, act, rows, dim, hidden, _ptr(x), ldx or dim, _ptr(gate_w), _ptr(up_w), _ptr(pre), _ptr(dy),
+                           ld_dy or hidden, _ptr(dx), ld_dx or dim, _ptr(dgate_w), _ptr(dup_w), _ptr(dgate_b), _ptr(dup_b),
+                           _ptr(workspace), int(workspace_bytes))
+
+
+def xema_gated_ffn_bwd_workspace_bytes(rows: int, dim: int, hidden: int) -> int:
+    n = _I64()
+    _check(lib().xema_gated_ffn_bwd_workspace_bytes(rows, dim, hidden, ctypes.byref(n)), "xema_gated_ffn_bwd_workspace_bytes")
+    return n.value
+
+
+def xema_op_gated_ffn_bwd(args: GatedFfnBwdArgs, stream=None) -> None:
+    _check(lib().xema_op_gated_ffn_bwd(ctypes.byref(args), _stream(stream)), "xema_op_gated_ffn_bwd")
+
+
+def lora_args(dtype: int, x, rows: int, dim: int, w, out_dim: int, bias, a, b, scale, rank: int, n_adapters: int, row_adapter, y,
+              y_dtype: int, workspace, workspace_bytes: int, ldx: int = 0, ldy: int = 0) -> LoraArgs:
+    """Leading dimensions of 0 stand for the width."""
+    return LoraArgs(dtype, rows, dim, out_dim, _ptr(x), ldx or dim, _ptr(w), _ptr(bias), _ptr(a), _ptr(b), _ptr(scale), rank, n_adapters,
+                    _ptr(row_adapter), _ptr(y), y_dtype, ldy or out_dim, _ptr(workspace), int(workspace_bytes))
+
+
+def xema_lora_workspace_bytes(rows: int, rank: int) -> int:
+    n = _I64()
+    _check(lib().xema_lora_workspace_bytes(rows, rank, ctypes.byref(n)), "xema_lora_workspace_bytes")
+    return n.value
+
+
+def xema_op_lora_linear(args: LoraArgs, stream=None) -> None:
+    _check(lib().xema_op_lora_linear(ctypes.byref(args), _stream(stream)), "xema_op_lora_linear")

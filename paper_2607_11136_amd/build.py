@@ -21,7 +21,7 @@ ARCH = "gfx950"
 
 SOURCES = ["plan.cpp", "k_elementwise.hip", "k_gemm.hip", "k_attention.hip", "block.hip", "step.hip",
            "k_upconv.hip", "vae.hip", "static_arena.hip",
-           "step_plan.cpp"]
+           "step_plan.cpp", "k_norm.hip", "k_ffn.hip", "k_lora.hip", "ffn.hip"]
 
 # Packed fp32 VALU forms are kept out of the generated code.
 HIPCC_FLAGS = ["-O3", "-fPIC", "-std=c++17", f"--offload-arch={ARCH}", "-I" + INCLUDE,

@@ -1,0 +1,349 @@
+// Gated feed-forward on gfx950 MFMA, forward and gradient (xema_ffn.h).
+#include <algorithm>
+
+#include "device_common.h"
+#include "ffn.h"
+#include "mma_tile.h"
+
+namespace xema {
+
+namespace {
+
+typedef TileShape<256, 256, 2, 4, 2> Big;
+typedef TileShape<128, 128, 2, 2, 3> Mid;
+typedef TileShape<64, 64, 2, 2, 4> Small;
+
+// act(g), and act'(g) where asked.  GELU's tanh form is g p with
+// p = 1 / (1 + e^(-2z)), z = sqrt(2/pi) (g + 0.044715 g^3), so its slope is
+// p + g p (1 - p) 2 z'; past |g| = 30 p is 0 or 1 in fp32 and the second term 0.
+template <bool SLOPE>
+__device__ __forceinline__ float activate(float g, int act, float* slope) {
+  constexpr float LOG2E = 1.4426950408889634f;
+  if (act == XEMA_ACT_SILU) {
+    const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-LOG2E * g));
+    if (SLOPE) *slope = s * fmaf(g, 1.0f - s, 1.0f);
+    return g * s;
+  }
+  constexpr float A2 = 2.0f * 0.7978845608028654f;
+  const float p = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-A2 * LOG2E * fmaf(0.044715f * g, g * g, g)));
+  if (SLOPE) {
+    const float c = fminf(fmaxf(g, -30.0f), 30.0f);
+    *slope = fmaf(c * p * (1.0f - p), A2 * fmaf(3.0f * 0.044715f * c, c, 1.0f), p);
+  }
+  return g * p;
+}
+
+struct GatedParams {
+  const void* x; const float* x_scale;
+  const void *gate_w, *up_w; const float *gate_scale, *up_scale;
+  const uint16_t *gate_b, *up_b;
+  void* y; void* pre;
+  int64_t rows, ldx, ldy;
+  int dim, hidden, act;
+};
+
+// y = act(x Wg^T + bg) * (x Wu^T + bu).  A tile's columns are gate and up rows
+// of the same hidden units, half and half within each wave, so that a lane
+// holds both factors of its outputs and the product needs no exchange.
+template <typename T, typename YT, typename S>
+__global__ __launch_bounds__(S::NW * 64, 1) void k_gated(GatedParams p) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[S::LDS];
+  constexpr int HN = S::BN / 2, NB = S::NJ / 2;      // hidden units per tile, blocks per wave
+  const int tiles_n = (p.hidden + HN - 1) / HN, tiles_m = (int)((p.rows + S::BM - 1) / S::BM);
+  int tm, tn;
+  tile_of((int)blockIdx.x, tiles_m, tiles_n, 1024 / S::BM, &tm, &tn);
+  const int64_t m0 = (int64_t)tm * S::BM;
+  const int n0 = tn * HN;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kbytes = p.dim * (int)sizeof(T);
+
+  RowOperand<S::BM, S::NW> a;
+  PairOperand<S::BN, S::NW, S::WC> b;
+  a.init((const T*)p.x + m0 * p.ldx, nullptr, p.rows - m0, p.ldx * sizeof(T), kbytes, 0x7fffffff, wave, lane);
+  b.init((const T*)p.gate_w + (int64_t)n0 * p.dim, (const T*)p.up_w + (int64_t)n0 * p.dim, p.hidden - n0, kbytes, kbytes, wave, lane);
+  f32x4 acc[S::MI][S::NJ];
+#pragma unroll
+  for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  tile_products<S, T, ROWS, ROWS>(a, b, (kbytes + KB - 1) / KB, smem, wave, lane, acc);
+
+  const int l16 = lane & 15, l4 = lane >> 4;
+  const int col0 = n0 + wave % S::WNW * (S::WC / 2);
+  float sg[NB][4], su[NB][4], bg[NB][4], bu[NB][4];
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int col = min(col0 + 16 * j + 4 * l4 + e, p.hidden - 1);
+      if (sizeof(T) == 1) {
+        sg[j][e] = p.gate_scale[col];
+        su[j][e] = p.up_scale[col];
+      }
+      bg[j][e] = p.gate_b ? bf16_bits_to_f32(p.gate_b[col]) : 0.f;
+      bu[j][e] = p.up_b ? bf16_bits_to_f32(p.up_b[col]) : 0.f;
+    }
+#pragma unroll
+  for (int i = 0; i < S::MI; ++i) {
+    const int64_t m = m0 + wave / S::WNW * S::WR + 16 * i + l16;
+    const bool valid = m < p.rows;
+    const int64_t mv = valid ? m : p.rows - 1;
+    const float sx = sizeof(T) == 1 ? p.x_scale[mv] : 1.f;
+    float g[NB][4], u[NB][4], y[NB][4];
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        g[j][e] = acc[i][j][e];
+        u[j][e] = acc[i][NB + j][e];
+        if (sizeof(T) == 1) {
+          g[j][e] *= sx * sg[j][e];
+          u[j][e] *= sx * su[j][e];
+        }
+        g[j][e] += bg[j][e];
+        u[j][e] += bu[j][e];
+        y[j][e] = activate<false>(g[j][e], p.act, nullptr) * u[j][e];
+      }
+    store_row<YT, NB>((YT*)p.y + mv * p.ldy, col0, p.hidden, y, l4, valid);
+    if (sizeof(T) == 2 && p.pre) {
+      YT* row = (YT*)p.pre + mv * 2 * p.hidden;
+      store_row<YT, NB>(row, col0, p.hidden, g, l4, valid);
+      store_row<YT, NB>(row + p.hidden, col0, p.hidden, u, l4, valid);
+    }
+  }
+}
+
+template <typename T, typename YT, typename S>
+hipError_t run_gated(const GatedParams& p, hipStream_t s) {
+  const int64_t tiles = (p.rows + S::BM - 1) / S::BM * ((p.hidden + S::BN / 2 - 1) / (S::BN / 2));
+  hipLaunchKernelGGL((k_gated<T, YT, S>), dim3((unsigned)tiles), dim3(S::NW * 64), 0, s, p);
+  return hipGetLastError();
+}
+
+enum TileKind { BIG, MID, SMALL };
+// v1: the largest tile that still gives each CU one
+TileKind pick_tile(int64_t m, int64_t n) {
+  auto tiles = [&](int t) { return (m + t - 1) / t * ((n + t - 1) / t); };
+  return tiles(256) >= 192 ? BIG : tiles(128) >= 192 ? MID : SMALL;
+}
+
+template <typename T, typename YT>
+hipError_t gated_t(const GatedParams& p, hipStream_t s) {
+  switch (pick_tile(p.rows, 2 * (int64_t)p.hidden)) {
+    case BIG: return run_gated<T, YT, Big>(p, s);
+    case MID: return run_gated<T, YT, Mid>(p, s);
+    default: return run_gated<T, YT, Small>(p, s);
+  }
+}
+
+// dg = dy u act'(g), du = dy act(g), rounded to T, and the column sums of the
+// rounded-free values over each chunk of rows.  A workgroup takes 256 columns,
+// 8 a thread, of `chunk` rows, 8 rows at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void k_gated_grad(const T* __restrict__ pre, const T* __restrict__ dy, int64_t ld_dy, int64_t rows,
+                                                    int hidden, int act, int chunk, T* __restrict__ dg, T* __restrict__ du,
+                                                    float* __restrict__ partial) {
+  typedef T t8 __attribute__((ext_vector_type(8)));
+  __shared__ float red[8][2][256 + 8];
+  const int c8 = threadIdx.x & 31, r8 = threadIdx.x >> 5;
+  const int col = (int)blockIdx.x * 256 + c8 * 8;
+  const bool in = col < hidden;
+  const int64_t r0 = (int64_t)blockIdx.y * chunk, r1 = r0 + chunk < rows ? r0 + chunk : rows;
+  float sg[8], su[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sg[e] = su[e] = 0.f;
+  if (in)
+    for (int64_t r = r0 + r8; r < r1; r += 8) {
+      const t8 g = *reinterpret_cast<const t8*>(pre + r * 2 * hidden + col);
+      const t8 u = *reinterpret_cast<const t8*>(pre + r * 2 * hidden + hidden + col);
+      const t8 d = *reinterpret_cast<const t8*>(dy + r * ld_dy + col);
+      t8 og, ou;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float slope;
+        const float a = activate<true>((float)g[e], act, &slope), df = (float)d[e];
+        const float vg = df * (float)u[e] * slope, vu = df * a;
+        sg[e] += vg;
+        su[e] += vu;
+        og[e] = (T)vg;
+        ou[e] = (T)vu;
+      }
+      *reinterpret_cast<t8*>(dg + r * hidden + col) = og;
+      *reinterpret_cast<t8*>(du + r * hidden + col) = ou;
+    }
+  if (!partial) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    red[r8][0][c8 * 8 + e] = sg[e];
+    red[r8][1][c8 * 8 + e] = su[e];
+  }
+  __syncthreads();
+  const int c = (int)blockIdx.x * 256 + threadIdx.x;
+  if (c < hidden) {
+    float a = 0.f, b = 0.f;
+    for (int r = 0; r < 8; ++r) {
+      a += red[r][0][threadIdx.x];
+      b += red[r][1][threadIdx.x];
+    }
+    partial[(int64_t)blockIdx.y * 2 * hidden + c] = a;
+    partial[(int64_t)blockIdx.y * 2 * hidden + hidden + c] = b;
+  }
+}
+
+// The chunks' column sums, in order, as bf16.
+__global__ __launch_bounds__(256) void k_gated_bias(const float* __restrict__ partial, int chunks, int hidden, uint16_t* __restrict__ dgate_b,
+                                                    uint16_t* __restrict__ dup_b) {
+  const int c = (int)blockIdx.x * 256 + threadIdx.x;
+  if (c >= 2 * hidden) return;
+  float v = 0.f;
+  for (int i = 0; i < chunks; ++i) v += partial[(int64_t)i * 2 * hidden + c];
+  (c < hidden ? dgate_b + c : dup_b + (c - hidden))[0] = __builtin_bit_cast(uint16_t, (bf16)v);
+}
+
+struct BwdParams {
+  const void *dg, *du;          // [rows, hidden]
+  const void *gate_w, *up_w;    // [hidden, dim]
+  const void* x;
+  void *dx, *dgate_w, *dup_w;
+  int64_t rows, ldx, ld_dx;
+  int dim, hidden;
+};
+
+// dx = dg Wg + du Wu: the weights are read k by k (a row of W is one k).
+template <typename T, typename S>
+__global__ __launch_bounds__(S::NW * 64, 1) void k_gated_dx(BwdParams p) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[S::LDS];
+  const int tiles_n = (p.dim + S::BN - 1) / S::BN, tiles_m = (int)((p.rows + S::BM - 1) / S::BM);
+  int tm, tn;
+  tile_of((int)blockIdx.x, tiles_m, tiles_n, 1024 / S::BM, &tm, &tn);
+  const int64_t m0 = (int64_t)tm * S::BM;
+  const int n0 = tn * S::BN;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int steps = (p.hidden + 63) / 64;
+  RowOperand<S::BM, S::NW> a;
+  ColumnOperand<S::BN, S::NW> b;
+  a.init((const T*)p.dg + m0 * p.hidden, (const T*)p.du + m0 * p.hidden, p.rows - m0, (int64_t)p.hidden * 2, p.hidden * 2, steps, wave, lane);
+  b.init((const T*)p.gate_w + n0, (const T*)p.up_w + n0, p.dim - n0, (int64_t)p.dim * 2, p.hidden, steps, wave, lane);
+  f32x4 acc[S::MI][S::NJ];
+#pragma unroll
+  for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  tile_products<S, T, ROWS, COLUMNS>(a, b, 2 * steps, smem, wave, lane, acc);
+  const int l16 = lane & 15, l4 = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < S::MI; ++i) {
+    const int64_t m = m0 + wave / S::WNW * S::WR + 16 * i + l16;
+    const bool valid = m < p.rows;
+    float v[S::NJ][4];
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[j][e] = acc[i][j][e];
+    store_row<T, S::NJ>((T*)p.dx + (valid ? m : 0) * p.ld_dx, n0 + wave % S::WNW * S::WC, p.dim, v, l4, valid);
+  }
+}
+
+// dWg = dg^T x and dWu = du^T x: both operands are read k (row) by k.
+template <typename T, typename S>
+__global__ __launch_bounds__(S::NW * 64, 1) void k_gated_dw(BwdParams p) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[S::LDS];
+  const int tiles_n = (p.dim + S::BN - 1) / S::BN, tiles_h = (p.hidden + S::BM - 1) / S::BM;
+  int tm, tn;
+  tile_of((int)blockIdx.x, 2 * tiles_h, tiles_n, 1024 / S::BM, &tm, &tn);
+  const bool up = tm >= tiles_h;
+  const int m0 = (up ? tm - tiles_h : tm) * S::BM, n0 = tn * S::BN;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  ColumnOperand<S::BM, S::NW> a;
+  ColumnOperand<S::BN, S::NW> b;
+  a.init((const T*)(up ? p.du : p.dg) + m0, nullptr, p.hidden - m0, (int64_t)p.hidden * 2, p.rows, 0x7fffffff, wave, lane);
+  b.init((const T*)p.x + n0, nullptr, p.dim - n0, p.ldx * 2, p.rows, 0x7fffffff, wave, lane);
+  f32x4 acc[S::MI][S::NJ];
+#pragma unroll
+  for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  tile_products<S, T, COLUMNS, COLUMNS>(a, b, (int)((p.rows + 63) / 64), smem, wave, lane, acc);
+  T* out = (T*)(up ? p.dup_w : p.dgate_w);
+  const int l16 = lane & 15, l4 = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < S::MI; ++i) {
+    const int m = m0 + wave / S::WNW * S::WR + 16 * i + l16;
+    const bool valid = m < p.hidden;
+    float v[S::NJ][4];
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[j][e] = acc[i][j][e];
+    store_row<T, S::NJ>(out + (int64_t)(valid ? m : 0) * p.dim, n0 + wave % S::WNW * S::WC, p.dim, v, l4, valid);
+  }
+}
+
+template <typename T, typename S>
+hipError_t run_dx(const BwdParams& p, hipStream_t s) {
+  const int64_t tiles = (p.rows + S::BM - 1) / S::BM * ((p.dim + S::BN - 1) / S::BN);
+  hipLaunchKernelGGL((k_gated_dx<T, S>), dim3((unsigned)tiles), dim3(S::NW * 64), 0, s, p);
+  return hipGetLastError();
+}
+
+template <typename T, typename S>
+hipError_t run_dw(const BwdParams& p, hipStream_t s) {
+  const int64_t tiles = 2 * ((p.hidden + S::BM - 1) / S::BM) * ((p.dim + S::BN - 1) / S::BN);
+  hipLaunchKernelGGL((k_gated_dw<T, S>), dim3((unsigned)tiles), dim3(S::NW * 64), 0, s, p);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t bwd_t(const xema_gated_ffn_bwd_args& a, hipStream_t s) {
+  const int64_t part = (a.rows * a.hidden * 2 + 255) / 256 * 256;
+  uint8_t* ws = (uint8_t*)a.workspace;
+  T *dg = (T*)ws, *du = (T*)(ws + part);
+  float* partial = a.dgate_b ? (float*)(ws + 2 * part) : nullptr;
+  const int chunks = (int)gated_bwd_row_chunks(a.rows);
+  hipError_t e = hipSuccess;
+  if (a.rows > 0) {
+    const int chunk = (int)((a.rows + chunks - 1) / chunks);
+    hipLaunchKernelGGL((k_gated_grad<T>), dim3((a.hidden + 255) / 256, chunks), dim3(256), 0, s, (const T*)a.pre, (const T*)a.dy, a.ld_dy,
+                       a.rows, a.hidden, a.act, chunk, dg, du, partial);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (a.dgate_b) {
+    hipLaunchKernelGGL(k_gated_bias, dim3((2 * a.hidden + 255) / 256), dim3(256), 0, s, partial, a.rows > 0 ? chunks : 0, a.hidden,
+                       (uint16_t*)a.dgate_b, (uint16_t*)a.dup_b);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  const BwdParams p{dg, du, a.gate_w, a.up_w, a.x, a.dx, a.dgate_w, a.dup_w, a.rows, a.ldx, a.ld_dx, a.dim, a.hidden};
+  if (a.dx && a.rows > 0) {
+    switch (pick_tile(a.rows, a.dim)) {
+      case BIG: e = run_dx<T, Big>(p, s); break;
+      case MID: e = run_dx<T, Mid>(p, s); break;
+      default: e = run_dx<T, Small>(p, s); break;
+    }
+    if (e != hipSuccess) return e;
+  }
+  if (a.dgate_w) {
+    switch (pick_tile(2 * (int64_t)a.hidden, a.dim)) {
+      case BIG: return run_dw<T, Big>(p, s);
+      case MID: return run_dw<T, Mid>(p, s);
+      default: return run_dw<T, Small>(p, s);
+    }
+  }
+  return e;
+}
+
+}  // namespace
+
+hipError_t launch_gated_ffn(const xema_gated_ffn_args& a, hipStream_t s) {
+  const GatedParams p{a.x, a.x_scale, a.gate_w, a.up_w, a.gate_scale, a.up_scale, (const uint16_t*)a.gate_b, (const uint16_t*)a.up_b,
+                      a.y, a.pre, a.rows, a.ldx, a.ldy, a.dim, a.hidden, a.act};
+  if (a.dtype == XEMA_E4M3) return a.y_dtype == XEMA_BF16 ? gated_t<e4m3, bf16>(p, s) : gated_t<e4m3, f16>(p, s);
+  return a.dtype == XEMA_BF16 ? gated_t<bf16, bf16>(p, s) : gated_t<f16, f16>(p, s);
+}
+
+int64_t gated_bwd_row_chunks(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(64, (rows + 63) / 64)); }
+
+hipError_t launch_gated_ffn_bwd(const xema_gated_ffn_bwd_args& a, hipStream_t s) {
+  return a.dtype == XEMA_BF16 ? bwd_t<bf16>(a, s) : bwd_t<f16>(a, s);
+}
+
+}  // namespace xema

@@ -1,0 +1,321 @@
+// One output tile of a matrix product on MFMA, for operands in either order,
+// widths that no tile divides and 16-bit or e4m3 elements: C[m][n] = sum over
+// k of A(m, k) B(n, k).
+//
+// Both operands go through LDS in steps of 128 bytes of k a row (64 16-bit or
+// 128 8-bit elements), loaded straight from memory (buffer_load ... lds).  An
+// operand stored row by row with k contiguous ("rows") keeps 128-byte LDS rows
+// in eight 16-byte slots, slot j of row r at j ^ ((r >> 1) & 7), so that the
+// 16 rows that a fragment read meets lie in other banks.  An operand stored k
+// by k ("columns": a gradient's transposed product) keeps its k rows, and
+// fragments come through the transposing LDS read (ds_read_b64_tr_b16: 16
+// lanes read 4 k rows of 16 columns, each lane receives one column's four k);
+// its 32-byte chunks are permuted by the k row, so that the eight k rows that
+// 32 lanes meet lie in other banks.
+//
+// Everything past an operand's end is read as zero: rows and columns by a
+// per-lane offset that the buffer's range check refuses, k of the last step
+// likewise.  No load leaves the operand.
+#pragma once
+
+#include "device_common.h"
+#include "mma.h"
+
+namespace xema {
+
+struct e4m3 { uint8_t bits; };
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int KB = 128;                       // bytes of k per row and step
+constexpr uint32_t OUT_OF_RANGE = 0x80000000u;
+constexpr int64_t MAX_RECORDS = 0x7ffffff0;   // of a buffer: below OUT_OF_RANGE
+
+enum OperandOrder { ROWS, COLUMNS };
+
+// 16-byte loads of an LDS tile of R rows, a row of memory being k.
+template <int R, int NW>
+struct RowLoads {
+  static constexpr int LOADS = R / 8 / NW;    // 1 KiB loads per wave and step
+  static_assert(LOADS * 8 * NW == R, "load split");
+  uint32_t off[LOADS];
+  uint32_t slot[2];                           // byte of k of this lane's slot, even and odd loads
+  // row `i` of the tile lies at (i * ld) bytes, for i < valid
+  __device__ __forceinline__ void init(int valid, uint32_t ld, int wave, int lane) {
+#pragma unroll
+    for (int c = 0; c < LOADS; ++c) {
+      const int row = (wave * LOADS + c) * 8 + lane / 8;
+      const uint32_t s = ((lane % 8) ^ row_swz(row)) * 16;
+      if (c < 2) slot[c] = s;
+      off[c] = row < valid ? row * ld + s : OUT_OF_RANGE;
+    }
+    if (LOADS == 1) slot[1] = slot[0];
+  }
+  __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t r, int c, int kt, int kbytes, uint8_t* st, int wave) const {
+    // (a step past the last one, which the pipeline's ring asks for, has no k in
+    // range; its scalar offset is 0, as the range check may subtract that)
+    const int k0 = kt * KB;
+    uint32_t v = off[c];
+    if (k0 + KB > kbytes) v = k0 + (int)slot[c & 1] < kbytes ? v : OUT_OF_RANGE;
+    load_lds16(r, st + (wave * LOADS + c) * 1024, v, k0 < kbytes ? (uint32_t)k0 : 0u);
+  }
+};
+
+// Chunk permutation of a k row of `COLS` 16-bit columns (see the file comment).
+template <int COLS>
+__device__ __forceinline__ int chunk_swz(int k) {
+  return COLS >= 128 ? (k & 3) | ((k >> 3) & 1) << 2 : ((k >> 1) & 1) | ((k >> 3) & 1) << 1;
+}
+
+// The same for a tile of 64 k rows of C columns, 16 bits each.
+template <int C, int NW>
+struct ColumnLoads {
+  static constexpr int RB = C * 2, RPL = 1024 / RB;
+  static constexpr int LOADS = C / 8 / NW;
+  static_assert(LOADS * 8 * NW == C, "load split");
+  uint32_t off[LOADS];
+  // column i < valid of k row j lies at j * ld + 2 i bytes
+  __device__ __forceinline__ void init(int valid, uint32_t ld, int wave, int lane) {
+#pragma unroll
+    for (int c = 0; c < LOADS; ++c) {
+      const int k = (wave * LOADS + c) * RPL + lane * 16 / RB;
+      const int at = lane * 16 % RB;
+      const int col = ((at / 32) ^ chunk_swz<C>(k)) * 16 + (at % 32) / 2;
+      off[c] = col < valid ? k * ld + col * 2 : OUT_OF_RANGE;
+    }
+  }
+  // `left`: k rows from this step on (its k rows past the last are out of range)
+  __device__ __forceinline__ void issue(const uint8_t* base, uint32_t ld, int64_t left, int c, uint8_t* st, int wave) const {
+    const int64_t bytes = left <= 0 ? 0 : left * ld;
+    load_lds16(make_rsrc(base, bytes < MAX_RECORDS ? bytes : MAX_RECORDS), st + (wave * LOADS + c) * 1024, off[c], 0);
+  }
+};
+
+// An operand for the main loop: N rows of the tile (output rows or columns),
+// in one or two parts along k.  begin() is called once per step, then issue()
+// for each of the LOADS loads.
+template <int N, int NW>
+struct RowOperand {
+  static constexpr int LOADS = RowLoads<N, NW>::LOADS;
+  RowLoads<N, NW> l;
+  const uint8_t *p0, *p1;
+  int64_t bytes;
+  int kbytes, steps0;
+  // rows from `part0` (and, from step `steps0` on, `part1`), `valid` of them
+  __device__ __forceinline__ void init(const void* part0, const void* part1, int64_t valid, int64_t ld_bytes, int kbytes_,
+                                       int steps0_, int wave, int lane) {
+    const int v = valid < N ? (int)valid : N;
+    l.init(v, (uint32_t)ld_bytes, wave, lane);
+    p0 = (const uint8_t*)part0; p1 = (const uint8_t*)part1;
+    bytes = v * ld_bytes;
+    kbytes = kbytes_; steps0 = steps0_;
+  }
+  __device__ __forceinline__ void issue(int kt, int c, uint8_t* st, int wave) const {
+    const bool second = kt >= steps0;
+    l.issue(make_rsrc(second ? p1 : p0, bytes), c, second ? kt - steps0 : kt, kbytes, st, wave);
+  }
+};
+
+template <int N, int NW>
+struct ColumnOperand {
+  static constexpr int LOADS = ColumnLoads<N, NW>::LOADS;
+  ColumnLoads<N, NW> l;
+  const uint8_t *p0, *p1;
+  int64_t k;
+  uint32_t ld;
+  int steps0;
+  __device__ __forceinline__ void init(const void* part0, const void* part1, int64_t valid, int64_t ld_bytes, int64_t k_,
+                                       int steps0_, int wave, int lane) {
+    ld = (uint32_t)ld_bytes;
+    l.init(valid < N ? (int)valid : N, ld, wave, lane);
+    p0 = (const uint8_t*)part0; p1 = (const uint8_t*)part1;
+    k = k_; steps0 = steps0_;
+  }
+  __device__ __forceinline__ void issue(int kt, int c, uint8_t* st, int wave) const {
+    const bool second = kt >= steps0;
+    const int64_t k0 = (int64_t)(second ? kt - steps0 : kt) * 64;
+    l.issue((second ? p1 : p0) + k0 * ld, ld, k - k0, c, st, wave);
+  }
+};
+
+// Rows of two matrices side by side: of every WC rows of the tile (one wave's
+// columns of the output) the first half comes from p0, the second from p1.
+template <int N, int NW, int WC>
+struct PairOperand {
+  static constexpr int LOADS = RowLoads<N, NW>::LOADS;
+  RowLoads<N, NW> l;
+  const uint8_t *p0, *p1;
+  int64_t bytes;
+  int kbytes;
+  __device__ __forceinline__ void init(const void* part0, const void* part1, int64_t valid, int64_t ld_bytes, int kbytes_,
+                                       int wave, int lane) {
+    l.init(N, 0, wave, lane);
+#pragma unroll
+    for (int c = 0; c < LOADS; ++c) {
+      const int row = (wave * LOADS + c) * 8 + lane / 8;
+      const int src = row / WC * (WC / 2) + row % (WC / 2);
+      l.off[c] = src < valid ? src * (uint32_t)ld_bytes + l.slot[c & 1] : OUT_OF_RANGE;
+    }
+    p0 = (const uint8_t*)part0; p1 = (const uint8_t*)part1;
+    bytes = (valid < N / 2 ? valid : N / 2) * ld_bytes;
+    kbytes = kbytes_;
+  }
+  __device__ __forceinline__ void issue(int kt, int c, uint8_t* st, int wave) const {
+    const bool second = ((wave * LOADS + c) * 8 / (WC / 2)) & 1;
+    l.issue(make_rsrc(second ? p1 : p0, bytes), c, kt, kbytes, st, wave);
+  }
+};
+
+// Fragment reads: 16 rows (or columns) of a tile for one MFMA.
+template <typename T>
+struct Frag {
+  typedef typename Mfma<T>::frag type;
+  static constexpr int KK = 2;                // MFMA k-steps per step
+  static __device__ __forceinline__ f32x4 run(type a, type b, f32x4 c) { return Mfma<T>::run16(a, b, c); }
+};
+template <>
+struct Frag<e4m3> {
+  typedef i32x8 type;
+  static constexpr int KK = 1;
+  // one 16x16x128 MFMA, unscaled (scale operands 0)
+  static __device__ __forceinline__ f32x4 run(type a, type b, f32x4 c) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
+  }
+};
+
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) i16x4* lds_i16x4_t;
+
+template <typename T, int N, OperandOrder ORDER>
+struct FragReader {
+  typedef typename Frag<T>::type frag;
+  uint32_t base;
+  // fragments of the rows row0 + 16 i (row0 a multiple of 16)
+  __device__ __forceinline__ void init(int row0, int lane) {
+    const int l16 = lane & 15, l4 = lane >> 4;
+    if (ORDER == ROWS) {
+      base = (row0 + l16) * KB + ((l4 ^ (l16 >> 1)) * 16);
+    } else {
+      const int k = l4 * 8 + (l16 >> 2);
+      base = k * (N * 2) + (((row0 / 16) ^ chunk_swz<N>(k)) * 32) + (l16 & 3) * 8;
+    }
+  }
+  __device__ __forceinline__ frag read(const uint8_t* st, int kk, int i) const {
+    if constexpr (ORDER == ROWS) {
+      if constexpr (sizeof(T) == 1) {
+        // 32 of a row's 128 k's: the slots l4 and 4 + l4, of both operands alike
+        const u32x4 a = *reinterpret_cast<const u32x4*>(st + base + i * 16 * KB);
+        const u32x4 b = *reinterpret_cast<const u32x4*>(st + (base ^ 64) + i * 16 * KB);
+        return frag{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+      } else {
+        return *reinterpret_cast<const frag*>(st + (base ^ (64 * kk)) + i * 16 * KB);
+      }
+    } else {
+      const uint8_t* p = st + (base ^ (32 * i)) + kk * 32 * N * 2;
+      const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t)p);
+      const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t)(p + 4 * N * 2));
+      const i16x8 v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+      return __builtin_bit_cast(frag, v);
+    }
+  }
+};
+
+// The tile's shape: BM x BN in WMW x WNW waves, NS stages of both operands.
+template <int BM_, int BN_, int WMW_, int WNW_, int NS_>
+struct TileShape {
+  static constexpr int BM = BM_, BN = BN_, WMW = WMW_, WNW = WNW_, NS = NS_;
+  static constexpr int NW = WMW * WNW, WR = BM / WMW, WC = BN / WNW, MI = WR / 16, NJ = WC / 16;
+  static constexpr int A_BYTES = BM * KB, B_BYTES = BN * KB, STAGE = A_BYTES + B_BYTES;
+  static constexpr int LDS = NS * STAGE;
+};
+
+// acc += the tile's products over `steps` steps.  Fragments: the B operand's
+// is the MFMA's first, so that a lane ends with four consecutive columns of
+// one row: acc[i][j][e] is row wm WR + 16 i + lane % 16, column
+// wn WC + 16 j + 4 (lane / 16) + e.
+template <typename S, typename T, OperandOrder AO, OperandOrder BO, typename AOp, typename BOp>
+__device__ __forceinline__ void tile_products(const AOp& a, const BOp& b, int steps, uint8_t* smem, int wave, int lane,
+                                              f32x4 (&acc)[S::MI][S::NJ]) {
+  constexpr int LPS = AOp::LOADS + BOp::LOADS, KK = Frag<T>::KK;
+  FragReader<T, S::BM, AO> ra;
+  FragReader<T, S::BN, BO> rb;
+  ra.init(wave / S::WNW * S::WR, lane);
+  rb.init(wave % S::WNW * S::WC, lane);
+  auto issue = [&](int kt, int s) {
+    uint8_t* st = smem + s * S::STAGE;
+#pragma unroll
+    for (int c = 0; c < AOp::LOADS; ++c) a.issue(kt, c, st, wave);
+#pragma unroll
+    for (int c = 0; c < BOp::LOADS; ++c) b.issue(kt, c, st + S::A_BYTES, wave);
+  };
+#pragma unroll
+  for (int s = 0; s < S::NS - 1; ++s) issue(s, s);
+  int cur = 0, fill = S::NS - 1;
+  for (int kt = 0; kt < steps; ++kt) {
+    // step kt has landed (the NS - 2 steps after it may be in flight), and
+    // every wave has read step kt - 1, whose stage step kt + NS - 1 takes
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm((S::NS - 2) * LPS));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    issue(kt + S::NS - 1, fill);
+    const uint8_t* st = smem + cur * S::STAGE;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+      typename Frag<T>::type fa[S::MI], fb[S::NJ];
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) fb[j] = rb.read(st + S::A_BYTES, kk, j);
+#pragma unroll
+      for (int i = 0; i < S::MI; ++i) fa[i] = ra.read(st, kk, i);
+#pragma unroll
+      for (int i = 0; i < S::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j) acc[i][j] = Frag<T>::run(fb[j], fa[i], acc[i][j]);
+    }
+    cur = cur + 1 == S::NS ? 0 : cur + 1;
+    fill = fill + 1 == S::NS ? 0 : fill + 1;
+  }
+  // the loads that ran ahead still write to LDS: let them finish
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+}
+
+// Tile (tm, tn) of workgroup wg among tiles_m x tiles_n: each XCD (wg % 8)
+// walks a contiguous range, `group` tile rows at a time, so that the tiles it
+// runs at once share operand panels in its L2.
+__device__ __forceinline__ void tile_of(int wg, int tiles_m, int tiles_n, int group, int* tm, int* tn) {
+  const int total = tiles_m * tiles_n, xcd = wg & 7, slot = wg >> 3;
+  const int per = total >> 3, rem = total & 7;
+  const int t = xcd * per + min(xcd, rem) + slot;
+  const int g = t / (group * tiles_n), first = g * group;
+  const int size = min(tiles_m - first, group);
+  const int in = t - g * group * tiles_n;
+  *tm = first + in % size;
+  *tn = in / size;
+}
+
+// Up to 32 columns of one row (NB 16-column blocks of a wave, a lane holding
+// columns 4 l4 .. + 3 of each) as 16-bit values; blocks whose 8 columns lie
+// past `cols` are not written (cols a multiple of 8).
+template <typename CT, int NB>
+__device__ __forceinline__ void store_row(CT* row, int col0, int cols, const float (&v)[NB][4], int l4, bool valid) {
+  typedef CT c4 __attribute__((ext_vector_type(4)));
+  c4 o[NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[j][e] = from_f32<CT>(v[j][e]);
+  if constexpr (NB % 2 == 0) {
+#pragma unroll
+    for (int j = 0; j < NB; j += 2)
+      store_block_pair<CT>(row + col0 + 16 * j, o[j], o[j + 1], l4,
+                           valid && col0 + 16 * j + 16 * (l4 & 1) + 8 * (l4 >> 1) < cols);
+  } else {
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      if (valid && col0 + 16 * j + 4 * l4 < cols) *reinterpret_cast<c4*>(row + col0 + 16 * j + 4 * l4) = o[j];
+  }
+}
+
+}  // namespace xema
