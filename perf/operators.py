@@ -231,6 +231,8 @@ def _own(st):
                                           st["scale"], c["rank"], c["adapters"], st["ids"], st["y"], t, ws, ws.numel()))
         return st["y"]
     train, t = c["kind"] == "gated_train", CODES[c["type"]]
+    if train and st["pre"].dtype != torch.uint8:     # the library keeps g and u in 24 bits each
+        st["pre"] = torch.empty(X.xema_gated_ffn_pre_bytes(c["rows"], c["hidden"]), dtype=torch.uint8, device=DEV)
     X.xema_op_gated_ffn(X.gated_ffn_args(t, ACTS[c["act"]], st["x"], c["rows"], c["dim"], st["gate_w"], st["up_w"], c["hidden"],
                                          st["y"], 0 if c["type"] == "e4m3" else t, gate_b=st.get("gate_b"), up_b=st.get("up_b"),
                                          x_scale=st.get("x_scale"), gate_scale=st.get("gate_scale"), up_scale=st.get("up_scale"),
