@@ -114,8 +114,13 @@ typedef enum { XEMA_ACT_SILU = 0, XEMA_ACT_GELU_TANH = 1 } xema_act;
  * (y_dtype = dtype).  dtype XEMA_E4M3: x and the weights are e4m3 with scales
  * x_scale [rows], gate_scale and up_scale [hidden] (fp32, 4-byte aligned), and
  * y is XEMA_BF16 or XEMA_F16.  The products are summed in fp32 and nothing is
- * rounded before y.  pre (may be NULL; 16-bit dtypes only) receives what the
- * gradient needs: [rows, 2 hidden] contiguous in `dtype`, a row g then u.  */
+ * rounded before y.  pre (may be NULL; 16-bit dtypes only; 16-byte aligned)
+ * receives what the gradient needs, g and u as 24-bit floating-point values
+ * (the upper 24 bits of fp32: its range, 16 significant bits) in
+ * xema_gated_ffn_pre_bytes(rows, hidden) bytes.  A layout for
+ * xema_op_gated_ffn_bwd alone: per row and four hidden units 24 bytes, the
+ * upper halves of g, those of u (four uint16 each), then their third bytes.
+ * (16-bit values there would double the error of every gradient.)           */
 typedef struct {
   int32_t dtype, act;
   int64_t rows; int32_t dim, hidden;
@@ -126,6 +131,7 @@ typedef struct {
   void* pre;
 } xema_gated_ffn_args;
 
+XEMA_API int xema_gated_ffn_pre_bytes(int64_t rows, int32_t hidden, int64_t* bytes);
 XEMA_API int xema_op_gated_ffn(const xema_gated_ffn_args* args, void* stream);
 
 /* Gradient of xema_op_gated_ffn (dtype XEMA_BF16 or XEMA_F16) for dy, the
@@ -134,7 +140,8 @@ XEMA_API int xema_op_gated_ffn(const xema_gated_ffn_args* args, void* stream);
  *   dx = dg gate_w + du up_w                        [rows, dim]
  *   dgate_w = dg^T x,  dup_w = du^T x               [hidden, dim] contiguous
  *   dgate_b, dup_b = column sums of dg, du          bf16 [hidden]
- * x, dy, dx, pre, the weights and their gradients have type `dtype`.  Each of
+ * pre is xema_op_gated_ffn's, of the same sizes, or laid out alike.
+ * x, dy, dx, the weights and their gradients have type `dtype`.  Each of
  * dx, the pair dgate_w and dup_w, and the pair dgate_b and dup_b may be NULL
  * (not all).  dg and du are formed in fp32 and rounded to `dtype` once, for
  * the products; the column sums take the fp32 values.  Where rows is 0 the

@@ -227,6 +227,7 @@ _FFN_SIGNATURES = {
     "xema_op_rmsnorm": (ctypes.c_int, [ctypes.POINTER(RmsnormArgs), _P]),
     "xema_rmsnorm_bwd_workspace_bytes": (ctypes.c_int, [_I64, _I32, ctypes.POINTER(_I64)]),
     "xema_op_rmsnorm_bwd": (ctypes.c_int, [ctypes.POINTER(RmsnormBwdArgs), _P]),
+    "xema_gated_ffn_pre_bytes": (ctypes.c_int, [_I64, _I32, ctypes.POINTER(_I64)]),
     "xema_op_gated_ffn": (ctypes.c_int, [ctypes.POINTER(GatedFfnArgs), _P]),
     "xema_gated_ffn_bwd_workspace_bytes": (ctypes.c_int, [_I64, _I32, _I32, ctypes.POINTER(_I64)]),
     "xema_op_gated_ffn_bwd": (ctypes.c_int, [ctypes.POINTER(GatedFfnBwdArgs), _P]),
@@ -626,6 +627,12 @@ def gated_ffn_args(dtype: int, act: int, x, rows: int, dim: int, gate_w, up_w, h
     """Leading dimensions of 0 stand for the width."""
     return GatedFfnArgs(dtype, act, rows, dim, hidden, _ptr(x), ldx or dim, _ptr(x_scale), _ptr(gate_w), _ptr(up_w), _ptr(gate_scale),
                         _ptr(up_scale), _ptr(gate_b), _ptr(up_b), _ptr(y), y_dtype, ldy or hidden, _ptr(pre))
+
+
+def xema_gated_ffn_pre_bytes(rows: int, hidden: int) -> int:
+    n = _I64()
+    _check(lib().xema_gated_ffn_pre_bytes(rows, hidden, ctypes.byref(n)), "xema_gated_ffn_pre_bytes")
+    return n.value
 
 
 def xema_op_gated_ffn(args: GatedFfnArgs, stream=None) -> None:

@@ -148,7 +148,7 @@ int check_gated(const xema_gated_ffn_args* a) {
   const int64_t F = a->hidden, wb = F * a->dim * elem(a->dtype);
   const Span x = matrix(a->x, a->dtype, a->rows, a->dim, a->ldx), gw{a->gate_w, wb}, uw{a->up_w, wb};
   const Span gb{a->gate_b, 2 * F}, ub{a->up_b, 2 * F}, y = matrix(a->y, a->y_dtype, a->rows, F, a->ldy);
-  const Span pre = matrix(a->pre, a->y_dtype, a->rows, 2 * F, 2 * F);
+  const Span pre{a->pre, 6 * a->rows * F};
   const Span xs{f8 ? a->x_scale : nullptr, 4 * a->rows}, gs{f8 ? a->gate_scale : nullptr, 4 * F}, us{f8 ? a->up_scale : nullptr, 4 * F};
   if (any_overlap(y, {x, gw, uw, gb, ub, pre, xs, gs, us}) || any_overlap(pre, {x, gw, uw, gb, ub})) return XEMA_ERR_INVALID_ARG;
   return XEMA_OK;
@@ -174,7 +174,7 @@ int check_gated_bwd(const xema_gated_ffn_bwd_args* a) {
   XEMA_CHECK(xema_gated_ffn_bwd_workspace_bytes(a->rows, a->dim, a->hidden, &need));
   if (a->workspace_bytes < need) return XEMA_ERR_WORKSPACE_TOO_SMALL;
   const Span x = matrix(a->x, a->dtype, a->rows, D, a->ldx), gw{a->gate_w, F * D * 2}, uw{a->up_w, F * D * 2};
-  const Span pre = matrix(a->pre, a->dtype, a->rows, 2 * F, 2 * F), dy = matrix(a->dy, a->dtype, a->rows, F, a->ld_dy);
+  const Span pre{a->pre, 6 * a->rows * F}, dy = matrix(a->dy, a->dtype, a->rows, F, a->ld_dy);
   const Span dx = matrix(a->dx, a->dtype, a->rows, D, a->ld_dx), dgw{a->dgate_w, F * D * 2}, duw{a->dup_w, F * D * 2};
   const Span dgb{a->dgate_b, 2 * F}, dub{a->dup_b, 2 * F}, ws{a->workspace, need};
   if (any_overlap(ws, {x, gw, uw, pre, dy, dx, dgw, duw, dgb, dub}) || any_overlap(dx, {x, gw, uw, pre, dy, dgw, duw, dgb, dub}) ||
@@ -239,6 +239,14 @@ extern "C" int xema_op_gated_ffn(const xema_gated_ffn_args* args, void* stream) 
   if (args->rows == 0) return XEMA_OK;
   XEMA_CHECK(check_stream(stream));
   return hip_status(launch_gated_ffn(*args, (hipStream_t)stream));
+}
+
+extern "C" int xema_gated_ffn_pre_bytes(int64_t rows, int32_t hidden, int64_t* bytes) {
+  if (!bytes) return XEMA_ERR_INVALID_ARG;
+  XEMA_CHECK(check_rows(rows));
+  XEMA_CHECK(check_width(hidden, XEMA_BF16));
+  *bytes = 6 * rows * hidden;
+  return XEMA_OK;
 }
 
 extern "C" int xema_gated_ffn_bwd_workspace_bytes(int64_t rows, int32_t dim, int32_t hidden, int64_t* bytes) {

@@ -33,6 +33,41 @@ __device__ __forceinline__ float activate(float g, int act, float* slope) {
   return g * p;
 }
 
+// The stored g and u: the upper 24 bits of fp32, rounded to nearest even
+// (infinities and NaN keep their upper bits, and a NaN stays one).  Four units
+// take 24 bytes: upper halves of g, of u, third bytes of g, of u.
+constexpr int PRE_GROUP = 24;
+__device__ __forceinline__ uint32_t round24(float v) {
+  const uint32_t b = __float_as_uint(v);
+  if ((b & 0x7f800000u) == 0x7f800000u) return b | (b & 0x7fffffu ? 0x400000u : 0u);
+  return b + 0x7fu + (b >> 8 & 1u);
+}
+__device__ __forceinline__ void store_pre(uint8_t* at, const float g[4], const float u[4]) {
+  uint32_t r[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    r[e] = round24(g[e]);
+    r[4 + e] = round24(u[e]);
+  }
+  u32x2 w[3];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) w[h][e] = __builtin_amdgcn_perm(r[4 * h + 2 * e + 1], r[4 * h + 2 * e], 0x07060302u);
+    uint32_t low = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) low |= (r[4 * h + e] >> 8 & 0xffu) << (8 * e);
+    w[2][h] = low;
+  }
+#pragma unroll
+  for (int i = 0; i < 3; ++i) reinterpret_cast<u32x2*>(at)[i] = w[i];
+}
+// Element e of one of the two, from its upper halves and third bytes.
+__device__ __forceinline__ float load24(const uint32_t* upper, uint32_t low, int e) {
+  const uint32_t hi = e & 1 ? upper[e >> 1] & 0xffff0000u : upper[e >> 1] << 16;
+  return __uint_as_float(hi | (low >> (8 * e) & 0xffu) << 8);
+}
+
 struct GatedParams {
   const void* x; const float* x_scale;
   const void *gate_w, *up_w; const float *gate_scale, *up_scale;
@@ -106,9 +141,11 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_gated(GatedParams p) {
       }
     store_row<YT, NB>((YT*)p.y + mv * p.ldy, col0, p.hidden, y, l4, valid);
     if (sizeof(T) == 2 && p.pre) {
-      YT* row = (YT*)p.pre + mv * 2 * p.hidden;
-      store_row<YT, NB>(row, col0, p.hidden, g, l4, valid);
-      store_row<YT, NB>(row + p.hidden, col0, p.hidden, u, l4, valid);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const int unit = col0 + 16 * j + 4 * l4;
+        if (valid && unit < p.hidden) store_pre((uint8_t*)p.pre + (m * p.hidden + unit) / 4 * PRE_GROUP, g[j], u[j]);
+      }
     }
   }
 }
@@ -140,7 +177,7 @@ hipError_t gated_t(const GatedParams& p, hipStream_t s) {
 // rounded-free values over each chunk of rows.  A workgroup takes 256 columns,
 // 8 a thread, of `chunk` rows, 8 rows at a time.
 template <typename T>
-__global__ __launch_bounds__(256) void k_gated_grad(const T* __restrict__ pre, const T* __restrict__ dy, int64_t ld_dy, int64_t rows,
+__global__ __launch_bounds__(256) void k_gated_grad(const uint8_t* __restrict__ pre, const T* __restrict__ dy, int64_t ld_dy, int64_t rows,
                                                     int hidden, int act, int chunk, T* __restrict__ dg, T* __restrict__ du,
                                                     float* __restrict__ partial) {
   typedef T t8 __attribute__((ext_vector_type(8)));
@@ -154,15 +191,21 @@ __global__ __launch_bounds__(256) void k_gated_grad(const T* __restrict__ pre, c
   for (int e = 0; e < 8; ++e) sg[e] = su[e] = 0.f;
   if (in)
     for (int64_t r = r0 + r8; r < r1; r += 8) {
-      const t8 g = *reinterpret_cast<const t8*>(pre + r * 2 * hidden + col);
-      const t8 u = *reinterpret_cast<const t8*>(pre + r * 2 * hidden + hidden + col);
+      uint32_t w[12];
+      const u32x4* at = reinterpret_cast<const u32x4*>(pre + (r * hidden + col) / 4 * PRE_GROUP);
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[4 * i + e] = at[i][e];
       const t8 d = *reinterpret_cast<const t8*>(dy + r * ld_dy + col);
       t8 og, ou;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         float slope;
-        const float a = activate<true>((float)g[e], act, &slope), df = (float)d[e];
-        const float vg = df * (float)u[e] * slope, vu = df * a;
+        const uint32_t* four = w + e / 4 * 6;
+        const float g = load24(four, four[4], e % 4), u = load24(four + 2, four[5], e % 4);
+        const float a = activate<true>(g, act, &slope), df = (float)d[e];
+        const float vg = df * u * slope, vu = df * a;
         sg[e] += vg;
         su[e] += vu;
         og[e] = (T)vg;
@@ -303,7 +346,7 @@ hipError_t bwd_t(const xema_gated_ffn_bwd_args& a, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (a.rows > 0) {
     const int chunk = (int)((a.rows + chunks - 1) / chunks);
-    hipLaunchKernelGGL((k_gated_grad<T>), dim3((a.hidden + 255) / 256, chunks), dim3(256), 0, s, (const T*)a.pre, (const T*)a.dy, a.ld_dy,
+    hipLaunchKernelGGL((k_gated_grad<T>), dim3((a.hidden + 255) / 256, chunks), dim3(256), 0, s, (const uint8_t*)a.pre, (const T*)a.dy, a.ld_dy,
                        a.rows, a.hidden, a.act, chunk, dg, du, partial);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }

@@ -219,6 +219,31 @@ def gated_inputs(rows, dim, hidden, dtype, bias, seed):
     return x, wg, wu, bg, bu
 
 
+def pack24(t):
+    """[rows, 2 hidden] (g, then u) in fp32, rounded to 24 bits, as xema_op_gated_ffn stores them."""
+    rows, hidden = t.shape[0], t.shape[1] // 2
+    b = t.float().view(torch.int32)
+    b = (b + 0x7F + ((b >> 8) & 1)) & -256
+    q = b.view(rows, 2, hidden // 4, 4).transpose(1, 2).contiguous()      # [rows, groups, (g, u), 4]
+    upper = ((q >> 16) & 0xFFFF).to(torch.int16).view(torch.uint8).view(rows, hidden // 4, 16)
+    low = ((q >> 8) & 0xFF).to(torch.uint8).view(rows, hidden // 4, 8)
+    return torch.cat((upper, low), 2).contiguous().view(rows, 6 * hidden)
+
+
+def unpack24(pre, hidden):
+    """What such bytes stand for, [rows, 2 hidden]."""
+    p = pre.view(-1, hidden // 4, 24)
+    rows = p.shape[0]
+    upper = p[:, :, :16].contiguous().view(torch.int16).view(rows, -1, 2, 4).to(torch.int32)
+    b = (upper << 16) | (p[:, :, 16:].contiguous().view(rows, -1, 2, 4).to(torch.int32) << 8)
+    return b.view(torch.float32).transpose(1, 2).reshape(rows, 2 * hidden)
+
+
+def empty_pre(rows, hidden):
+    assert X.xema_gated_ffn_pre_bytes(rows, hidden) == 6 * rows * hidden
+    return empty(rows, 6 * hidden, 0, torch.uint8)
+
+
 def run_gated(x, wg, wu, bg, bu, act, y, pre=None, stream=None):
     rows, dim, hidden = x.shape[0], x.shape[1], wg.shape[0]
     X.xema_op_gated_ffn(X.gated_ffn_args(CODE[x.dtype], act, x, rows, dim, wg, wu, hidden, y, CODE[y.dtype], gate_b=bg, up_b=bu, pre=pre,
@@ -229,12 +254,13 @@ def run_gated(x, wg, wu, bg, bu, act, y, pre=None, stream=None):
 @pytest.mark.parametrize("dtype,act,bias", [(BF16, 0, False), (F16, 1, True), (BF16, 1, True), (F16, 0, False)])
 def test_gated_ffn(rows, dim, hidden, dtype, act, bias):
     x, wg, wu, bg, bu = gated_inputs(rows, dim, hidden, dtype, bias, rows + dim)
-    y, pre = empty(rows, hidden, 16, dtype), empty(rows, 2 * hidden, 0, dtype)
+    y, pre = empty(rows, hidden, 16, dtype), empty_pre(rows, hidden)
     run_gated(x, wg, wu, bg, bu, act, y, pre)
     want, e, g, eg, u, eu = R.gated(x, wg, wu, bg, bu, act)
     R.within(y[:, :hidden], want, R.rounded(want, e, dtype), "y")
-    R.within(pre[:, :hidden], g, R.rounded(g, eg, dtype), "g")
-    R.within(pre[:, hidden:], u, R.rounded(u, eu, dtype), "u")
+    kept = unpack24(pre, hidden)
+    R.within(kept[:, :hidden], g, eg + 2.0 ** -16 * (g.abs() + eg), "g")
+    R.within(kept[:, hidden:], u, eu + 2.0 ** -16 * (u.abs() + eu), "u")
     gap_kept(y, hidden)
     y2 = empty(rows, hidden, 0, dtype)
     run_gated(x, wg, wu, bg, bu, act, y2)
@@ -276,7 +302,7 @@ def test_gated_ffn_extreme_gates(act):
     wg, wu = torch.zeros((16, 16), device=DEV, dtype=BF16), torch.zeros((16, 16), device=DEV, dtype=BF16)
     wg[:len(gates), 0] = torch.tensor(gates)
     wu[:, 1] = 1
-    y, pre = empty(1, 16, 0, BF16), empty(1, 32, 0, BF16)
+    y, pre = empty(1, 16, 0, BF16), empty_pre(1, 16)
     run_gated(x, wg, wu, None, None, act, y, pre)
     g = wg[:, 0].double()
     a, slope = R.activation(g, act)
@@ -315,9 +341,10 @@ def run_bwd(x, wg, wu, pre, dy, act, bias=True, dx=True, dw=True, gap=8, stream=
 def test_gated_ffn_bwd(rows, dim, hidden, dtype, act):
     x, wg, wu, _, _ = gated_inputs(rows, dim, hidden, dtype, False, rows + dim)
     g = gen(rows)
-    pre, dy = normal(g, (rows, 2 * hidden), 1.5, dtype), strided(normal(g, (rows, hidden), 0.5, dtype), 24)[0]
+    kept = unpack24(pack24(normal(g, (rows, 2 * hidden), 1.5, F32)), hidden)
+    pre, dy = pack24(kept), strided(normal(g, (rows, hidden), 0.5, dtype), 24)[0]
     out = run_bwd(x, wg, wu, pre, dy, act)
-    want = R.gated_bwd(x, wg, wu, pre, dy, act, dtype)
+    want = R.gated_bwd(x, wg, wu, kept, dy, act, dtype)
     for n in ("dgate_b", "dup_b", "dx", "dgate_w", "dup_w"):
         v, e = want[n]
         got = out[n][:, :dim] if n == "dx" else out[n]
@@ -338,7 +365,7 @@ def test_gated_ffn_bwd_is_the_slope_of_the_forward():
     x, wg, wu, bg, bu = gated_inputs(rows, dim, hidden, F16, True, 1)
     x = x.contiguous()
     dy = normal(gen(2), (rows, hidden), 1.0, F16)
-    y, pre = empty(rows, hidden, 0, F16), empty(rows, 2 * hidden, 0, F16)
+    y, pre = empty(rows, hidden, 0, F16), empty_pre(rows, hidden)
     run_gated(x, wg, wu, bg, bu, act, y, pre)
     out = run_bwd(x, wg, wu, pre, dy, act, gap=0)
     names = {"dx": 0, "dgate_w": 1, "dup_w": 2, "dgate_b": 3, "dup_b": 4}
@@ -350,7 +377,7 @@ def test_gated_ffn_bwd_is_the_slope_of_the_forward():
         up, down = list(at), list(at)
         up[i], down[i] = at[i] + h * v, at[i] - h * v
         slope = float((loss(up) - loss(down)) / (2 * h))
-        # roundings: pre, dg and du, and the result, three halves of a step each in the sum of magnitudes
+        # roundings: dg and du, and the result, half a step each in the sum of magnitudes (and pre's, far below)
         most = float((out[n].double() * v).abs().sum())
         half = R.HALF[out[n].dtype if n.endswith("_b") else F16]
         assert abs(slope - float((out[n].double() * v).sum())) < 4 * half * most + 1e-5, n
