@@ -9,7 +9,7 @@ namespace xema {
 
 namespace {
 
-typedef TileShape<256, 256, 2, 4, 2> Big;
+typedef TileShape<256, 256, 2, 4, 0> Big;
 typedef TileShape<128, 128, 2, 2, 3> Mid;
 typedef TileShape<64, 64, 2, 2, 4> Small;
 

@@ -18,6 +18,8 @@
 // likewise.  No load leaves the operand.
 #pragma once
 
+#include <type_traits>
+
 #include "device_common.h"
 #include "mma.h"
 
@@ -28,7 +30,6 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int KB = 128;                       // bytes of k per row and step
 constexpr uint32_t OUT_OF_RANGE = 0x80000000u;
-constexpr int64_t MAX_RECORDS = 0x7ffffff0;   // of a buffer: below OUT_OF_RANGE
 
 enum OperandOrder { ROWS, COLUMNS };
 
@@ -38,25 +39,27 @@ struct RowLoads {
   static constexpr int LOADS = R / 8 / NW;    // 1 KiB loads per wave and step
   static_assert(LOADS * 8 * NW == R, "load split");
   uint32_t off[LOADS];
-  uint32_t slot[2];                           // byte of k of this lane's slot, even and odd loads
-  // row `i` of the tile lies at (i * ld) bytes, for i < valid
-  __device__ __forceinline__ void init(int valid, uint32_t ld, int wave, int lane) {
+  int left[2];                                // bytes of k from this lane's slot on, even and odd loads
+  // byte of k of this lane's slot in load c of a step
+  static __device__ __forceinline__ int slot(int c, int wave, int lane) {
+    return ((lane % 8) ^ row_swz((wave * LOADS + c) * 8 + lane / 8)) * 16;
+  }
+  // row `i` of the tile lies at (i * ld) bytes, for i < valid; kbytes of k
+  __device__ __forceinline__ void init(int valid, uint32_t ld, int kbytes, int wave, int lane) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) left[c] = kbytes - slot(c, wave, lane);
 #pragma unroll
     for (int c = 0; c < LOADS; ++c) {
       const int row = (wave * LOADS + c) * 8 + lane / 8;
-      const uint32_t s = ((lane % 8) ^ row_swz(row)) * 16;
-      if (c < 2) slot[c] = s;
-      off[c] = row < valid ? row * ld + s : OUT_OF_RANGE;
+      off[c] = row < valid ? row * ld + slot(c, wave, lane) : OUT_OF_RANGE;
     }
-    if (LOADS == 1) slot[1] = slot[0];
   }
+  // Slots past the last k are out of range.  (A step past the last one, which
+  // the pipeline asks for, has no k in range; its scalar offset is 0, as the
+  // range check may subtract that.)
   __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t r, int c, int kt, int kbytes, uint8_t* st, int wave) const {
-    // (a step past the last one, which the pipeline's ring asks for, has no k in
-    // range; its scalar offset is 0, as the range check may subtract that)
     const int k0 = kt * KB;
-    uint32_t v = off[c];
-    if (k0 + KB > kbytes) v = k0 + (int)slot[c & 1] < kbytes ? v : OUT_OF_RANGE;
-    load_lds16(r, st + (wave * LOADS + c) * 1024, v, k0 < kbytes ? (uint32_t)k0 : 0u);
+    load_lds16(r, st + (wave * LOADS + c) * 1024, k0 < left[c & 1] ? off[c] : OUT_OF_RANGE, k0 < kbytes ? (uint32_t)k0 : 0u);
   }
 };
 
@@ -83,10 +86,9 @@ struct ColumnLoads {
       off[c] = col < valid ? k * ld + col * 2 : OUT_OF_RANGE;
     }
   }
-  // `left`: k rows from this step on (its k rows past the last are out of range)
-  __device__ __forceinline__ void issue(const uint8_t* base, uint32_t ld, int64_t left, int c, uint8_t* st, int wave) const {
-    const int64_t bytes = left <= 0 ? 0 : left * ld;
-    load_lds16(make_rsrc(base, bytes < MAX_RECORDS ? bytes : MAX_RECORDS), st + (wave * LOADS + c) * 1024, off[c], 0);
+  // `left`: k rows from this step on (those past the last are out of range)
+  __device__ __forceinline__ void issue(const uint8_t* base, uint32_t ld, int left, int c, uint8_t* st, int wave) const {
+    load_lds16(make_rsrc(base, max(min(left, 64), 0) * ld), st + (wave * LOADS + c) * 1024, off[c], 0);
   }
 };
 
@@ -104,7 +106,7 @@ struct RowOperand {
   __device__ __forceinline__ void init(const void* part0, const void* part1, int64_t valid, int64_t ld_bytes, int kbytes_,
                                        int steps0_, int wave, int lane) {
     const int v = valid < N ? (int)valid : N;
-    l.init(v, (uint32_t)ld_bytes, wave, lane);
+    l.init(v, (uint32_t)ld_bytes, kbytes_, wave, lane);
     p0 = (const uint8_t*)part0; p1 = (const uint8_t*)part1;
     bytes = v * ld_bytes;
     kbytes = kbytes_; steps0 = steps0_;
@@ -120,20 +122,19 @@ struct ColumnOperand {
   static constexpr int LOADS = ColumnLoads<N, NW>::LOADS;
   ColumnLoads<N, NW> l;
   const uint8_t *p0, *p1;
-  int64_t k;
+  int k, steps0;
   uint32_t ld;
-  int steps0;
   __device__ __forceinline__ void init(const void* part0, const void* part1, int64_t valid, int64_t ld_bytes, int64_t k_,
                                        int steps0_, int wave, int lane) {
     ld = (uint32_t)ld_bytes;
     l.init(valid < N ? (int)valid : N, ld, wave, lane);
     p0 = (const uint8_t*)part0; p1 = (const uint8_t*)part1;
-    k = k_; steps0 = steps0_;
+    k = (int)k_; steps0 = steps0_;
   }
   __device__ __forceinline__ void issue(int kt, int c, uint8_t* st, int wave) const {
     const bool second = kt >= steps0;
-    const int64_t k0 = (int64_t)(second ? kt - steps0 : kt) * 64;
-    l.issue((second ? p1 : p0) + k0 * ld, ld, k - k0, c, st, wave);
+    const int k0 = (second ? kt - steps0 : kt) * 64;
+    l.issue((second ? p1 : p0) + (int64_t)k0 * ld, ld, k - k0, c, st, wave);
   }
 };
 
@@ -148,12 +149,12 @@ struct PairOperand {
   int kbytes;
   __device__ __forceinline__ void init(const void* part0, const void* part1, int64_t valid, int64_t ld_bytes, int kbytes_,
                                        int wave, int lane) {
-    l.init(N, 0, wave, lane);
+    l.init(N, 0, kbytes_, wave, lane);
 #pragma unroll
     for (int c = 0; c < LOADS; ++c) {
       const int row = (wave * LOADS + c) * 8 + lane / 8;
       const int src = row / WC * (WC / 2) + row % (WC / 2);
-      l.off[c] = src < valid ? src * (uint32_t)ld_bytes + l.slot[c & 1] : OUT_OF_RANGE;
+      l.off[c] = src < valid ? src * (uint32_t)ld_bytes + l.slot(c, wave, lane) : OUT_OF_RANGE;
     }
     p0 = (const uint8_t*)part0; p1 = (const uint8_t*)part1;
     bytes = (valid < N / 2 ? valid : N / 2) * ld_bytes;
@@ -186,6 +187,14 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) i16x4* lds_i16x4_t;
 
+// The transposing LDS read.  The restrict parameter gives it an alias scope:
+// without one the compiler takes it to depend on every load into LDS in flight
+// and waits for all of them before each read (dW 2.9 -> 1.3 ms); what it does
+// depend on, the main loops wait for themselves.
+__device__ __forceinline__ i16x4 read_transposed(lds_i16x4_t __restrict__ p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
+}
+
 template <typename T, int N, OperandOrder ORDER>
 struct FragReader {
   typedef typename Frag<T>::type frag;
@@ -212,21 +221,22 @@ struct FragReader {
       }
     } else {
       const uint8_t* p = st + (base ^ (32 * i)) + kk * 32 * N * 2;
-      const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t)p);
-      const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t)(p + 4 * N * 2));
+      const i16x4 a = read_transposed((lds_i16x4_t)p);
+      const i16x4 b = read_transposed((lds_i16x4_t)(p + 4 * N * 2));
       const i16x8 v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
       return __builtin_bit_cast(frag, v);
     }
   }
 };
 
-// The tile's shape: BM x BN in WMW x WNW waves, NS stages of both operands.
+// The tile's shape: BM x BN in WMW x WNW waves.  NS: stages of both operands
+// in a ring, or 0 for the deep pipeline (two stages of A, three of B).
 template <int BM_, int BN_, int WMW_, int WNW_, int NS_>
 struct TileShape {
   static constexpr int BM = BM_, BN = BN_, WMW = WMW_, WNW = WNW_, NS = NS_;
   static constexpr int NW = WMW * WNW, WR = BM / WMW, WC = BN / WNW, MI = WR / 16, NJ = WC / 16;
   static constexpr int A_BYTES = BM * KB, B_BYTES = BN * KB, STAGE = A_BYTES + B_BYTES;
-  static constexpr int LDS = NS * STAGE;
+  static constexpr int LDS = NS ? NS * STAGE : 2 * A_BYTES + 3 * B_BYTES;
 };
 
 // acc += the tile's products over `steps` steps.  Fragments: the B operand's
@@ -234,8 +244,8 @@ struct TileShape {
 // one row: acc[i][j][e] is row wm WR + 16 i + lane % 16, column
 // wn WC + 16 j + 4 (lane / 16) + e.
 template <typename S, typename T, OperandOrder AO, OperandOrder BO, typename AOp, typename BOp>
-__device__ __forceinline__ void tile_products(const AOp& a, const BOp& b, int steps, uint8_t* smem, int wave, int lane,
-                                              f32x4 (&acc)[S::MI][S::NJ]) {
+__device__ __forceinline__ void tile_products_ring(const AOp& a, const BOp& b, int steps, uint8_t* smem, int wave, int lane,
+                                                   f32x4 (&acc)[S::MI][S::NJ]) {
   constexpr int LPS = AOp::LOADS + BOp::LOADS, KK = Frag<T>::KK;
   FragReader<T, S::BM, AO> ra;
   FragReader<T, S::BN, BO> rb;
@@ -279,6 +289,129 @@ __device__ __forceinline__ void tile_products(const AOp& a, const BOp& b, int st
   }
   // the loads that ran ahead still write to LDS: let them finish
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+}
+
+// The same with the deep pipeline, for tiles large enough to be bound by their
+// MFMAs.  A step is KK MI panels (a 16-row block of A at one MFMA k-step) of NJ
+// MFMAs.  A's fragments are read AHEAD panels ahead and B's a k-step ahead, so
+// that by panel MEET every wave has read all of step kt, and from there on
+// reads step kt + 1.  At the barrier there step kt + 1 has landed, and A of
+// step kt + 2 goes to the stage of A freed; B has three stages, so that of step
+// kt + 2 goes out at the start of step kt already.  The loads of a step are
+// spread over its panels.
+template <typename S, typename T, OperandOrder AO, OperandOrder BO, typename AOp, typename BOp>
+__device__ __forceinline__ void tile_products_deep(const AOp& a, const BOp& b, int steps, uint8_t* smem, int wave, int lane,
+                                                   f32x4 (&acc)[S::MI][S::NJ]) {
+  typedef typename Frag<T>::type frag;
+  constexpr int MI = S::MI, NJ = S::NJ, KK = Frag<T>::KK, PANELS = KK * MI;
+  constexpr int AHEAD = KK == 1 ? 3 : MI == 8 ? 5 : 4, RING = KK == 1 ? 4 : 8, MEET = PANELS - AHEAD;
+  static_assert(PANELS % RING == 0 && RING > AHEAD, "fragment registers");
+  // LDS instructions of one fragment of A and of B
+  constexpr int RA = AO == COLUMNS || sizeof(T) == 1 ? 2 : 1, RB = BO == COLUMNS || sizeof(T) == 1 ? 2 : 1;
+  constexpr int B1 = MI == 8 ? 3 : 0;         // KK = 2: the panel from which B of the second k-step is read, over four
+  static_assert(KK == 1 || (B1 + 4 <= MEET && MEET + 4 <= PANELS), "step read before the barrier");
+  static_assert(AOp::LOADS <= 2 * AHEAD && BOp::LOADS <= MEET, "loads of a step");
+  FragReader<T, S::BM, AO> ra;
+  FragReader<T, S::BN, BO> rb;
+  ra.init(wave / S::WNW * S::WR, lane);
+  rb.init(wave % S::WNW * S::WC, lane);
+  uint8_t* const b_ring = smem + 2 * S::A_BYTES;
+  frag fx[RING], fw[2][NJ];
+  int bs = 0;                                 // the stage of B of step kt
+  // PARITY: of the step, where fw holds one step's B and the next's (KK = 1)
+  auto step = [&](int kt, auto parity) {
+    constexpr int P = KK == 1 ? decltype(parity)::value : 0;
+    uint8_t* a_here = smem + (kt & 1) * S::A_BYTES;
+    const uint8_t* a_next = smem + ((kt & 1) ^ 1) * S::A_BYTES;
+    const uint8_t* b_here = b_ring + bs * S::B_BYTES;
+    bs = bs + 1 == 3 ? 0 : bs + 1;
+    const uint8_t* b_next = b_ring + bs * S::B_BYTES;
+    uint8_t* b_free = b_ring + (bs + 1 == 3 ? 0 : bs + 1) * S::B_BYTES;
+#pragma unroll
+    for (int m = 0; m < PANELS; ++m) {
+      if (m == MEET) {
+        // A and B of step kt + 1 have landed; B of step kt + 2 may be in flight
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(BOp::LOADS));
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const int kk = m / MI, i = m % MI, n = m + AHEAD;
+      fx[n % RING] = n < PANELS ? ra.read(a_here, n / MI, n % MI) : ra.read(a_next, (n - PANELS) / MI, (n - PANELS) % MI);
+      // B of the second k-step, or of step kt + 1, spread over the panels from b0 on
+      constexpr int SPREAD = KK == 1 ? AHEAD : 4;
+      const bool rb1 = KK == 2 && m >= B1 && m < B1 + SPREAD, rb0 = m >= MEET && m < MEET + SPREAD;
+      const int nb = rb1 ? m - B1 : m - MEET, j0 = nb * NJ / SPREAD, j1 = (nb + 1) * NJ / SPREAD;
+#pragma unroll
+      for (int j = j0; j < j1; ++j) {
+        if (rb1) fw[1][j] = rb.read(b_here, 1, j);
+        if (rb0) fw[KK == 1 ? P ^ 1 : 0][j] = rb.read(b_next, 0, j);
+      }
+      int loads = 0;
+      if (m < BOp::LOADS) {
+        b.issue(kt + 2, m, b_free, wave);
+        ++loads;
+      }
+#pragma unroll
+      for (int c = 0; c < AOp::LOADS; ++c)
+        if (m >= MEET && c * AHEAD / AOp::LOADS == m - MEET) {
+          a.issue(kt + 2, c, a_here, wave);
+          ++loads;
+        }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = Frag<T>::run(fw[KK == 1 ? P : kk][j], fx[m % RING], acc[i][j]);
+      // the panel's MFMAs around its LDS reads and loads
+      __builtin_amdgcn_sched_group_barrier(0x008, NJ / 2, 0);
+      const int reads = RA + (rb1 || rb0 ? (j1 - j0) * RB : 0);
+      if (reads == 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      else if (reads == 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      else if (reads == 3) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+      else if (reads == 4) __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+      else __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+      if (loads == 1) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+      else if (loads == 2) __builtin_amdgcn_sched_group_barrier(0x020, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, NJ - NJ / 2, 0);
+    }
+  };
+#pragma unroll
+  for (int c = 0; c < AOp::LOADS; ++c) a.issue(0, c, smem, wave);
+#pragma unroll
+  for (int c = 0; c < BOp::LOADS; ++c) b.issue(0, c, b_ring, wave);
+#pragma unroll
+  for (int c = 0; c < BOp::LOADS; ++c) b.issue(1, c, b_ring + S::B_BYTES, wave);
+#pragma unroll
+  for (int c = 0; c < AOp::LOADS; ++c) a.issue(1, c, smem + S::A_BYTES, wave);
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(AOp::LOADS + BOp::LOADS));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) fw[0][j] = rb.read(b_ring, 0, j);
+#pragma unroll
+  for (int m = 0; m < AHEAD; ++m) fx[m] = ra.read(smem, m / MI, m % MI);
+  if constexpr (KK == 1) {
+    int kt = 0;
+    for (; kt + 1 < steps; kt += 2) {
+      step(kt, std::integral_constant<int, 0>());
+      step(kt + 1, std::integral_constant<int, 1>());
+    }
+    if (kt < steps) step(kt, std::integral_constant<int, 0>());
+  } else {
+    for (int kt = 0; kt < steps; ++kt) step(kt, std::integral_constant<int, 0>());
+  }
+  // the loads that ran ahead still write to LDS: let them finish
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+}
+
+template <typename S, typename T, OperandOrder AO, OperandOrder BO, typename AOp, typename BOp>
+__device__ __forceinline__ void tile_products(const AOp& a, const BOp& b, int steps, uint8_t* smem, int wave, int lane,
+                                              f32x4 (&acc)[S::MI][S::NJ]) {
+  if constexpr (S::NS == 0) tile_products_deep<S, T, AO, BO>(a, b, steps, smem, wave, lane, acc);
+  else tile_products_ring<S, T, AO, BO>(a, b, steps, smem, wave, lane, acc);
 }
 
 // Tile (tm, tn) of workgroup wg among tiles_m x tiles_n: each XCD (wg % 8)
