@@ -2,6 +2,7 @@
 #include <algorithm>
 
 #include "device_common.h"
+#include "few_rows.h"
 #include "ffn.h"
 #include "mma_tile.h"
 
@@ -150,6 +151,52 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_gated(GatedParams p) {
   }
 }
 
+// The same for few rows: 16 hidden units a workgroup, gate rows as block 0 and
+// up rows as block 1.
+template <typename T, typename YT, int MT, int UNROLL>
+__global__ __launch_bounds__(FEW_WAVES * 64) void k_gated_few(GatedParams p) {
+  typedef FewRows<MT, 2> S;
+  __shared__ __attribute__((aligned(16))) float red[S::FLOATS];
+  const int n0 = (int)blockIdx.x * 16, l16 = threadIdx.x & 15;
+  const int64_t kb = (int64_t)p.dim * sizeof(T);
+  const int64_t unit = min(n0 + l16, p.hidden - 1);
+  const uint8_t* x[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t m = 16 * i + l16;
+    x[i] = (const uint8_t*)p.x + (m < p.rows ? m : p.rows - 1) * p.ldx * sizeof(T);
+  }
+  const uint8_t* const w[2] = {(const uint8_t*)p.gate_w + unit * kb, (const uint8_t*)p.up_w + unit * kb};
+  few_rows_products<T, MT, 2, UNROLL>(x, w, (int)kb, red);
+  // four units of one row per thread
+  const int t = (int)threadIdx.x, m = t / 4, c = t % 4 * 4, col = n0 + c;
+  if (m >= 16 * MT || m >= p.rows || col >= p.hidden) return;
+  const f32x4 rg = *reinterpret_cast<const f32x4*>(red + m * S::ROW + c), ru = *reinterpret_cast<const f32x4*>(red + m * S::ROW + 16 + c);
+  float g[4], u[4];
+  typedef YT y4 __attribute__((ext_vector_type(4)));
+  y4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    g[e] = rg[e];
+    u[e] = ru[e];
+    if (sizeof(T) == 1) {
+      g[e] *= p.x_scale[m] * p.gate_scale[col + e];
+      u[e] *= p.x_scale[m] * p.up_scale[col + e];
+    }
+    g[e] += p.gate_b ? bf16_bits_to_f32(p.gate_b[col + e]) : 0.f;
+    u[e] += p.up_b ? bf16_bits_to_f32(p.up_b[col + e]) : 0.f;
+    y[e] = (YT)(activate<false>(g[e], p.act, nullptr) * u[e]);
+  }
+  *reinterpret_cast<y4*>((YT*)p.y + m * p.ldy + col) = y;
+  if (sizeof(T) == 2 && p.pre) store_pre((uint8_t*)p.pre + ((int64_t)m * p.hidden + col) / 4 * PRE_GROUP, g, u);
+}
+
+template <typename T, typename YT, int MT, int UNROLL>
+hipError_t run_gated_few(const GatedParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((k_gated_few<T, YT, MT, UNROLL>), dim3((p.hidden + 15) / 16), dim3(FEW_WAVES * 64), 0, s, p);
+  return hipGetLastError();
+}
+
 template <typename T, typename YT, typename S>
 hipError_t run_gated(const GatedParams& p, hipStream_t s) {
   const int64_t tiles = (p.rows + S::BM - 1) / S::BM * ((p.hidden + S::BN / 2 - 1) / (S::BN / 2));
@@ -166,6 +213,8 @@ TileKind pick_tile(int64_t m, int64_t n) {
 
 template <typename T, typename YT>
 hipError_t gated_t(const GatedParams& p, hipStream_t s) {
+  if (p.rows <= 16) return run_gated_few<T, YT, 1, 4>(p, s);
+  if (p.rows <= 32) return run_gated_few<T, YT, 2, 2>(p, s);
   switch (pick_tile(p.rows, 2 * (int64_t)p.hidden)) {
     case BIG: return run_gated<T, YT, Big>(p, s);
     case MID: return run_gated<T, YT, Mid>(p, s);

@@ -1,8 +1,7 @@
 // A projection shared by requests with low-rank adapters of their own
 // (xema_op_lora_linear, xema_ffn.h).
-#include <utility>
-
 #include "device_common.h"
+#include "few_rows.h"
 #include "ffn.h"
 #include "mma_tile.h"
 
@@ -23,88 +22,208 @@ struct LoraParams {
   int dim, out_dim, rank, n_adapters;
 };
 
-// t[r] = scale[i] x[r] a[i]^T, as value and remainder.  A wave per row and rank.
+__device__ __forceinline__ bool has_adapter(const LoraParams& p, int id) { return id >= 0 && id < p.n_adapters; }
+
+constexpr int REDUCE_WAVES = 4;
+
+// Value and remainder of s in T, eight ranks of one row.
 template <typename T>
-__global__ __launch_bounds__(256) void k_lora_reduce(LoraParams p) {
+__device__ __forceinline__ void store_reduced(T* t, int rank, int q, const float s[8]) {
   typedef T t8 __attribute__((ext_vector_type(8)));
-  const int64_t r = blockIdx.x;
-  const int id = p.ids[r];
-  if (id < 0 || id >= p.n_adapters) return;
-  const int lane = threadIdx.x & 63;
-  const T* x = (const T*)p.x + r * p.ldx;
-  for (int q = threadIdx.x >> 6; q < p.rank; q += 4) {
-    const T* a = (const T*)p.a + ((int64_t)id * p.rank + q) * p.dim;
-    float s = 0.f;
-    for (int k = lane * 8; k < p.dim; k += 512) {
-      const t8 u = *reinterpret_cast<const t8*>(x + k), v = *reinterpret_cast<const t8*>(a + k);
+  t8 hi, lo;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf((float)u[e], (float)v[e], s);
+  for (int e = 0; e < 8; ++e) {
+    // (one fp32 value for both: the product that made it, fused into the first
+    // conversion, may round to the other neighbour than the remainder is of)
+    const float v = as_rounded_f32(s[e]);
+    hi[e] = (T)v;
+    lo[e] = (T)(v - (float)hi[e]);
+  }
+  *reinterpret_cast<t8*>(t + q) = hi;
+  *reinterpret_cast<t8*>(t + rank + q) = lo;
+}
+
+// t[r] = scale[i] x[r] a[i]^T as value and remainder.  `share` workgroups per
+// block of 16 MT rows.  Where the rows of a block that have an adapter share
+// it, the block's first workgroup multiplies all of them on MFMA, its waves
+// interleaved pieces of k, and the others have nothing to do; otherwise they
+// take the rows in turn, four ranks a wave at a time.
+template <typename T, int MT, int RT>
+__global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p, int share) {
+  typedef T t8 __attribute__((ext_vector_type(8)));
+  typedef typename Frag<T>::type frag;
+  constexpr int RB = 16 * MT, RR = 16 * RT;
+  __shared__ __attribute__((aligned(16))) float red[REDUCE_WAVES][RB][RR + 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, l4 = lane >> 4;
+  const int mine = (int)blockIdx.x % share;
+  const int64_t m0 = (int64_t)(blockIdx.x / share) * RB;
+  const int id = lane < RB && m0 + lane < p.rows ? p.ids[m0 + lane] : -2;
+  const uint64_t live = __ballot(has_adapter(p, id));
+  if (!live) return;
+  const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(live));
+  if (__ballot(id == one) == live) {
+    if (mine) return;
+    const T* a = (const T*)p.a + (int64_t)one * p.rank * p.dim;
+    const T *xr[MT], *ar[RT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int64_t m = m0 + 16 * i + l16;
+      xr[i] = (const T*)p.x + (m < p.rows ? m : p.rows - 1) * p.ldx;
     }
-    s = wave_sum(s) * p.scale[id];
-    if (lane == 0) {
-      T* t = (T*)p.t + r * 2 * p.rank + q;
-      const T hi = (T)s;
-      t[0] = hi;
-      t[p.rank] = (T)(s - (float)hi);
+#pragma unroll
+    for (int q = 0; q < RT; ++q) ar[q] = a + (int64_t)min(16 * q + l16, p.rank - 1) * p.dim;
+    f32x4 acc[MT][RT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int q = 0; q < RT; ++q) acc[i][q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    constexpr int UNROLL = RT + MT <= 5 ? 2 : 1;
+    for (int k0 = wave * 64; k0 < p.dim; k0 += REDUCE_WAVES * 64 * UNROLL) {
+      frag fx[UNROLL][2][MT], fa[UNROLL][2][RT];
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int k = k0 + u * REDUCE_WAVES * 64 + 32 * h + 8 * l4;
+          const bool in = k < p.dim;
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            fx[u][h][i] = frag{};
+            if (in) fx[u][h][i] = *reinterpret_cast<const frag*>(xr[i] + k);
+          }
+#pragma unroll
+          for (int q = 0; q < RT; ++q) {
+            fa[u][h][q] = frag{};
+            if (in) fa[u][h][q] = *reinterpret_cast<const frag*>(ar[q] + k);
+          }
+        }
+#pragma unroll
+      for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int q = 0; q < RT; ++q) acc[i][q] = Frag<T>::run(fa[u][h][q], fx[u][h][i], acc[i][q]);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int q = 0; q < RT; ++q) *reinterpret_cast<f32x4*>(&red[wave][16 * i + l16][16 * q + 4 * l4]) = acc[i][q];
+    __syncthreads();
+    const float scale = p.scale[one];
+    for (int at = threadIdx.x; at < RB * p.rank / 8; at += REDUCE_WAVES * 64) {
+      const int row = at / (p.rank / 8), q = at % (p.rank / 8) * 8;
+      if (!(live >> row & 1)) continue;
+      float s[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] = (red[0][row][q + e] + red[1][row][q + e] + red[2][row][q + e] + red[3][row][q + e]) * scale;
+      store_reduced<T>((T*)p.t + (m0 + row) * 2 * p.rank, p.rank, q, s);
+    }
+    return;
+  }
+  float* sums = &red[0][0][0];
+  for (int row = mine; row < RB; row += share) {
+    if (!(live >> row & 1)) continue;
+    const int own = __builtin_amdgcn_readlane(id, row);
+    const T* x = (const T*)p.x + (m0 + row) * p.ldx;
+    const T* a = (const T*)p.a + (int64_t)own * p.rank * p.dim;
+    for (int q = wave * 4; q < p.rank; q += REDUCE_WAVES * 4) {
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+      for (int k = lane * 8; k < p.dim; k += 512) {
+        const t8 u = *reinterpret_cast<const t8*>(x + k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const t8 v = *reinterpret_cast<const t8*>(a + (int64_t)(q + i) * p.dim + k);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[i] = fmaf((float)u[e], (float)v[e], s[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[i] = wave_sum(s[i]);
+        if (lane == 0) sums[q + i] = s[i];
+      }
+    }
+    __syncthreads();
+    const float scale = p.scale[own];
+    if ((int)threadIdx.x < p.rank / 8) {
+      float s[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] = sums[threadIdx.x * 8 + e] * scale;
+      store_reduced<T>((T*)p.t + (m0 + row) * 2 * p.rank, p.rank, (int)threadIdx.x * 8, s);
+    }
+    __syncthreads();
+  }
+}
+
+// acc += t[r] b[i]^T where all the wave's rows that are written have adapter
+// `one`: two MFMA k-ranges, values and remainders, over the same b.
+template <typename T, typename S>
+__device__ __forceinline__ void add_one_adapter(const LoraParams& p, int64_t m0, int n0, int lane, int one, f32x4 (&acc)[S::MI][S::NJ]) {
+  typedef typename Frag<T>::type frag;
+  const int l16 = lane & 15, l4 = lane >> 4;
+  const int slots = p.rank / 4, rs = p.rank / 8;       // 16-byte slots of a row of t and of a row of b
+  const T* b = (const T*)p.b + (int64_t)one * p.out_dim * p.rank;
+#pragma unroll 1
+  for (int k = 0; k < slots; k += 4) {
+    const int at = k + l4;
+    const bool in = at < slots;
+    frag fb[S::NJ];
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j) {
+      fb[j] = frag{};
+      if (in) fb[j] = *reinterpret_cast<const frag*>(b + (int64_t)min(n0 + 16 * j + l16, p.out_dim - 1) * p.rank + (at < rs ? at : at - rs) * 8);
+    }
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) {
+      const int64_t m = m0 + 16 * i + l16;
+      frag ft{};
+      if (in) ft = *reinterpret_cast<const frag*>((const T*)p.t + (m < p.rows ? m : p.rows - 1) * 2 * p.rank + at * 8);
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) acc[i][j] = Frag<T>::run(fb[j], ft, acc[i][j]);
     }
   }
 }
 
-template <typename F, int... J>
-__device__ __forceinline__ void each_block(F&& f, std::integer_sequence<int, J...>) {
-  (f(std::integral_constant<int, J>()), ...);
+// sum += t b^T for one row and four columns, eight ranks at a time.
+template <typename T>
+__device__ __forceinline__ void add_row(const LoraParams& p, const T* t, const T* const (&b)[4], float (&sum)[4]) {
+  typedef T t8 __attribute__((ext_vector_type(8)));
+  for (int q = 0; q < p.rank; q += 8) {
+    const t8 hi = *reinterpret_cast<const t8*>(t + q), lo = *reinterpret_cast<const t8*>(t + p.rank + q);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const t8 v = *reinterpret_cast<const t8*>(b[c] + q);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[c] = fmaf((float)hi[e] + (float)lo[e], (float)v[e], sum[c]);
+    }
+  }
 }
 
-// acc += t[r] b[i]^T for the rows of each adapter among the wave's rows, one
-// adapter at a time.  Products of a row with another request's adapter are
-// formed beside and dropped, never multiplied by zero: that adapter may hold
-// infinities.
+// acc += t[r] b[i]^T where the wave's rows have different adapters, or some
+// none: every lane its own rows' products, so that no row meets another's
+// adapter (which may hold infinities).
 template <typename T, typename S>
-__device__ __forceinline__ void add_adapters(const LoraParams& p, int64_t m0, int n0, int wave, int lane, const int (&id)[S::MI],
-                                             f32x4 (&acc)[S::MI][S::NJ]) {
-  typedef typename Frag<T>::type frag;
+__device__ __forceinline__ void add_own_adapters(const LoraParams& p, int64_t m0, int n0, int lane, const int (&id)[S::MI],
+                                                 f32x4 (&acc)[S::MI][S::NJ]) {
   const int l16 = lane & 15, l4 = lane >> 4;
-  const int slots = p.rank / 4, rs = p.rank / 8;       // 16-byte slots of a row of t and of a row of b
-  int todo = 0;                                        // blocks of this lane whose row's adapter is to come
 #pragma unroll
-  for (int i = 0; i < S::MI; ++i)
-    if (id[i] >= 0 && id[i] < p.n_adapters) todo |= 1 << i;
-  for (;;) {
-    const uint64_t any = __ballot(todo != 0);
-    if (!any) break;
-    int first = -1;
+  for (int i = 0; i < S::MI; ++i) {
+    if (!has_adapter(p, id[i])) continue;
+    const T* t = (const T*)p.t + (m0 + 16 * i + l16) * 2 * p.rank;
+    const T* bw = (const T*)p.b + (int64_t)id[i] * p.out_dim * p.rank;
 #pragma unroll
-    for (int i = 0; i < S::MI; ++i) first = first < 0 && (todo >> i & 1) ? id[i] : first;
-    const int cur = __builtin_amdgcn_readlane(first, __builtin_ctzll(any));
-    int hit = 0;
+    for (int j = 0; j < S::NJ; ++j) {
+      const T* b[4];
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < S::MI; ++i) hit |= (id[i] == cur) << i;
-    const T* bw = (const T*)p.b + (int64_t)cur * p.out_dim * p.rank;
-    auto block = [&](auto jc) {
-      constexpr int j = decltype(jc)::value;
-      const int n = min(n0 + 16 * j + l16, p.out_dim - 1);
-      f32x4 sum[S::MI];
+      for (int e = 0; e < 4; ++e) b[e] = bw + (int64_t)min(n0 + 16 * j + 4 * l4 + e, p.out_dim - 1) * p.rank;
+      add_row<T>(p, t, b, sum);
 #pragma unroll
-      for (int i = 0; i < S::MI; ++i) sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      for (int k = 0; k < slots; k += 4) {
-        const int at = k + l4;
-        frag fb{};
-        if (at < slots) fb = *reinterpret_cast<const frag*>(bw + (int64_t)n * p.rank + (at < rs ? at : at - rs) * 8);
-#pragma unroll
-        for (int i = 0; i < S::MI; ++i) {
-          frag ft{};
-          // (a row past the end, or without this adapter, contributes nothing)
-          if (at < slots && id[i] == cur) ft = *reinterpret_cast<const frag*>((const T*)p.t + (m0 + 16 * i + l16) * 2 * p.rank + at * 8);
-          sum[i] = Frag<T>::run(fb, ft, sum[i]);
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = id[i] == cur ? acc[i][j][e] + sum[i][e] : acc[i][j][e];
-    };
-    each_block(block, std::make_integer_sequence<int, S::NJ>());
-    todo &= ~hit;
+      for (int e = 0; e < 4; ++e) acc[i][j][e] += sum[e];
+    }
   }
 }
 
@@ -137,8 +256,24 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_lora_project(LoraParams p) {
   for (int i = 0; i < S::MI; ++i)
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  tile_products<S, T, ROWS, ROWS>(a, b, (kbytes + KB - 1) / KB, smem, wave, lane, acc);
-  if (p.n_adapters) add_adapters<T, S>(p, mw, nw, wave, lane, id, acc);
+  // the adapters of the rows that get a value: none, one, or several (and none)
+  int some = -1;
+  bool own = false, without = false;
+#pragma unroll
+  for (int i = 0; i < S::MI; ++i) {
+    if (has_adapter(p, id[i])) {
+      own |= some >= 0 && some != id[i];
+      some = id[i];
+    }
+    without |= id[i] == -1;
+  }
+  const uint64_t any = __ballot(some >= 0);
+  const int one = any ? __builtin_amdgcn_readlane(some, __builtin_ctzll(any)) : -1;
+  const bool mixed = any && __ballot(own || without || (some >= 0 && some != one));
+  tile_products<S, T, ROWS, ROWS>(a, b, (kbytes + KB - 1) / KB, smem, wave, lane, acc, [&] {
+    if (any && !mixed) add_one_adapter<T, S>(p, mw, nw, lane, one, acc);
+  });
+  if (mixed) add_own_adapters<T, S>(p, mw, nw, lane, id, acc);
 
   float bv[S::NJ][4];
 #pragma unroll
@@ -164,13 +299,75 @@ hipError_t run_project(const LoraParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Few rows (few_rows.h), 16 NB columns a workgroup.
+template <typename T, typename YT, int MT, int NB, int UNROLL>
+__global__ __launch_bounds__(FEW_WAVES * 64) void k_lora_project_few(LoraParams p) {
+  typedef FewRows<MT, NB> S;
+  __shared__ __attribute__((aligned(16))) float red[S::FLOATS];
+  const int n0 = (int)blockIdx.x * S::COLS, l16 = threadIdx.x & 15;
+  const uint8_t *x[MT], *w[NB];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int64_t m = 16 * i + l16;
+    x[i] = (const uint8_t*)p.x + (m < p.rows ? m : p.rows - 1) * p.ldx * 2;
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) w[b] = (const uint8_t*)p.w + (int64_t)min(n0 + 16 * b + l16, p.out_dim - 1) * p.dim * 2;
+  few_rows_products<T, MT, NB, UNROLL>(x, w, p.dim * 2, red);
+  for (int at = threadIdx.x; at < 16 * MT * S::COLS / 4; at += FEW_WAVES * 64) {
+    const int m = at / (S::COLS / 4), c = at % (S::COLS / 4) * 4, col = n0 + c;
+    if (m >= p.rows || col >= p.out_dim) continue;
+    const int id = p.ids[m];
+    if (id < -1) continue;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = red[m * S::ROW + c + e] + (p.bias ? bf16_bits_to_f32(p.bias[col + e]) : 0.f);
+    if (id >= 0) {
+      if (id < p.n_adapters) {
+        const T* b[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) b[e] = (const T*)p.b + ((int64_t)id * p.out_dim + col + e) * p.rank;
+        add_row<T>(p, (const T*)p.t + (int64_t)m * 2 * p.rank, b, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __builtin_nanf("");
+      }
+    }
+    typedef YT y4 __attribute__((ext_vector_type(4)));
+    y4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (YT)v[e];
+    *reinterpret_cast<y4*>((YT*)p.y + m * p.ldy + col) = y;
+  }
+}
+
+template <typename T, typename YT, int MT, int NB, int UNROLL>
+hipError_t run_project_few(const LoraParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((k_lora_project_few<T, YT, MT, NB, UNROLL>), dim3((p.out_dim + 16 * NB - 1) / (16 * NB)), dim3(FEW_WAVES * 64), 0, s, p);
+  return hipGetLastError();
+}
+
+template <typename T, int MT>
+hipError_t run_reduce(const LoraParams& p, hipStream_t s) {
+  // a workgroup per row while these are few enough to be requests of one token
+  const int share = p.rows <= 2048 ? 16 : 4;
+  const dim3 grid((unsigned)((p.rows + 16 * MT - 1) / (16 * MT) * share)), block(REDUCE_WAVES * 64);
+  if (p.rank <= 16) hipLaunchKernelGGL((k_lora_reduce<T, MT, 1>), grid, block, 0, s, p, share);
+  else if (p.rank <= 32) hipLaunchKernelGGL((k_lora_reduce<T, MT, 2>), grid, block, 0, s, p, share);
+  else if (p.rank <= 64) hipLaunchKernelGGL((k_lora_reduce<T, MT, 4>), grid, block, 0, s, p, share);
+  else hipLaunchKernelGGL((k_lora_reduce<T, MT, 8>), grid, block, 0, s, p, share);
+  return hipGetLastError();
+}
+
 template <typename T, typename YT>
 hipError_t lora_t(const LoraParams& p, hipStream_t s) {
   if (p.n_adapters) {
-    hipLaunchKernelGGL((k_lora_reduce<T>), dim3((unsigned)p.rows), dim3(256), 0, s, p);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = p.rows >= 12288 ? run_reduce<T, 4>(p, s) : run_reduce<T, 1>(p, s);
     if (e != hipSuccess) return e;
   }
+  if (p.rows <= 16) return run_project_few<T, YT, 1, 1, 4>(p, s);
+  if (p.rows <= 32) return run_project_few<T, YT, 2, 1, 4>(p, s);
+  if (p.rows <= 64) return run_project_few<T, YT, 4, 1, 2>(p, s);
   auto tiles = [&](int t) { return (p.rows + t - 1) / t * ((p.out_dim + t - 1) / t); };
   if (tiles(256) >= 192) return run_project<T, YT, Big>(p, s);
   return tiles(128) >= 192 ? run_project<T, YT, Mid>(p, s) : run_project<T, YT, Small>(p, s);

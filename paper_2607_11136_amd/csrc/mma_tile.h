@@ -88,7 +88,9 @@ struct ColumnLoads {
   }
   // `left`: k rows from this step on (those past the last are out of range)
   __device__ __forceinline__ void issue(const uint8_t* base, uint32_t ld, int left, int c, uint8_t* st, int wave) const {
-    load_lds16(make_rsrc(base, max(min(left, 64), 0) * ld), st + (wave * LOADS + c) * 1024, off[c], 0);
+    // (a scalar: the median of three is a vector instruction, and descriptors made of it are loaded lane by lane)
+    const int rows = __builtin_amdgcn_readfirstlane(max(min(left, 64), 0));
+    load_lds16(make_rsrc(base, (uint32_t)rows * ld), st + (wave * LOADS + c) * 1024, off[c], 0);
   }
 };
 
@@ -243,9 +245,9 @@ struct TileShape {
 // is the MFMA's first, so that a lane ends with four consecutive columns of
 // one row: acc[i][j][e] is row wm WR + 16 i + lane % 16, column
 // wn WC + 16 j + 4 (lane / 16) + e.
-template <typename S, typename T, OperandOrder AO, OperandOrder BO, typename AOp, typename BOp>
+template <typename S, typename T, OperandOrder AO, OperandOrder BO, typename AOp, typename BOp, typename F>
 __device__ __forceinline__ void tile_products_ring(const AOp& a, const BOp& b, int steps, uint8_t* smem, int wave, int lane,
-                                                   f32x4 (&acc)[S::MI][S::NJ]) {
+                                                   f32x4 (&acc)[S::MI][S::NJ], F&& meanwhile) {
   constexpr int LPS = AOp::LOADS + BOp::LOADS, KK = Frag<T>::KK;
   FragReader<T, S::BM, AO> ra;
   FragReader<T, S::BN, BO> rb;
@@ -260,6 +262,7 @@ __device__ __forceinline__ void tile_products_ring(const AOp& a, const BOp& b, i
   };
 #pragma unroll
   for (int s = 0; s < S::NS - 1; ++s) issue(s, s);
+  meanwhile();
   int cur = 0, fill = S::NS - 1;
   for (int kt = 0; kt < steps; ++kt) {
     // step kt has landed (the NS - 2 steps after it may be in flight), and
@@ -299,9 +302,9 @@ __device__ __forceinline__ void tile_products_ring(const AOp& a, const BOp& b, i
 // step kt + 2 goes to the stage of A freed; B has three stages, so that of step
 // kt + 2 goes out at the start of step kt already.  The loads of a step are
 // spread over its panels.
-template <typename S, typename T, OperandOrder AO, OperandOrder BO, typename AOp, typename BOp>
+template <typename S, typename T, OperandOrder AO, OperandOrder BO, typename AOp, typename BOp, typename F>
 __device__ __forceinline__ void tile_products_deep(const AOp& a, const BOp& b, int steps, uint8_t* smem, int wave, int lane,
-                                                   f32x4 (&acc)[S::MI][S::NJ]) {
+                                                   f32x4 (&acc)[S::MI][S::NJ], F&& meanwhile) {
   typedef typename Frag<T>::type frag;
   constexpr int MI = S::MI, NJ = S::NJ, KK = Frag<T>::KK, PANELS = KK * MI;
   constexpr int AHEAD = KK == 1 ? 3 : MI == 8 ? 5 : 4, RING = KK == 1 ? 4 : 8, MEET = PANELS - AHEAD;
@@ -383,6 +386,7 @@ __device__ __forceinline__ void tile_products_deep(const AOp& a, const BOp& b, i
   for (int c = 0; c < BOp::LOADS; ++c) b.issue(1, c, b_ring + S::B_BYTES, wave);
 #pragma unroll
   for (int c = 0; c < AOp::LOADS; ++c) a.issue(1, c, smem + S::A_BYTES, wave);
+  meanwhile();
   __builtin_amdgcn_sched_barrier(0);
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(AOp::LOADS + BOp::LOADS));
   asm volatile("" ::: "memory");
@@ -407,11 +411,16 @@ __device__ __forceinline__ void tile_products_deep(const AOp& a, const BOp& b, i
   __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
 }
 
-template <typename S, typename T, OperandOrder AO, OperandOrder BO, typename AOp, typename BOp>
+// meanwhile() runs once while the first steps' loads are in flight (it may use
+// acc, and load into registers).
+struct Nothing {
+  __device__ __forceinline__ void operator()() const {}
+};
+template <typename S, typename T, OperandOrder AO, OperandOrder BO, typename AOp, typename BOp, typename F = Nothing>
 __device__ __forceinline__ void tile_products(const AOp& a, const BOp& b, int steps, uint8_t* smem, int wave, int lane,
-                                              f32x4 (&acc)[S::MI][S::NJ]) {
-  if constexpr (S::NS == 0) tile_products_deep<S, T, AO, BO>(a, b, steps, smem, wave, lane, acc);
-  else tile_products_ring<S, T, AO, BO>(a, b, steps, smem, wave, lane, acc);
+                                              f32x4 (&acc)[S::MI][S::NJ], F&& meanwhile = F()) {
+  if constexpr (S::NS == 0) tile_products_deep<S, T, AO, BO>(a, b, steps, smem, wave, lane, acc, meanwhile);
+  else tile_products_ring<S, T, AO, BO>(a, b, steps, smem, wave, lane, acc, meanwhile);
 }
 
 // Tile (tm, tn) of workgroup wg among tiles_m x tiles_n: each XCD (wg % 8)
@@ -424,8 +433,9 @@ __device__ __forceinline__ void tile_of(int wg, int tiles_m, int tiles_n, int gr
   const int g = t / (group * tiles_n), first = g * group;
   const int size = min(tiles_m - first, group);
   const int in = t - g * group * tiles_n;
-  *tm = first + in % size;
-  *tn = in / size;
+  // (scalars: the buffer descriptors made from them must be)
+  *tm = __builtin_amdgcn_readfirstlane(first + in % size);
+  *tn = __builtin_amdgcn_readfirstlane(in / size);
 }
 
 // Up to 32 columns of one row (NB 16-column blocks of a wave, a lane holding

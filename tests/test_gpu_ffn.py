@@ -207,7 +207,7 @@ def test_rmsnorm_bwd_in_place(which):
 
 # -- gated feed-forward ------------------------------------------------------------------------------------------
 
-SIZES = [(1, 8, 8), (1, 4096, 1024), (2, 64, 40), (16, 72, 136), (17, 512, 1368), (63, 128, 64), (65, 136, 200), (130, 328, 520), (257, 1544, 264),
+SIZES = [(1, 8, 8), (1, 4096, 1024), (2, 64, 40), (16, 72, 136), (17, 512, 1368), (32, 1096, 72), (33, 1096, 72), (63, 128, 64), (65, 136, 200), (130, 328, 520), (257, 1544, 264),
          (700, 256, 2056), (1500, 192, 4104)]
 
 
@@ -272,7 +272,7 @@ def test_gated_ffn(rows, dim, hidden, dtype, act, bias):
 E4M3_SUM = 2.0 ** -14
 
 
-@pytest.mark.parametrize("rows,dim,hidden", [(1, 16, 8), (1, 4096, 1024), (3, 144, 40), (65, 272, 200), (130, 336, 520), (700, 128, 2056),
+@pytest.mark.parametrize("rows,dim,hidden", [(1, 16, 8), (1, 4096, 1024), (3, 144, 40), (16, 2064, 24), (31, 1040, 72), (65, 272, 200), (130, 336, 520), (700, 128, 2056),
                                              (1500, 512, 4104)])
 @pytest.mark.parametrize("yt,act,bias", [(BF16, 0, False), (F16, 1, True)])
 def test_gated_ffn_8bit(rows, dim, hidden, yt, act, bias):
@@ -435,7 +435,8 @@ def spread_ids(rows, n, how, seed):
 
 
 LORA_SIZES = [(1, 8, 8, 8, 1), (1, 4096, 1032, 16, 3), (5, 72, 136, 8, 2), (48, 512, 1024, 16, 20), (65, 136, 200, 24, 4), (130, 328, 520, 64, 7),
-              (257, 1544, 264, 128, 5), (700, 256, 2056, 32, 40), (1500, 192, 4104, 8, 3), (9000, 256, 1544, 16, 4)]
+              (257, 1544, 264, 128, 5), (700, 256, 2056, 32, 40), (1500, 192, 4104, 8, 3), (9000, 256, 1544, 16, 4),
+              (12500, 136, 520, 32, 5), (16, 2056, 72, 32, 3), (33, 1032, 88, 128, 2)]
 
 
 @pytest.mark.parametrize("rows,dim,out_dim,rank,n", LORA_SIZES)
