@@ -11,6 +11,7 @@ namespace xema {
 namespace {
 
 typedef TileShape<256, 256, 2, 4, 0> Big;
+typedef TileShape<128, 256, 2, 4, 0> Wide;
 typedef TileShape<128, 128, 2, 2, 3> Mid;
 typedef TileShape<64, 64, 2, 2, 4> Small;
 
@@ -153,9 +154,10 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_gated(GatedParams p) {
 
 // The same for few rows: 16 hidden units a workgroup, gate rows as block 0 and
 // up rows as block 1.
+constexpr int FEW_WAVES = 8;
 template <typename T, typename YT, int MT, int UNROLL>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_gated_few(GatedParams p) {
-  typedef FewRows<MT, 2> S;
+  typedef FewRows<MT, 2, FEW_WAVES> S;
   __shared__ __attribute__((aligned(16))) float red[S::FLOATS];
   const int n0 = (int)blockIdx.x * 16, l16 = threadIdx.x & 15;
   const int64_t kb = (int64_t)p.dim * sizeof(T);
@@ -167,7 +169,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_gated_few(GatedParams p) {
     x[i] = (const uint8_t*)p.x + (m < p.rows ? m : p.rows - 1) * p.ldx * sizeof(T);
   }
   const uint8_t* const w[2] = {(const uint8_t*)p.gate_w + unit * kb, (const uint8_t*)p.up_w + unit * kb};
-  few_rows_products<T, MT, 2, UNROLL>(x, w, (int)kb, red);
+  few_rows_products<T, MT, 2, FEW_WAVES, UNROLL>(x, w, (int)kb, red);
   // four units of one row per thread
   const int t = (int)threadIdx.x, m = t / 4, c = t % 4 * 4, col = n0 + c;
   if (m >= 16 * MT || m >= p.rows || col >= p.hidden) return;

@@ -10,6 +10,7 @@ namespace xema {
 namespace {
 
 typedef TileShape<256, 256, 2, 4, 0> Big;
+typedef TileShape<128, 256, 2, 4, 0> Wide;
 typedef TileShape<128, 128, 2, 2, 3> Mid;
 typedef TileShape<64, 64, 2, 2, 4> Small;
 
@@ -24,7 +25,7 @@ struct LoraParams {
 
 __device__ __forceinline__ bool has_adapter(const LoraParams& p, int id) { return id >= 0 && id < p.n_adapters; }
 
-constexpr int REDUCE_WAVES = 4;
+constexpr int REDUCE_WAVES = 8;
 
 // Value and remainder of s in T, eight ranks of one row.
 template <typename T>
@@ -55,7 +56,9 @@ __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p,
   constexpr int RB = 16 * MT, RR = 16 * RT;
   __shared__ __attribute__((aligned(16))) float red[REDUCE_WAVES][RB][RR + 4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, l4 = lane >> 4;
-  const int mine = (int)blockIdx.x % share;
+  // (workgroups go round the 8 XCDs in turn: the first of each block must not
+  // always meet the same one)
+  const int mine = (int)((blockIdx.x + blockIdx.x / share) % share);
   const int64_t m0 = (int64_t)(blockIdx.x / share) * RB;
   const int id = lane < RB && m0 + lane < p.rows ? p.ids[m0 + lane] : -2;
   const uint64_t live = __ballot(has_adapter(p, id));
@@ -77,7 +80,7 @@ __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p,
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int q = 0; q < RT; ++q) acc[i][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-    constexpr int UNROLL = RT + MT <= 5 ? 2 : 1;
+    constexpr int UNROLL = RT + MT <= 4 ? 2 : 1;
     for (int k0 = wave * 64; k0 < p.dim; k0 += REDUCE_WAVES * 64 * UNROLL) {
       frag fx[UNROLL][2][MT], fa[UNROLL][2][RT];
 #pragma unroll
@@ -117,112 +120,173 @@ __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p,
       if (!(live >> row & 1)) continue;
       float s[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[e] = (red[0][row][q + e] + red[1][row][q + e] + red[2][row][q + e] + red[3][row][q + e]) * scale;
+      for (int e = 0; e < 8; ++e) {
+        s[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < REDUCE_WAVES; ++w) s[e] += red[w][row][q + e];
+        s[e] *= scale;
+      }
       store_reduced<T>((T*)p.t + (m0 + row) * 2 * p.rank, p.rank, q, s);
     }
     return;
   }
-  float* sums = &red[0][0][0];
+  // four ranks a wave at a time; where that leaves waves over, k in parts too
+  float* sums = &red[0][0][0];                                   // [parts][rank]
+  const int batches = min(p.rank / 4, REDUCE_WAVES), parts = REDUCE_WAVES / batches;
+  const int batch = wave % batches, part = wave / batches;       // (part `parts`: waves that no batch needs)
   for (int row = mine; row < RB; row += share) {
     if (!(live >> row & 1)) continue;
     const int own = __builtin_amdgcn_readlane(id, row);
+    const float scale = p.scale[own];
     const T* x = (const T*)p.x + (m0 + row) * p.ldx;
     const T* a = (const T*)p.a + (int64_t)own * p.rank * p.dim;
-    for (int q = wave * 4; q < p.rank; q += REDUCE_WAVES * 4) {
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (part < parts)
+      for (int q = batch * 4; q < p.rank; q += batches * 4) {
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-      for (int k = lane * 8; k < p.dim; k += 512) {
-        const t8 u = *reinterpret_cast<const t8*>(x + k);
+        for (int k = part * 512 + lane * 8; k < p.dim; k += parts * 512) {
+          const t8 u = *reinterpret_cast<const t8*>(x + k);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const t8 v = *reinterpret_cast<const t8*>(a + (int64_t)(q + i) * p.dim + k);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[i] = fmaf((float)u[e], (float)v[e], s[i]);
+          }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const t8 v = *reinterpret_cast<const t8*>(a + (int64_t)(q + i) * p.dim + k);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) s[i] = fmaf((float)u[e], (float)v[e], s[i]);
+          s[i] = wave_sum(s[i]);
+          if (lane == 0) sums[part * p.rank + q + i] = s[i];
         }
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[i] = wave_sum(s[i]);
-        if (lane == 0) sums[q + i] = s[i];
-      }
-    }
     __syncthreads();
-    const float scale = p.scale[own];
     if ((int)threadIdx.x < p.rank / 8) {
       float s[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[e] = sums[threadIdx.x * 8 + e] * scale;
+      for (int e = 0; e < 8; ++e) {
+        s[e] = 0.f;
+        for (int w = 0; w < parts; ++w) s[e] += sums[w * p.rank + threadIdx.x * 8 + e];
+        s[e] *= scale;
+      }
       store_reduced<T>((T*)p.t + (m0 + row) * 2 * p.rank, p.rank, (int)threadIdx.x * 8, s);
     }
     __syncthreads();
   }
 }
 
-// acc += t[r] b[i]^T where all the wave's rows that are written have adapter
-// `one`: two MFMA k-ranges, values and remainders, over the same b.
+// The adapters of a wave's rows by blocks of 16: a block is pure where all its
+// rows that get a value have the same adapter.
+template <int MI>
+struct WaveAdapters {
+  int id[MI];          // of this lane's row of each block
+  int block[MI];       // a pure block's adapter, -1 for a block without one, -2 for a mixed block (scalars)
+  int first, second;   // the first two pure blocks' adapters, -1 for none
+  __device__ __forceinline__ void init(const LoraParams& p, int64_t m0, int lane) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int64_t m = m0 + 16 * i + (lane & 15);
+      id[i] = m < p.rows ? p.ids[m] : -2;
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const uint64_t with = __ballot(has_adapter(p, id[i])), without = __ballot(id[i] == -1);
+      const int one = with ? __builtin_amdgcn_readlane(id[i], __builtin_ctzll(with)) : -1;
+      block[i] = !with ? -1 : without || __ballot(id[i] == one) != with ? -2 : one;
+    }
+    // (a third adapter within the wave's rows: its blocks count as mixed)
+    first = second = -1;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      if (block[i] < 0 || block[i] == first) continue;
+      if (first < 0) first = block[i];
+      else if (second < 0) second = block[i];
+      else if (block[i] != second) block[i] = -2;
+    }
+  }
+};
+
+// acc += t[r] b[i]^T for the pure blocks with adapter `one` (-1: none): the
+// values' MFMA k-range and the remainders', over the same b.
 template <typename T, typename S>
-__device__ __forceinline__ void add_one_adapter(const LoraParams& p, int64_t m0, int n0, int lane, int one, f32x4 (&acc)[S::MI][S::NJ]) {
+__device__ __forceinline__ void add_to_pure(const LoraParams& p, int64_t m0, int n0, int lane, const WaveAdapters<S::MI>& who, int one,
+                                            f32x4 (&acc)[S::MI][S::NJ]) {
   typedef typename Frag<T>::type frag;
   const int l16 = lane & 15, l4 = lane >> 4;
-  const int slots = p.rank / 4, rs = p.rank / 8;       // 16-byte slots of a row of t and of a row of b
+  const int slots = one >= 0 ? p.rank / 4 : 0, rs = p.rank / 8;    // 16-byte slots of a row of t and of a row of b
   const T* b = (const T*)p.b + (int64_t)one * p.out_dim * p.rank;
 #pragma unroll 1
   for (int k = 0; k < slots; k += 4) {
     const int at = k + l4;
     const bool in = at < slots;
-    frag fb[S::NJ];
+    frag fb[S::NJ], ft[S::MI];
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) {
       fb[j] = frag{};
-      if (in) fb[j] = *reinterpret_cast<const frag*>(b + (int64_t)min(n0 + 16 * j + l16, p.out_dim - 1) * p.rank + (at < rs ? at : at - rs) * 8);
+      if (in) fb[j] = *reinterpret_cast<const frag*>(b + min(n0 + 16 * j + l16, p.out_dim - 1) * p.rank + (at < rs ? at : at - rs) * 8);
     }
 #pragma unroll
     for (int i = 0; i < S::MI; ++i) {
       const int64_t m = m0 + 16 * i + l16;
-      frag ft{};
-      if (in) ft = *reinterpret_cast<const frag*>((const T*)p.t + (m < p.rows ? m : p.rows - 1) * 2 * p.rank + at * 8);
+      ft[i] = frag{};
+      if (in) ft[i] = *reinterpret_cast<const frag*>((const T*)p.t + (m < p.rows ? m : p.rows - 1) * 2 * p.rank + at * 8);
+    }
+    // (formed for every block and kept for those of this adapter: branches
+    // around the MFMAs would double the accumulators' registers)
 #pragma unroll
-      for (int j = 0; j < S::NJ; ++j) acc[i][j] = Frag<T>::run(fb[j], ft, acc[i][j]);
+    for (int i = 0; i < S::MI; ++i) {
+      const bool keep = who.block[i] == one;
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) {
+        const f32x4 v = Frag<T>::run(fb[j], ft[i], acc[i][j]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = keep ? v[e] : acc[i][j][e];
+      }
     }
   }
 }
 
-// sum += t b^T for one row and four columns, eight ranks at a time.
-template <typename T>
-__device__ __forceinline__ void add_row(const LoraParams& p, const T* t, const T* const (&b)[4], float (&sum)[4]) {
+// sum += t b^T for one row and C columns, eight ranks at a time.
+template <typename T, int C>
+__device__ __forceinline__ void add_row(const LoraParams& p, const T* t, const T* const (&b)[C], float (&sum)[C]) {
   typedef T t8 __attribute__((ext_vector_type(8)));
   for (int q = 0; q < p.rank; q += 8) {
     const t8 hi = *reinterpret_cast<const t8*>(t + q), lo = *reinterpret_cast<const t8*>(t + p.rank + q);
+    t8 v[C];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const t8 v = *reinterpret_cast<const t8*>(b[c] + q);
+    for (int c = 0; c < C; ++c) v[c] = *reinterpret_cast<const t8*>(b[c] + q);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[c] = fmaf((float)hi[e] + (float)lo[e], (float)v[e], sum[c]);
-    }
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[c] = fmaf((float)hi[e] + (float)lo[e], (float)v[c][e], sum[c]);
   }
 }
 
-// acc += t[r] b[i]^T where the wave's rows have different adapters, or some
-// none: every lane its own rows' products, so that no row meets another's
-// adapter (which may hold infinities).
+// acc += t[r] b[i]^T for the mixed blocks: every lane its own row's products,
+// so that no row meets another's adapter (which may hold infinities: a product
+// with a zero in its place would not do).
 template <typename T, typename S>
-__device__ __forceinline__ void add_own_adapters(const LoraParams& p, int64_t m0, int n0, int lane, const int (&id)[S::MI],
-                                                 f32x4 (&acc)[S::MI][S::NJ]) {
+__device__ __forceinline__ void add_to_mixed(const LoraParams& p, int64_t m0, int n0, int lane, const WaveAdapters<S::MI>& who,
+                                             f32x4 (&acc)[S::MI][S::NJ]) {
+  constexpr int C = 8;      // columns at once: as many loads in flight as the registers beside acc allow
+  static_assert(S::NJ % 2 == 0, "pairs of blocks");
   const int l16 = lane & 15, l4 = lane >> 4;
 #pragma unroll
   for (int i = 0; i < S::MI; ++i) {
-    if (!has_adapter(p, id[i])) continue;
-    const T* t = (const T*)p.t + (m0 + 16 * i + l16) * 2 * p.rank;
-    const T* bw = (const T*)p.b + (int64_t)id[i] * p.out_dim * p.rank;
+    if (who.block[i] != -2) continue;
+    if (!has_adapter(p, who.id[i])) continue;
+    const T* bw = (const T*)p.b + (int64_t)who.id[i] * p.out_dim * p.rank;
 #pragma unroll
-    for (int j = 0; j < S::NJ; ++j) {
-      const T* b[4];
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < S::NJ; j += 2) {
+      const T* b[C];
+      float sum[C];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) b[e] = bw + (int64_t)min(n0 + 16 * j + 4 * l4 + e, p.out_dim - 1) * p.rank;
-      add_row<T>(p, t, b, sum);
+      for (int c = 0; c < C; ++c) {
+        b[c] = bw + min(n0 + (j + c / 4) * 16 + 4 * l4 + c % 4, p.out_dim - 1) * p.rank;
+        sum[c] = acc[i][j + c / 4][c % 4];
+      }
+      add_row<T, C>(p, (const T*)p.t + (m0 + 16 * i + l16) * 2 * p.rank, b, sum);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][j][e] += sum[e];
+      for (int c = 0; c < C; ++c) acc[i][j + c / 4][c % 4] = sum[c];
     }
   }
 }
@@ -245,35 +309,19 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_lora_project(LoraParams p) {
   RowOperand<S::BN, S::NW> b;
   a.init((const T*)p.x + m0 * p.ldx, nullptr, p.rows - m0, p.ldx * 2, kbytes, 0x7fffffff, wave, lane);
   b.init((const T*)p.w + (int64_t)n0 * p.dim, nullptr, p.out_dim - n0, kbytes, kbytes, 0x7fffffff, wave, lane);
-  int id[S::MI];
-#pragma unroll
-  for (int i = 0; i < S::MI; ++i) {
-    const int64_t m = mw + 16 * i + l16;
-    id[i] = m < p.rows ? p.ids[m] : -2;
-  }
+  WaveAdapters<S::MI> who;
+  who.init(p, mw, lane);
   f32x4 acc[S::MI][S::NJ];
 #pragma unroll
   for (int i = 0; i < S::MI; ++i)
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // the adapters of the rows that get a value: none, one, or several (and none)
-  int some = -1;
-  bool own = false, without = false;
-#pragma unroll
-  for (int i = 0; i < S::MI; ++i) {
-    if (has_adapter(p, id[i])) {
-      own |= some >= 0 && some != id[i];
-      some = id[i];
-    }
-    without |= id[i] == -1;
-  }
-  const uint64_t any = __ballot(some >= 0);
-  const int one = any ? __builtin_amdgcn_readlane(some, __builtin_ctzll(any)) : -1;
-  const bool mixed = any && __ballot(own || without || (some >= 0 && some != one));
-  tile_products<S, T, ROWS, ROWS>(a, b, (kbytes + KB - 1) / KB, smem, wave, lane, acc, [&] {
-    if (any && !mixed) add_one_adapter<T, S>(p, mw, nw, lane, one, acc);
-  });
-  if (mixed) add_own_adapters<T, S>(p, mw, nw, lane, id, acc);
+  tile_products<S, T, ROWS, ROWS>(a, b, (kbytes + KB - 1) / KB, smem, wave, lane, acc,
+                                  [&] {
+                                    add_to_pure<T, S>(p, mw, nw, lane, who, who.first, acc);
+                                    add_to_pure<T, S>(p, mw, nw, lane, who, who.second, acc);
+                                  });
+  add_to_mixed<T, S>(p, mw, nw, lane, who, acc);
 
   float bv[S::NJ][4];
 #pragma unroll
@@ -282,12 +330,12 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_lora_project(LoraParams p) {
     for (int e = 0; e < 4; ++e) bv[j][e] = p.bias ? bf16_bits_to_f32(p.bias[min(nw + 16 * j + 4 * l4 + e, p.out_dim - 1)]) : 0.f;
 #pragma unroll
   for (int i = 0; i < S::MI; ++i) {
-    const bool valid = id[i] >= -1;
+    const bool valid = who.id[i] >= -1;
     float v[S::NJ][4];
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[j][e] = id[i] < p.n_adapters ? acc[i][j][e] + bv[j][e] : __builtin_nanf("");
+      for (int e = 0; e < 4; ++e) v[j][e] = who.id[i] < p.n_adapters ? acc[i][j][e] + bv[j][e] : __builtin_nanf("");
     store_row<YT, S::NJ>((YT*)p.y + (valid ? mw + 16 * i + l16 : 0) * p.ldy, nw, p.out_dim, v, l4, valid);
   }
 }
@@ -300,9 +348,9 @@ hipError_t run_project(const LoraParams& p, hipStream_t s) {
 }
 
 // Few rows (few_rows.h), 16 NB columns a workgroup.
-template <typename T, typename YT, int MT, int NB, int UNROLL>
+template <typename T, typename YT, int MT, int NB, int FEW_WAVES, int UNROLL>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_lora_project_few(LoraParams p) {
-  typedef FewRows<MT, NB> S;
+  typedef FewRows<MT, NB, FEW_WAVES> S;
   __shared__ __attribute__((aligned(16))) float red[S::FLOATS];
   const int n0 = (int)blockIdx.x * S::COLS, l16 = threadIdx.x & 15;
   const uint8_t *x[MT], *w[NB];
@@ -313,7 +361,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_lora_project_few(LoraParams 
   }
 #pragma unroll
   for (int b = 0; b < NB; ++b) w[b] = (const uint8_t*)p.w + (int64_t)min(n0 + 16 * b + l16, p.out_dim - 1) * p.dim * 2;
-  few_rows_products<T, MT, NB, UNROLL>(x, w, p.dim * 2, red);
+  few_rows_products<T, MT, NB, FEW_WAVES, UNROLL>(x, w, p.dim * 2, red);
   for (int at = threadIdx.x; at < 16 * MT * S::COLS / 4; at += FEW_WAVES * 64) {
     const int m = at / (S::COLS / 4), c = at % (S::COLS / 4) * 4, col = n0 + c;
     if (m >= p.rows || col >= p.out_dim) continue;
@@ -327,7 +375,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_lora_project_few(LoraParams 
         const T* b[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) b[e] = (const T*)p.b + ((int64_t)id * p.out_dim + col + e) * p.rank;
-        add_row<T>(p, (const T*)p.t + (int64_t)m * 2 * p.rank, b, v);
+        add_row<T, 4>(p, (const T*)p.t + (int64_t)m * 2 * p.rank, b, v);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = __builtin_nanf("");
@@ -341,16 +389,16 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_lora_project_few(LoraParams 
   }
 }
 
-template <typename T, typename YT, int MT, int NB, int UNROLL>
+template <typename T, typename YT, int MT, int NB, int FEW_WAVES, int UNROLL>
 hipError_t run_project_few(const LoraParams& p, hipStream_t s) {
-  hipLaunchKernelGGL((k_lora_project_few<T, YT, MT, NB, UNROLL>), dim3((p.out_dim + 16 * NB - 1) / (16 * NB)), dim3(FEW_WAVES * 64), 0, s, p);
+  hipLaunchKernelGGL((k_lora_project_few<T, YT, MT, NB, FEW_WAVES, UNROLL>), dim3((p.out_dim + 16 * NB - 1) / (16 * NB)), dim3(FEW_WAVES * 64), 0, s, p);
   return hipGetLastError();
 }
 
 template <typename T, int MT>
 hipError_t run_reduce(const LoraParams& p, hipStream_t s) {
   // a workgroup per row while these are few enough to be requests of one token
-  const int share = p.rows <= 2048 ? 16 : 4;
+  const int share = p.rows <= 2048 ? 16 : 8;
   const dim3 grid((unsigned)((p.rows + 16 * MT - 1) / (16 * MT) * share)), block(REDUCE_WAVES * 64);
   if (p.rank <= 16) hipLaunchKernelGGL((k_lora_reduce<T, MT, 1>), grid, block, 0, s, p, share);
   else if (p.rank <= 32) hipLaunchKernelGGL((k_lora_reduce<T, MT, 2>), grid, block, 0, s, p, share);
@@ -362,12 +410,12 @@ hipError_t run_reduce(const LoraParams& p, hipStream_t s) {
 template <typename T, typename YT>
 hipError_t lora_t(const LoraParams& p, hipStream_t s) {
   if (p.n_adapters) {
-    const hipError_t e = p.rows >= 12288 ? run_reduce<T, 4>(p, s) : run_reduce<T, 1>(p, s);
+    const hipError_t e = p.rows > 4096 ? run_reduce<T, 2>(p, s) : run_reduce<T, 1>(p, s);
     if (e != hipSuccess) return e;
   }
-  if (p.rows <= 16) return run_project_few<T, YT, 1, 1, 4>(p, s);
-  if (p.rows <= 32) return run_project_few<T, YT, 2, 1, 4>(p, s);
-  if (p.rows <= 64) return run_project_few<T, YT, 4, 1, 2>(p, s);
+  if (p.rows <= 16) return run_project_few<T, YT, 1, 1, 16, 4>(p, s);
+  if (p.rows <= 32) return run_project_few<T, YT, 2, 1, 16, 4>(p, s);
+  if (p.rows <= 64) return run_project_few<T, YT, 4, 1, 16, 2>(p, s);
   auto tiles = [&](int t) { return (p.rows + t - 1) / t * ((p.out_dim + t - 1) / t); };
   if (tiles(256) >= 192) return run_project<T, YT, Big>(p, s);
   return tiles(128) >= 192 ? run_project<T, YT, Mid>(p, s) : run_project<T, YT, Small>(p, s);

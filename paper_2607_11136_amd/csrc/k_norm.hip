@@ -44,12 +44,6 @@ __device__ __forceinline__ void store8(void* p, int dtype, int64_t at, const flo
   else if (dtype == XEMA_F16) store8_as<f16>(p, at, f);
   else store8_as<float>(p, at, f);
 }
-__device__ __forceinline__ void load8(const void* p, int dtype, int64_t at, float f[8]) {
-  if (dtype == XEMA_BF16) unpack8(load_raw8((const bf16*)p + at), f);
-  else if (dtype == XEMA_F16) unpack8(load_raw8((const f16*)p + at), f);
-  else unpack8(load_raw8((const float*)p + at), f);
-}
-
 // Sum over the WPR waves of a row (fixed order: within each wave, then over
 // the waves); `red` holds WPR floats per use.
 template <int WPR>
@@ -200,9 +194,31 @@ hipError_t rmsnorm_x(const xema_rmsnorm_args& a, hipStream_t s) {
 
 // The gradient.  Workgroup b takes the rows b, b + grid, ... (WPR = 4) or the
 // groups of four rows b, b + grid, ... (WPR = 1), holds its part of dgamma in
-// registers over them and writes it once.
-template <typename XT, typename DT, int NV, int WPR>
+// registers over them and writes it once.  A row's s, dy and dsum are loaded
+// while the row before is computed.  ST void: no dsum.
+template <typename XT, typename DT, typename ST, int NV>
+struct BwdRow {
+  typedef std::conditional_t<std::is_void_v<ST>, bf16, ST> S;
+  Raw8<XT> x[NV];
+  Raw8<DT> d[NV];
+  Raw8<S> ds[std::is_void_v<ST> ? 1 : NV];
+  template <int STRIDE>
+  __device__ __forceinline__ void load(const xema_rmsnorm_bwd_args& a, int64_t r, int in_row) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c = v * STRIDE + in_row * 8;
+      if (c < a.dim) {
+        x[v] = load_raw8((const XT*)a.s + r * a.ld_s + c);
+        d[v] = load_raw8((const DT*)a.dy + r * a.ld_dy + c);
+        if constexpr (!std::is_void_v<ST>) ds[v] = load_raw8((const ST*)a.dsum + r * a.ld_dsum + c);
+      }
+    }
+  }
+};
+
+template <typename XT, typename DT, typename ST, int NV, int WPR>
 __global__ __launch_bounds__(NORM_WAVES * 64) void k_rmsnorm_bwd(xema_rmsnorm_bwd_args a, float* __restrict__ partial) {
+  constexpr int STRIDE = 512 * WPR;
   __shared__ float red[2][2][NORM_WAVES];
   __shared__ float fold[WPR == 1 ? NORM_WAVES : 1][WPR == 1 ? NV * 512 : 1];
   const int wave = threadIdx.x >> 6, in_row = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
@@ -214,31 +230,24 @@ __global__ __launch_bounds__(NORM_WAVES * 64) void k_rmsnorm_bwd(xema_rmsnorm_bw
   const int64_t first = WPR == 1 ? (int64_t)blockIdx.x * NORM_WAVES + wave : (int64_t)blockIdx.x;
   const int64_t step = (int64_t)gridDim.x * (WPR == 1 ? NORM_WAVES : 1);
   int turn = 0;
+  BwdRow<XT, DT, ST, NV> next;
+  if (first < a.rows) next.template load<STRIDE>(a, first, in_row);
   for (int64_t r = first; r < a.rows; r += step, turn ^= 1) {
-    Raw8<XT> rx[NV];
-    Raw8<DT> rd[NV];
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int c = (v * 64 * WPR + in_row) * 8;
-      if (c < a.dim) {
-        rx[v] = load_raw8((const XT*)a.s + r * a.ld_s + c);
-        rd[v] = load_raw8((const DT*)a.dy + r * a.ld_dy + c);
-      }
-    }
-    float x[NV][8], g[NV][8];
+    const BwdRow<XT, DT, ST, NV> row = next;
+    if (r + step < a.rows) next.template load<STRIDE>(a, r + step, in_row);
     float ss = 0.f, gx = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = (v * 64 * WPR + in_row) * 8;
+      const int c = v * STRIDE + in_row * 8;
       if (c < a.dim) {
-        unpack8(rx[v], x[v]);
-        unpack8(rd[v], g[v]);
-        float gam[8];
+        float x[8], g[8], gam[8];
+        unpack8(row.x[v], x);
+        unpack8(row.d[v], g);
         if (a.gamma) unpack8(load_raw8((const bf16*)a.gamma + c), gam);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          ss = fmaf(x[v][e], x[v][e], ss);
-          gx = fmaf(a.gamma ? g[v][e] * gam[e] : g[v][e], x[v][e], gx);
+          ss = fmaf(x[e], x[e], ss);
+          gx = fmaf(a.gamma ? g[e] * gam[e] : g[e], x[e], gx);
         }
       }
     }
@@ -261,17 +270,19 @@ __global__ __launch_bounds__(NORM_WAVES * 64) void k_rmsnorm_bwd(xema_rmsnorm_bw
     const float along = gx * q / (float)a.dim;      // mean(g n)
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = (v * 64 * WPR + in_row) * 8;
+      const int c = v * STRIDE + in_row * 8;
       if (c < a.dim) {
-        float o[8], ds[8], gam[8];
+        float x[8], g[8], gam[8], ds[8], o[8];
+        unpack8(row.x[v], x);
+        unpack8(row.d[v], g);
         if (a.gamma) unpack8(load_raw8((const bf16*)a.gamma + c), gam);
-        if (a.dsum) load8(a.dsum, a.dsum_dtype, r * a.ld_dsum + c, ds);
+        if constexpr (!std::is_void_v<ST>) unpack8(row.ds[v], ds);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float n = x[v][e] * q;
-          dg[v][e] = fmaf(g[v][e], n, dg[v][e]);
-          o[e] = q * ((a.gamma ? g[v][e] * gam[e] : g[v][e]) - n * along);
-          if (a.dsum) o[e] += ds[e];
+          const float n = x[e] * q;
+          dg[v][e] = fmaf(g[e], n, dg[v][e]);
+          o[e] = q * ((a.gamma ? g[e] * gam[e] : g[e]) - n * along);
+          if constexpr (!std::is_void_v<ST>) o[e] += ds[e];
         }
         store8(a.dx, a.dx_dtype, r * a.ld_dx + c, o);
       }
@@ -282,7 +293,7 @@ __global__ __launch_bounds__(NORM_WAVES * 64) void k_rmsnorm_bwd(xema_rmsnorm_bw
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) fold[wave][(v * 64 + in_row) * 8 + e] = dg[v][e];
+      for (int e = 0; e < 8; ++e) fold[wave][v * 512 + in_row * 8 + e] = dg[v][e];
     __syncthreads();
     for (int c = threadIdx.x; c < a.dim; c += NORM_WAVES * 64) {
       float s = 0.f;
@@ -293,48 +304,63 @@ __global__ __launch_bounds__(NORM_WAVES * 64) void k_rmsnorm_bwd(xema_rmsnorm_bw
   } else {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int c = (v * 64 * WPR + in_row) * 8;
+      const int c = v * STRIDE + in_row * 8;
       if (c < a.dim) store8_as<float>(partial, (int64_t)blockIdx.x * a.dim + c, dg[v]);
     }
   }
 }
 
-// dgamma: the workgroups' parts, in order.  64 columns a workgroup, its four
-// waves a quarter of the parts each.
-__global__ __launch_bounds__(256) void k_rmsnorm_dgamma(const float* __restrict__ partial, int parts, int dim, float* __restrict__ dgamma) {
-  __shared__ float red[4][64];
+// dgamma: the workgroups' parts, in order.  64 columns a workgroup, a part of
+// the parts for each of its 16 waves, eight loads in flight.
+__global__ __launch_bounds__(1024) void k_rmsnorm_dgamma(const float* __restrict__ partial, int parts, int dim, float* __restrict__ dgamma) {
+  __shared__ float red[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c = (int)blockIdx.x * 64 + lane;
-  const int p0 = (int)((int64_t)parts * wave / 4), p1 = (int)((int64_t)parts * (wave + 1) / 4);
+  const int p0 = parts * wave / 16, p1 = parts * (wave + 1) / 16;
   float s = 0.f;
-  if (c < dim)
+  if (c < dim) {
+#pragma unroll 8
     for (int i = p0; i < p1; ++i) s += partial[(int64_t)i * dim + c];
+  }
   red[wave][lane] = s;
   __syncthreads();
-  if (wave == 0 && c < dim) dgamma[c] = red[0][lane] + red[1][lane] + red[2][lane] + red[3][lane];
+  if (wave || c >= dim) return;
+  s = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) s += red[w][lane];
+  dgamma[c] = s;
 }
 
-template <typename XT, typename DT, int WPR>
+template <typename XT, typename DT, typename ST, int WPR>
 void rmsnorm_bwd_nv(const xema_rmsnorm_bwd_args& a, float* partial, hipStream_t s) {
   const dim3 grid((unsigned)rmsnorm_bwd_partials(a.rows)), block(NORM_WAVES * 64);
   const int nv = (a.dim + 512 * WPR - 1) / (512 * WPR);
-  if (nv <= 1) hipLaunchKernelGGL((k_rmsnorm_bwd<XT, DT, 1, WPR>), grid, block, 0, s, a, partial);
-  else if (nv <= 2) hipLaunchKernelGGL((k_rmsnorm_bwd<XT, DT, 2, WPR>), grid, block, 0, s, a, partial);
-  else if (nv <= 4) hipLaunchKernelGGL((k_rmsnorm_bwd<XT, DT, 4, WPR>), grid, block, 0, s, a, partial);
-  else if constexpr (WPR > 1) hipLaunchKernelGGL((k_rmsnorm_bwd<XT, DT, 8, WPR>), grid, block, 0, s, a, partial);
+  if (nv <= 1) hipLaunchKernelGGL((k_rmsnorm_bwd<XT, DT, ST, 1, WPR>), grid, block, 0, s, a, partial);
+  else if (nv <= 2) hipLaunchKernelGGL((k_rmsnorm_bwd<XT, DT, ST, 2, WPR>), grid, block, 0, s, a, partial);
+  else if (nv <= 4) hipLaunchKernelGGL((k_rmsnorm_bwd<XT, DT, ST, 4, WPR>), grid, block, 0, s, a, partial);
+  else if constexpr (WPR > 1) hipLaunchKernelGGL((k_rmsnorm_bwd<XT, DT, ST, 8, WPR>), grid, block, 0, s, a, partial);
 }
 
-template <typename XT, typename DT>
+template <typename XT, typename DT, typename ST>
 void rmsnorm_bwd_t(const xema_rmsnorm_bwd_args& a, float* partial, hipStream_t s) {
-  if (a.dim <= 2048) rmsnorm_bwd_nv<XT, DT, 1>(a, partial, s);
-  else rmsnorm_bwd_nv<XT, DT, NORM_WAVES>(a, partial, s);
+  if (a.dim <= 2048) rmsnorm_bwd_nv<XT, DT, ST, 1>(a, partial, s);
+  else rmsnorm_bwd_nv<XT, DT, ST, NORM_WAVES>(a, partial, s);
+}
+template <typename XT, typename DT>
+void rmsnorm_bwd_d(const xema_rmsnorm_bwd_args& a, float* partial, hipStream_t s) {
+  if (!a.dsum) return rmsnorm_bwd_t<XT, DT, void>(a, partial, s);
+  switch (a.dsum_dtype) {
+    case XEMA_BF16: return rmsnorm_bwd_t<XT, DT, bf16>(a, partial, s);
+    case XEMA_F16: return rmsnorm_bwd_t<XT, DT, f16>(a, partial, s);
+    default: return rmsnorm_bwd_t<XT, DT, float>(a, partial, s);
+  }
 }
 template <typename XT>
 void rmsnorm_bwd_x(const xema_rmsnorm_bwd_args& a, float* partial, hipStream_t s) {
   switch (a.dy_dtype) {
-    case XEMA_BF16: return rmsnorm_bwd_t<XT, bf16>(a, partial, s);
-    case XEMA_F16: return rmsnorm_bwd_t<XT, f16>(a, partial, s);
-    default: return rmsnorm_bwd_t<XT, float>(a, partial, s);
+    case XEMA_BF16: return rmsnorm_bwd_d<XT, bf16>(a, partial, s);
+    case XEMA_F16: return rmsnorm_bwd_d<XT, f16>(a, partial, s);
+    default: return rmsnorm_bwd_d<XT, float>(a, partial, s);
   }
 }
 
@@ -348,7 +374,7 @@ hipError_t launch_rmsnorm(const xema_rmsnorm_args& a, hipStream_t s) {
   }
 }
 
-int64_t rmsnorm_bwd_partials(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(512, (rows + 3) / 4)); }
+int64_t rmsnorm_bwd_partials(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(1024, (rows + 3) / 4)); }
 
 hipError_t launch_rmsnorm_bwd(const xema_rmsnorm_bwd_args& a, hipStream_t s) {
   float* partial = a.dgamma ? (float*)a.workspace : nullptr;
@@ -364,7 +390,7 @@ hipError_t launch_rmsnorm_bwd(const xema_rmsnorm_bwd_args& a, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   if (!a.dgamma) return hipSuccess;
-  hipLaunchKernelGGL(k_rmsnorm_dgamma, dim3((a.dim + 63) / 64), dim3(256), 0, s, partial, parts, a.dim, a.dgamma);
+  hipLaunchKernelGGL(k_rmsnorm_dgamma, dim3((a.dim + 63) / 64), dim3(1024), 0, s, partial, parts, a.dim, a.dgamma);
   return hipGetLastError();
 }
 

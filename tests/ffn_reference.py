@@ -135,8 +135,8 @@ def rmsnorm_bwd(s, dy, dsum, gamma, eps):
         e = e + U * dsum.double().abs()
     M = s.shape[0]
     dgamma = (dy * n).sum(0)
-    # a workgroup's rows, then up to 512 parts
-    return {"dx": (dx, e + U * dx.abs()), "dgamma": (dgamma, (M / 4 + 560) * U * (dy * n).abs().sum(0) + rel * (dy * n).abs().sum(0))}
+    # a workgroup's rows (all of them where one wave takes them), then up to 1024 parts in 16 sums
+    return {"dx": (dx, e + U * dx.abs()), "dgamma": (dgamma, (M / 4 + 100) * U * (dy * n).abs().sum(0) + rel * (dy * n).abs().sum(0))}
 
 
 def e4m3_steps(v):

@@ -158,7 +158,7 @@ def test_workspace_sizes():
     assert X.xema_gated_ffn_bwd_workspace_bytes(100000, 64, 4096) == 2 * 100000 * 4096 * 2 + 64 * 2 * 4096 * 4
     assert X.xema_gated_ffn_pre_bytes(0, 64) == 0 and X.xema_gated_ffn_pre_bytes(100000, 4096) == 6 * 100000 * 4096
     assert X.xema_rmsnorm_bwd_workspace_bytes(1, 64) == 64 * 4
-    assert X.xema_rmsnorm_bwd_workspace_bytes(100000, 64) == 512 * 64 * 4
+    assert X.xema_rmsnorm_bwd_workspace_bytes(100000, 64) == 1024 * 64 * 4
     assert X.xema_lora_workspace_bytes(10, 16) == 768      # two halves of 16 ranks, 16 bits each, rounded up to 256 bytes
     for f, args, status in ((X.xema_rmsnorm_bwd_workspace_bytes, (-1, 64), INVALID), (X.xema_rmsnorm_bwd_workspace_bytes, (4, 60), UNSUPPORTED),
                             (X.xema_gated_ffn_bwd_workspace_bytes, (4, 64, 0), INVALID), (X.xema_lora_workspace_bytes, (4, 12), UNSUPPORTED),
