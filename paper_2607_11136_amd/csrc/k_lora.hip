@@ -44,51 +44,48 @@ __device__ __forceinline__ void store_reduced(T* t, int rank, int q, const float
   *reinterpret_cast<t8*>(t + rank + q) = lo;
 }
 
-// t[r] = scale[i] x[r] a[i]^T as value and remainder.  `share` workgroups per
-// block of 16 MT rows.  Where the rows of a block that have an adapter share
-// it, the block's first workgroup multiplies all of them on MFMA, its waves
-// interleaved pieces of k, and the others have nothing to do; otherwise they
-// take the rows in turn, four ranks a wave at a time.
+// t[r] = scale[i] x[r] a[i]^T as value and remainder.  A workgroup per block of
+// 16 MT rows multiplies all of them on MFMA with the adapter that they share,
+// its waves a part of k each; where a block has several adapters (requests
+// that meet in it), with one after the other, and a row keeps its own.
 template <typename T, int MT, int RT>
-__global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p, int share) {
-  typedef T t8 __attribute__((ext_vector_type(8)));
+__global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p) {
   typedef typename Frag<T>::type frag;
   constexpr int RB = 16 * MT, RR = 16 * RT;
   __shared__ __attribute__((aligned(16))) float red[REDUCE_WAVES][RB][RR + 4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, l4 = lane >> 4;
-  // (workgroups go round the 8 XCDs in turn: the first of each block must not
-  // always meet the same one)
-  const int mine = (int)((blockIdx.x + blockIdx.x / share) % share);
-  const int64_t m0 = (int64_t)(blockIdx.x / share) * RB;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, l4 = lane >> 4;
+  const int64_t m0 = (int64_t)blockIdx.x * RB;
   const int id = lane < RB && m0 + lane < p.rows ? p.ids[m0 + lane] : -2;
-  const uint64_t live = __ballot(has_adapter(p, id));
-  if (!live) return;
-  const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(live));
-  if (__ballot(id == one) == live) {
-    if (mine) return;
-    const T* a = (const T*)p.a + (int64_t)one * p.rank * p.dim;
-    const T *xr[MT], *ar[RT];
+  const T* xr[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int64_t m = m0 + 16 * i + l16;
-      xr[i] = (const T*)p.x + (m < p.rows ? m : p.rows - 1) * p.ldx;
-    }
+  for (int i = 0; i < MT; ++i) {
+    const int64_t m = m0 + 16 * i + l16;
+    xr[i] = (const T*)p.x + (m < p.rows ? m : p.rows - 1) * p.ldx;
+  }
+  const int span = (p.dim + REDUCE_WAVES * 64 - 1) / (REDUCE_WAVES * 64) * 64;
+  const int begin = wave * span, end = min(begin + span, p.dim);
+  for (uint64_t todo = __ballot(has_adapter(p, id)); todo;) {
+    const int one = __builtin_amdgcn_readlane(id, __builtin_ctzll(todo));
+    const uint64_t rows = __ballot(id == one);
+    todo &= ~rows;
+    const float scale = p.scale[one];
+    const T* ar[RT];
 #pragma unroll
-    for (int q = 0; q < RT; ++q) ar[q] = a + (int64_t)min(16 * q + l16, p.rank - 1) * p.dim;
+    for (int q = 0; q < RT; ++q) ar[q] = (const T*)p.a + ((int64_t)one * p.rank + min(16 * q + l16, p.rank - 1)) * p.dim;
     f32x4 acc[MT][RT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int q = 0; q < RT; ++q) acc[i][q] = f32x4{0.f, 0.f, 0.f, 0.f};
     constexpr int UNROLL = RT + MT <= 4 ? 2 : 1;
-    for (int k0 = wave * 64; k0 < p.dim; k0 += REDUCE_WAVES * 64 * UNROLL) {
+    for (int k0 = begin; k0 < end; k0 += 64 * UNROLL) {
       frag fx[UNROLL][2][MT], fa[UNROLL][2][RT];
 #pragma unroll
       for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int k = k0 + u * REDUCE_WAVES * 64 + 32 * h + 8 * l4;
-          const bool in = k < p.dim;
+          const int k = k0 + u * 64 + 32 * h + 8 * l4;
+          const bool in = k < end;
 #pragma unroll
           for (int i = 0; i < MT; ++i) {
             fx[u][h][i] = frag{};
@@ -114,10 +111,9 @@ __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p,
 #pragma unroll
       for (int q = 0; q < RT; ++q) *reinterpret_cast<f32x4*>(&red[wave][16 * i + l16][16 * q + 4 * l4]) = acc[i][q];
     __syncthreads();
-    const float scale = p.scale[one];
     for (int at = threadIdx.x; at < RB * p.rank / 8; at += REDUCE_WAVES * 64) {
       const int row = at / (p.rank / 8), q = at % (p.rank / 8) * 8;
-      if (!(live >> row & 1)) continue;
+      if (!(rows >> row & 1)) continue;
       float s[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -128,50 +124,54 @@ __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p,
       }
       store_reduced<T>((T*)p.t + (m0 + row) * 2 * p.rank, p.rank, q, s);
     }
-    return;
+    if (todo) __syncthreads();
   }
-  // four ranks a wave at a time; where that leaves waves over, k in parts too
-  float* sums = &red[0][0][0];                                   // [parts][rank]
+}
+
+// The same for few rows: a workgroup per row, four ranks a wave at a time;
+// where that leaves waves over, k in parts too.
+template <typename T>
+__global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce_rows(LoraParams p) {
+  typedef T t8 __attribute__((ext_vector_type(8)));
+  __shared__ float sums[REDUCE_WAVES * 16];                      // [parts][rank], at most 8 x 16 or 1 x 128
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t r = blockIdx.x;
+  const int own = p.ids[r];
+  if (!has_adapter(p, own)) return;
+  const float scale = p.scale[own];
   const int batches = min(p.rank / 4, REDUCE_WAVES), parts = REDUCE_WAVES / batches;
   const int batch = wave % batches, part = wave / batches;       // (part `parts`: waves that no batch needs)
-  for (int row = mine; row < RB; row += share) {
-    if (!(live >> row & 1)) continue;
-    const int own = __builtin_amdgcn_readlane(id, row);
-    const float scale = p.scale[own];
-    const T* x = (const T*)p.x + (m0 + row) * p.ldx;
-    const T* a = (const T*)p.a + (int64_t)own * p.rank * p.dim;
-    if (part < parts)
-      for (int q = batch * 4; q < p.rank; q += batches * 4) {
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
+  const T* x = (const T*)p.x + r * p.ldx;
+  const T* a = (const T*)p.a + (int64_t)own * p.rank * p.dim;
+  if (part < parts)
+    for (int q = batch * 4; q < p.rank; q += batches * 4) {
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-        for (int k = part * 512 + lane * 8; k < p.dim; k += parts * 512) {
-          const t8 u = *reinterpret_cast<const t8*>(x + k);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const t8 v = *reinterpret_cast<const t8*>(a + (int64_t)(q + i) * p.dim + k);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s[i] = fmaf((float)u[e], (float)v[e], s[i]);
-          }
-        }
+      for (int k = part * 512 + lane * 8; k < p.dim; k += parts * 512) {
+        const t8 u = *reinterpret_cast<const t8*>(x + k);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          s[i] = wave_sum(s[i]);
-          if (lane == 0) sums[part * p.rank + q + i] = s[i];
+          const t8 v = *reinterpret_cast<const t8*>(a + (int64_t)(q + i) * p.dim + k);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s[i] = fmaf((float)u[e], (float)v[e], s[i]);
         }
       }
-    __syncthreads();
-    if ((int)threadIdx.x < p.rank / 8) {
-      float s[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        s[e] = 0.f;
-        for (int w = 0; w < parts; ++w) s[e] += sums[w * p.rank + threadIdx.x * 8 + e];
-        s[e] *= scale;
+      for (int i = 0; i < 4; ++i) {
+        s[i] = wave_sum(s[i]);
+        if (lane == 0) sums[part * p.rank + q + i] = s[i];
       }
-      store_reduced<T>((T*)p.t + (m0 + row) * 2 * p.rank, p.rank, (int)threadIdx.x * 8, s);
     }
-    __syncthreads();
+  __syncthreads();
+  if ((int)threadIdx.x >= p.rank / 8) return;
+  float s[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    s[e] = 0.f;
+    for (int w = 0; w < parts; ++w) s[e] += sums[w * p.rank + threadIdx.x * 8 + e];
+    s[e] *= scale;
   }
+  store_reduced<T>((T*)p.t + r * 2 * p.rank, p.rank, (int)threadIdx.x * 8, s);
 }
 
 // The adapters of a wave's rows by blocks of 16: a block is pure where all its
@@ -397,20 +397,29 @@ hipError_t run_project_few(const LoraParams& p, hipStream_t s) {
 
 template <typename T, int MT>
 hipError_t run_reduce(const LoraParams& p, hipStream_t s) {
-  // a workgroup per row while these are few enough to be requests of one token
-  const int share = p.rows <= 2048 ? 16 : 8;
-  const dim3 grid((unsigned)((p.rows + 16 * MT - 1) / (16 * MT) * share)), block(REDUCE_WAVES * 64);
-  if (p.rank <= 16) hipLaunchKernelGGL((k_lora_reduce<T, MT, 1>), grid, block, 0, s, p, share);
-  else if (p.rank <= 32) hipLaunchKernelGGL((k_lora_reduce<T, MT, 2>), grid, block, 0, s, p, share);
-  else if (p.rank <= 64) hipLaunchKernelGGL((k_lora_reduce<T, MT, 4>), grid, block, 0, s, p, share);
-  else hipLaunchKernelGGL((k_lora_reduce<T, MT, 8>), grid, block, 0, s, p, share);
+  const dim3 grid((unsigned)((p.rows + 16 * MT - 1) / (16 * MT))), block(REDUCE_WAVES * 64);
+  if (p.rank <= 16) hipLaunchKernelGGL((k_lora_reduce<T, MT, 1>), grid, block, 0, s, p);
+  else if (p.rank <= 32) hipLaunchKernelGGL((k_lora_reduce<T, MT, 2>), grid, block, 0, s, p);
+  else if (p.rank <= 64) hipLaunchKernelGGL((k_lora_reduce<T, MT, 4>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((k_lora_reduce<T, MT, 8>), grid, block, 0, s, p);
   return hipGetLastError();
+}
+
+// A row by itself reads all of its adapter's a, which pays while the rows are
+// few (and then likely single tokens, each with an adapter of its own).
+template <typename T>
+hipError_t reduce(const LoraParams& p, hipStream_t s) {
+  if (p.rows * p.rank <= 32768) {
+    hipLaunchKernelGGL((k_lora_reduce_rows<T>), dim3((unsigned)p.rows), dim3(REDUCE_WAVES * 64), 0, s, p);
+    return hipGetLastError();
+  }
+  return p.rows > 4096 ? run_reduce<T, 2>(p, s) : run_reduce<T, 1>(p, s);
 }
 
 template <typename T, typename YT>
 hipError_t lora_t(const LoraParams& p, hipStream_t s) {
   if (p.n_adapters) {
-    const hipError_t e = p.rows > 4096 ? run_reduce<T, 2>(p, s) : run_reduce<T, 1>(p, s);
+    const hipError_t e = reduce<T>(p, s);
     if (e != hipSuccess) return e;
   }
   if (p.rows <= 16) return run_project_few<T, YT, 1, 1, 16, 4>(p, s);
