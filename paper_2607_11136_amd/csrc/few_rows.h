@@ -14,8 +14,8 @@ namespace xema {
 template <int MT, int NB, int WAVES_>
 struct FewRows {
   static constexpr int WAVES = WAVES_;
-  static constexpr int COLS = 16 * NB, ROW = COLS + 4;     // (padded against bank conflicts)
-  static constexpr int FLOATS = WAVES * 16 * MT * ROW;
+  static constexpr int ROWS = 16 * MT, COLS = 16 * NB, ROW = COLS + 4;     // (padded against bank conflicts)
+  static constexpr int FLOATS = WAVES * ROWS * ROW;
 };
 
 // One 16-row operand piece: the 32 bytes of a lane, zero past the last k.
@@ -28,9 +28,10 @@ __device__ __forceinline__ void load_piece(const uint8_t* row, int at, int kbyte
   }
 }
 
-// red[m * ROW + n] (of wave 0) = sum over k of x row m and weight row n, for
-// the weight rows w[b] (each lane's own row lane % 16 of block b) and the rows
-// x[i] of x (rows past the last may repeat one).  Ends with a barrier.
+// The waves' sums over k of x row m and weight row n at
+// red[(wave * 16 MT + m) * ROW + n], for the weight rows w[b] (each lane's own
+// row lane % 16 of block b) and the rows x[i] of x (rows past the last may
+// repeat one).  Ends with a barrier.
 template <typename T, int MT, int NB, int WAVES, int UNROLL>
 __device__ __forceinline__ void few_rows_products(const uint8_t* const (&x)[MT], const uint8_t* const (&w)[NB], int kbytes, float* red) {
   typedef FewRows<MT, NB, WAVES> S;
@@ -72,14 +73,22 @@ __device__ __forceinline__ void few_rows_products(const uint8_t* const (&x)[MT],
     for (int b = 0; b < NB; ++b)
       *reinterpret_cast<f32x4*>(red + (wave * 16 * MT + 16 * i + l16) * S::ROW + 16 * b + 4 * l4) = acc[i][b];
   __syncthreads();
-  for (int at = threadIdx.x; at < 16 * MT * S::COLS; at += WAVES * 64) {
-    float* p = red + at / S::COLS * S::ROW + at % S::COLS;
-    float s = p[0];
+}
+
+// Row m, columns n .. n + 3 of the product, the waves' sums in wave order.
+template <typename S>
+__device__ __forceinline__ f32x4 few_rows_sum4(const float* red, int m, int n) {
+  f32x4 s = *reinterpret_cast<const f32x4*>(red + m * S::ROW + n);
 #pragma unroll
-    for (int v = 1; v < WAVES; ++v) s += p[v * 16 * MT * S::ROW];
-    p[0] = s;
-  }
-  __syncthreads();
+  for (int v = 1; v < S::WAVES; ++v) s += *reinterpret_cast<const f32x4*>(red + (v * S::ROWS + m) * S::ROW + n);
+  return s;
+}
+template <typename S>
+__device__ __forceinline__ float few_rows_sum(const float* red, int m, int n) {
+  float s = red[m * S::ROW + n];
+#pragma unroll
+  for (int v = 1; v < S::WAVES; ++v) s += red[(v * S::ROWS + m) * S::ROW + n];
+  return s;
 }
 
 }  // namespace xema

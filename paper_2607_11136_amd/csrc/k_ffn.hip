@@ -173,7 +173,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_gated_few(GatedParams p) {
   // four units of one row per thread
   const int t = (int)threadIdx.x, m = t / 4, c = t % 4 * 4, col = n0 + c;
   if (m >= 16 * MT || m >= p.rows || col >= p.hidden) return;
-  const f32x4 rg = *reinterpret_cast<const f32x4*>(red + m * S::ROW + c), ru = *reinterpret_cast<const f32x4*>(red + m * S::ROW + 16 + c);
+  const f32x4 rg = few_rows_sum4<S>(red, m, c), ru = few_rows_sum4<S>(red, m, 16 + c);
   float g[4], u[4];
   typedef YT y4 __attribute__((ext_vector_type(4)));
   y4 y;

@@ -249,6 +249,7 @@ __device__ __forceinline__ void add_to_pure(const LoraParams& p, int64_t m0, int
 template <typename T, int C>
 __device__ __forceinline__ void add_row(const LoraParams& p, const T* t, const T* const (&b)[C], float (&sum)[C]) {
   typedef T t8 __attribute__((ext_vector_type(8)));
+#pragma unroll(C == 1 ? 4 : 1)
   for (int q = 0; q < p.rank; q += 8) {
     const t8 hi = *reinterpret_cast<const t8*>(t + q), lo = *reinterpret_cast<const t8*>(t + p.rank + q);
     t8 v[C];
@@ -351,6 +352,7 @@ hipError_t run_project(const LoraParams& p, hipStream_t s) {
 template <typename T, typename YT, int MT, int NB, int FEW_WAVES, int UNROLL>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_lora_project_few(LoraParams p) {
   typedef FewRows<MT, NB, FEW_WAVES> S;
+  static_assert(S::ROWS * S::COLS <= FEW_WAVES * 64, "an output a thread");
   __shared__ __attribute__((aligned(16))) float red[S::FLOATS];
   const int n0 = (int)blockIdx.x * S::COLS, l16 = threadIdx.x & 15;
   const uint8_t *x[MT], *w[NB];
@@ -361,32 +363,21 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_lora_project_few(LoraParams 
   }
 #pragma unroll
   for (int b = 0; b < NB; ++b) w[b] = (const uint8_t*)p.w + (int64_t)min(n0 + 16 * b + l16, p.out_dim - 1) * p.dim * 2;
+  // an output a thread (what it needs of its row besides is loaded first)
+  const int m = (int)threadIdx.x / S::COLS, c = (int)threadIdx.x % S::COLS, col = n0 + c;
+  const bool in = m < S::ROWS && m < p.rows && col < p.out_dim;
+  const int id = in ? p.ids[m] : -2;
+  const float bias = in && p.bias ? bf16_bits_to_f32(p.bias[col]) : 0.f;
   few_rows_products<T, MT, NB, FEW_WAVES, UNROLL>(x, w, p.dim * 2, red);
-  for (int at = threadIdx.x; at < 16 * MT * S::COLS / 4; at += FEW_WAVES * 64) {
-    const int m = at / (S::COLS / 4), c = at % (S::COLS / 4) * 4, col = n0 + c;
-    if (m >= p.rows || col >= p.out_dim) continue;
-    const int id = p.ids[m];
-    if (id < -1) continue;
-    float v[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = red[m * S::ROW + c + e] + (p.bias ? bf16_bits_to_f32(p.bias[col + e]) : 0.f);
-    if (id >= 0) {
-      if (id < p.n_adapters) {
-        const T* b[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) b[e] = (const T*)p.b + ((int64_t)id * p.out_dim + col + e) * p.rank;
-        add_row<T, 4>(p, (const T*)p.t + (int64_t)m * 2 * p.rank, b, v);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = __builtin_nanf("");
-      }
-    }
-    typedef YT y4 __attribute__((ext_vector_type(4)));
-    y4 y;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (YT)v[e];
-    *reinterpret_cast<y4*>((YT*)p.y + m * p.ldy + col) = y;
+  if (id < -1) return;
+  float v[1] = {few_rows_sum<S>(red, m, c) + bias};
+  if (id >= p.n_adapters) {
+    v[0] = __builtin_nanf("");
+  } else if (id >= 0) {
+    const T* const b[1] = {(const T*)p.b + ((int64_t)id * p.out_dim + col) * p.rank};
+    add_row<T, 1>(p, (const T*)p.t + (int64_t)m * 2 * p.rank, b, v);
   }
+  ((YT*)p.y)[m * p.ldy + col] = (YT)v[0];
 }
 
 template <typename T, typename YT, int MT, int NB, int FEW_WAVES, int UNROLL>
@@ -424,6 +415,7 @@ hipError_t lora_t(const LoraParams& p, hipStream_t s) {
   }
   if (p.rows <= 16) return run_project_few<T, YT, 1, 1, 16, 4>(p, s);
   if (p.rows <= 32) return run_project_few<T, YT, 2, 1, 16, 4>(p, s);
+  if (p.rows <= 48) return run_project_few<T, YT, 3, 1, 16, 2>(p, s);
   if (p.rows <= 64) return run_project_few<T, YT, 4, 1, 16, 2>(p, s);
   auto tiles = [&](int t) { return (p.rows + t - 1) / t * ((p.out_dim + t - 1) / t); };
   if (tiles(256) >= 192) return run_project<T, YT, Big>(p, s);
