@@ -10,11 +10,6 @@ namespace xema {
 
 namespace {
 
-typedef TileShape<256, 256, 2, 4, 0> Big;
-typedef TileShape<128, 256, 2, 4, 0> Wide;
-typedef TileShape<128, 128, 2, 2, 3> Mid;
-typedef TileShape<64, 64, 2, 2, 4> Small;
-
 // act(g), and act'(g) where asked.  GELU's tanh form is g p with
 // p = 1 / (1 + e^(-2z)), z = sqrt(2/pi) (g + 0.044715 g^3), so its slope is
 // p + g p (1 - p) 2 z'; past |g| = 30 p is 0 or 1 in fp32 and the second term 0.
@@ -206,22 +201,14 @@ hipError_t run_gated(const GatedParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-enum TileKind { BIG, MID, SMALL };
-// v1: the largest tile that still gives each CU one
-TileKind pick_tile(int64_t m, int64_t n) {
-  auto tiles = [&](int t) { return (m + t - 1) / t * ((n + t - 1) / t); };
-  return tiles(256) >= 192 ? BIG : tiles(128) >= 192 ? MID : SMALL;
-}
-
 template <typename T, typename YT>
 hipError_t gated_t(const GatedParams& p, hipStream_t s) {
+  // (weights from HBM, us, this kernel and the best tile: 16 x 2 4096 x 4096 17
+  // and 21, 32 rows 20 and 22; 16 x 2 11008 x 4096 40 and 39, 32 rows 51 and 40)
   if (p.rows <= 16) return run_gated_few<T, YT, 1, 4>(p, s);
-  if (p.rows <= 32) return run_gated_few<T, YT, 2, 2>(p, s);
-  switch (pick_tile(p.rows, 2 * (int64_t)p.hidden)) {
-    case BIG: return run_gated<T, YT, Big>(p, s);
-    case MID: return run_gated<T, YT, Mid>(p, s);
-    default: return run_gated<T, YT, Small>(p, s);
-  }
+  if (p.rows <= 32 && p.hidden <= 8192) return run_gated_few<T, YT, 2, 2>(p, s);
+  return with_tile(pick_tile(p.rows, 2 * (int64_t)p.hidden, ((int64_t)p.dim * sizeof(T) + KB - 1) / KB),
+                   [&](auto shape) { return run_gated<T, YT, decltype(shape)>(p, s); });
 }
 
 // dg = dy u act'(g), du = dy act(g), rounded to T, and the column sums of the
@@ -408,19 +395,12 @@ hipError_t bwd_t(const xema_gated_ffn_bwd_args& a, hipStream_t s) {
   }
   const BwdParams p{dg, du, a.gate_w, a.up_w, a.x, a.dx, a.dgate_w, a.dup_w, a.rows, a.ldx, a.ld_dx, a.dim, a.hidden};
   if (a.dx && a.rows > 0) {
-    switch (pick_tile(a.rows, a.dim)) {
-      case BIG: e = run_dx<T, Big>(p, s); break;
-      case MID: e = run_dx<T, Mid>(p, s); break;
-      default: e = run_dx<T, Small>(p, s); break;
-    }
+    e = with_tile(pick_tile(a.rows, a.dim, 2 * ((a.hidden + 63) / 64)), [&](auto shape) { return run_dx<T, decltype(shape)>(p, s); });
     if (e != hipSuccess) return e;
   }
   if (a.dgate_w) {
-    switch (pick_tile(2 * (int64_t)a.hidden, a.dim)) {
-      case BIG: return run_dw<T, Big>(p, s);
-      case MID: return run_dw<T, Mid>(p, s);
-      default: return run_dw<T, Small>(p, s);
-    }
+    // (the two gradients' tiles are apart where hidden is no multiple of a tile's)
+    return with_tile(pick_tile(2 * (int64_t)a.hidden, a.dim, (a.rows + 63) / 64), [&](auto shape) { return run_dw<T, decltype(shape)>(p, s); });
   }
   return e;
 }

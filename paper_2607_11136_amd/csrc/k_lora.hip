@@ -9,11 +9,6 @@ namespace xema {
 
 namespace {
 
-typedef TileShape<256, 256, 2, 4, 0> Big;
-typedef TileShape<128, 256, 2, 4, 0> Wide;
-typedef TileShape<128, 128, 2, 2, 3> Mid;
-typedef TileShape<64, 64, 2, 2, 4> Small;
-
 struct LoraParams {
   const void *x, *w; const uint16_t* bias;
   const void *a, *b; const float* scale;
@@ -249,7 +244,7 @@ __device__ __forceinline__ void add_to_pure(const LoraParams& p, int64_t m0, int
 template <typename T, int C>
 __device__ __forceinline__ void add_row(const LoraParams& p, const T* t, const T* const (&b)[C], float (&sum)[C]) {
   typedef T t8 __attribute__((ext_vector_type(8)));
-#pragma unroll(C == 1 ? 4 : 1)
+#pragma unroll(C <= 2 ? 4 : 1)
   for (int q = 0; q < p.rank; q += 8) {
     const t8 hi = *reinterpret_cast<const t8*>(t + q), lo = *reinterpret_cast<const t8*>(t + p.rank + q);
     t8 v[C];
@@ -352,7 +347,7 @@ hipError_t run_project(const LoraParams& p, hipStream_t s) {
 template <typename T, typename YT, int MT, int NB, int FEW_WAVES, int UNROLL>
 __global__ __launch_bounds__(FEW_WAVES * 64) void k_lora_project_few(LoraParams p) {
   typedef FewRows<MT, NB, FEW_WAVES> S;
-  static_assert(S::ROWS * S::COLS <= FEW_WAVES * 64, "an output a thread");
+  static_assert(S::ROWS * 16 <= FEW_WAVES * 64, "NB outputs a thread");
   __shared__ __attribute__((aligned(16))) float red[S::FLOATS];
   const int n0 = (int)blockIdx.x * S::COLS, l16 = threadIdx.x & 15;
   const uint8_t *x[MT], *w[NB];
@@ -363,21 +358,31 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_lora_project_few(LoraParams 
   }
 #pragma unroll
   for (int b = 0; b < NB; ++b) w[b] = (const uint8_t*)p.w + (int64_t)min(n0 + 16 * b + l16, p.out_dim - 1) * p.dim * 2;
-  // an output a thread (what it needs of its row besides is loaded first)
-  const int m = (int)threadIdx.x / S::COLS, c = (int)threadIdx.x % S::COLS, col = n0 + c;
+  // NB outputs a thread (what they need of their row besides is loaded first)
+  const int m = (int)threadIdx.x / 16, c = (int)threadIdx.x % 16 * NB, col = n0 + c;
   const bool in = m < S::ROWS && m < p.rows && col < p.out_dim;
   const int id = in ? p.ids[m] : -2;
-  const float bias = in && p.bias ? bf16_bits_to_f32(p.bias[col]) : 0.f;
+  float v[NB];
+#pragma unroll
+  for (int e = 0; e < NB; ++e) v[e] = in && p.bias ? bf16_bits_to_f32(p.bias[col + e]) : 0.f;
   few_rows_products<T, MT, NB, FEW_WAVES, UNROLL>(x, w, p.dim * 2, red);
   if (id < -1) return;
-  float v[1] = {few_rows_sum<S>(red, m, c) + bias};
+#pragma unroll
+  for (int e = 0; e < NB; ++e) v[e] += few_rows_sum<S>(red, m, c + e);
   if (id >= p.n_adapters) {
-    v[0] = __builtin_nanf("");
+#pragma unroll
+    for (int e = 0; e < NB; ++e) v[e] = __builtin_nanf("");
   } else if (id >= 0) {
-    const T* const b[1] = {(const T*)p.b + ((int64_t)id * p.out_dim + col) * p.rank};
-    add_row<T, 1>(p, (const T*)p.t + (int64_t)m * 2 * p.rank, b, v);
+    const T* b[NB];
+#pragma unroll
+    for (int e = 0; e < NB; ++e) b[e] = (const T*)p.b + ((int64_t)id * p.out_dim + col + e) * p.rank;
+    add_row<T, NB>(p, (const T*)p.t + (int64_t)m * 2 * p.rank, b, v);
   }
-  ((YT*)p.y)[m * p.ldy + col] = (YT)v[0];
+  typedef YT yn __attribute__((ext_vector_type(NB)));
+  yn y;
+#pragma unroll
+  for (int e = 0; e < NB; ++e) y[e] = (YT)v[e];
+  *reinterpret_cast<yn*>((YT*)p.y + m * p.ldy + col) = y;
 }
 
 template <typename T, typename YT, int MT, int NB, int FEW_WAVES, int UNROLL>
@@ -413,13 +418,24 @@ hipError_t lora_t(const LoraParams& p, hipStream_t s) {
     const hipError_t e = reduce<T>(p, s);
     if (e != hipSuccess) return e;
   }
-  if (p.rows <= 16) return run_project_few<T, YT, 1, 1, 16, 4>(p, s);
-  if (p.rows <= 32) return run_project_few<T, YT, 2, 1, 16, 4>(p, s);
-  if (p.rows <= 48) return run_project_few<T, YT, 3, 1, 16, 2>(p, s);
-  if (p.rows <= 64) return run_project_few<T, YT, 4, 1, 16, 2>(p, s);
-  auto tiles = [&](int t) { return (p.rows + t - 1) / t * ((p.out_dim + t - 1) / t); };
-  if (tiles(256) >= 192) return run_project<T, YT, Big>(p, s);
-  return tiles(128) >= 192 ? run_project<T, YT, Mid>(p, s) : run_project<T, YT, Small>(p, s);
+  // Few rows: one round of workgroups (one a CU), 16 or 32 columns each.  Past
+  // that, and past 64 rows, every workgroup's reading all of x costs more than
+  // the tiles (us, with the reduction; columns 16, 32, tiles):
+  //   48 x 4096 x 4096   25, 29, 31      48 x 4096 x 6144   41, 30, 31
+  //   16 x 4096 x 11008  35, 35, 31      48 x 4096 x 11008  59, 52, 34
+  if (p.rows <= 64 && p.out_dim <= 4096) {
+    if (p.rows <= 16) return run_project_few<T, YT, 1, 1, 16, 4>(p, s);
+    if (p.rows <= 32) return run_project_few<T, YT, 2, 1, 16, 4>(p, s);
+    if (p.rows <= 48) return run_project_few<T, YT, 3, 1, 16, 2>(p, s);
+    return run_project_few<T, YT, 4, 1, 16, 2>(p, s);
+  }
+  if (p.rows <= 64 && p.out_dim <= 8192) {
+    if (p.rows <= 16) return run_project_few<T, YT, 1, 2, 16, 4>(p, s);
+    if (p.rows <= 32) return run_project_few<T, YT, 2, 2, 16, 2>(p, s);
+    if (p.rows <= 48) return run_project_few<T, YT, 3, 2, 16, 2>(p, s);
+    return run_project_few<T, YT, 4, 2, 16, 1>(p, s);
+  }
+  return with_tile(pick_tile(p.rows, p.out_dim, (p.dim * 2 + KB - 1) / KB), [&](auto shape) { return run_project<T, YT, decltype(shape)>(p, s); });
 }
 
 }  // namespace

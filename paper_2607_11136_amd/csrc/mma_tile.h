@@ -22,6 +22,7 @@
 
 #include "device_common.h"
 #include "mma.h"
+#include "tile_rules.h"
 
 namespace xema {
 
@@ -241,6 +242,25 @@ struct TileShape {
   static constexpr int LDS = NS ? NS * STAGE : 2 * A_BYTES + 3 * B_BYTES;
 };
 
+// The tiles that launchers choose from (tile_rules.h), in FfnTile's order.
+typedef TileShape<256, 256, 2, 4, 0> Tile256x256;
+typedef TileShape<128, 256, 2, 4, 0> Tile128x256;
+typedef TileShape<128, 128, 2, 2, 0> Tile128x128;
+typedef TileShape<64, 128, 2, 2, 3> Tile64x128;
+typedef TileShape<64, 64, 2, 2, 4> Tile64x64;
+
+// run(shape) of the chosen tile.
+template <typename F>
+hipError_t with_tile(FfnTile t, F&& run) {
+  switch (t) {
+    case FFN_256x256: return run(Tile256x256());
+    case FFN_128x256: return run(Tile128x256());
+    case FFN_128x128: return run(Tile128x128());
+    case FFN_64x128: return run(Tile64x128());
+    default: return run(Tile64x64());
+  }
+}
+
 // acc += the tile's products over `steps` steps.  Fragments: the B operand's
 // is the MFMA's first, so that a lane ends with four consecutive columns of
 // one row: acc[i][j][e] is row wm WR + 16 i + lane % 16, column
@@ -307,13 +327,13 @@ __device__ __forceinline__ void tile_products_deep(const AOp& a, const BOp& b, i
                                                    f32x4 (&acc)[S::MI][S::NJ], F&& meanwhile) {
   typedef typename Frag<T>::type frag;
   constexpr int MI = S::MI, NJ = S::NJ, KK = Frag<T>::KK, PANELS = KK * MI;
-  constexpr int AHEAD = KK == 1 ? 3 : MI == 8 ? 5 : 4, RING = KK == 1 ? 4 : 8, MEET = PANELS - AHEAD;
+  constexpr int AHEAD = KK == 1 ? (MI == 8 ? 3 : 2) : MI == 8 ? 5 : 4, RING = KK == 1 ? 4 : 8, MEET = PANELS - AHEAD;
   static_assert(PANELS % RING == 0 && RING > AHEAD, "fragment registers");
   // LDS instructions of one fragment of A and of B
   constexpr int RA = AO == COLUMNS || sizeof(T) == 1 ? 2 : 1, RB = BO == COLUMNS || sizeof(T) == 1 ? 2 : 1;
   constexpr int B1 = MI == 8 ? 3 : 0;         // KK = 2: the panel from which B of the second k-step is read, over four
   static_assert(KK == 1 || (B1 + 4 <= MEET && MEET + 4 <= PANELS), "step read before the barrier");
-  static_assert(AOp::LOADS <= 2 * AHEAD && BOp::LOADS <= MEET, "loads of a step");
+  static_assert(AOp::LOADS <= 2 * AHEAD && BOp::LOADS <= 2 * MEET, "loads of a step");
   FragReader<T, S::BM, AO> ra;
   FragReader<T, S::BN, BO> rb;
   ra.init(wave / S::WNW * S::WR, lane);
@@ -353,10 +373,12 @@ __device__ __forceinline__ void tile_products_deep(const AOp& a, const BOp& b, i
         if (rb0) fw[KK == 1 ? P ^ 1 : 0][j] = rb.read(b_next, 0, j);
       }
       int loads = 0;
-      if (m < BOp::LOADS) {
-        b.issue(kt + 2, m, b_free, wave);
-        ++loads;
-      }
+#pragma unroll
+      for (int c = 0; c < BOp::LOADS; ++c)
+        if (m < MEET && (BOp::LOADS <= MEET ? c : c * MEET / BOp::LOADS) == m) {
+          b.issue(kt + 2, c, b_free, wave);
+          ++loads;
+        }
 #pragma unroll
       for (int c = 0; c < AOp::LOADS; ++c)
         if (m >= MEET && c * AHEAD / AOp::LOADS == m - MEET) {

@@ -112,6 +112,47 @@ inline GemmPick gemm_pick(int64_t M, int N, int K, int heads_dim) {
 }
 
 // ---------------------------------------------------------------------------
+// The feed-forward sub-block's products (mma_tile.h)
+// ---------------------------------------------------------------------------
+enum FfnTile { FFN_256x256, FFN_128x256, FFN_128x128, FFN_64x128, FFN_64x64, FFN_TILES };
+// Microseconds of a 128-byte step of k with few CUs busy and with all of them,
+// and of a tile beside its steps.  The first two tiles fill a CU.  Of the others
+// two share one, each hiding the other's latency: full_us is then the step of
+// such a pair.
+struct FfnCost { int rows, cols; double alone_us, full_us, tile_us; bool shares; };
+constexpr FfnCost kFfnCost[FFN_TILES] = {{256, 256, 1.03, 1.41, 6.6, false}, {128, 256, 0.63, 0.85, 4.1, false},
+                                         {128, 128, 0.52, 0.97, 4.2, true},  {64, 128, 0.35, 0.56, 3.2, true},
+                                         {64, 64, 0.265, 0.41, 2.7, true}};
+
+inline double ffn_tile_us(const FfnCost& c, int64_t m, int64_t n, int64_t steps) {
+  const int64_t tiles = (m + c.rows - 1) / c.rows * ((n + c.cols - 1) / c.cols);
+  const int64_t slots = c.shares ? 2 * RULE_CUS : RULE_CUS, rounds = tiles / slots, rest = tiles % slots;
+  // the last round runs at the few CUs' pace while half of them idle, and pairs
+  // are faster by up to 15% while few CUs have one
+  const double last = rest == 0                       ? 0
+                      : c.shares && rest > RULE_CUS   ? c.full_us * (0.85 + 0.15 * (rest - RULE_CUS) / RULE_CUS)
+                      : c.shares || rest <= RULE_CUS / 2 ? c.alone_us
+                                                         : c.alone_us + (c.full_us - c.alone_us) * (rest - RULE_CUS / 2) / (RULE_CUS / 2);
+  const double ends = (double)rounds + (rest ? 1 : 0);
+  return c.tile_us * (c.shares ? 0.5 + 0.5 * ends : ends) + (double)steps * (rounds * c.full_us + last);
+}
+
+// The tile for an m x n result of `steps` steps of k.  Over 304 calls (16 to 4096
+// rows, widths of 512 to 11008, the five products) the picked tile takes 0.8%
+// more than the fastest in the mean and 15% at most.  us, 256 x 256 tiles and
+// the picked one: 48 x 2 4096 x 4096 73 and 19; 777 x 2 4096 x 4096 76 and 53;
+// 1024 x 4096 x 4096 (projection) 75 and 39; 2048 x 2 11008 x 4096 271 and 271.
+inline FfnTile pick_tile(int64_t m, int64_t n, int64_t steps) {
+  int best = 0;
+  double least = 0;
+  for (int t = 0; t < FFN_TILES; ++t) {
+    const double us = ffn_tile_us(kFfnCost[t], m, n, steps);
+    if (t == 0 || us < least) { best = t; least = us; }
+  }
+  return (FfnTile)best;
+}
+
+// ---------------------------------------------------------------------------
 // k_upconv.  A tile is RG R fragments of 16 corners (a corner: the four outputs
 // between four source pixels) and 128 / RG channels.
 // ---------------------------------------------------------------------------

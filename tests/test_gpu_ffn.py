@@ -436,7 +436,8 @@ def spread_ids(rows, n, how, seed):
 
 LORA_SIZES = [(1, 8, 8, 8, 1), (1, 4096, 1032, 16, 3), (5, 72, 136, 8, 2), (48, 512, 1024, 16, 20), (65, 136, 200, 24, 4), (130, 328, 520, 64, 7),
               (257, 1544, 264, 128, 5), (700, 256, 2056, 32, 40), (1500, 192, 4104, 8, 3), (9000, 256, 1544, 16, 4),
-              (12500, 136, 520, 32, 5), (16, 2056, 72, 32, 3), (33, 1032, 88, 128, 2)]
+              (12500, 136, 520, 32, 5), (16, 2056, 72, 32, 3), (33, 1032, 88, 128, 2),
+              (7, 264, 4360, 16, 3), (20, 136, 4136, 24, 4), (47, 72, 8192, 8, 2), (64, 520, 4104, 40, 9), (64, 2056, 520, 16, 3), (30, 64, 8200, 8, 2)]
 
 
 @pytest.mark.parametrize("rows,dim,out_dim,rank,n", LORA_SIZES)
