@@ -271,106 +271,103 @@ __global__ __launch_bounds__(256) void k_gated_grad(const uint8_t* __restrict__ 
   }
 }
 
-// The chunks' column sums, in order, as bf16.
-__global__ __launch_bounds__(256) void k_gated_bias(const float* __restrict__ partial, int chunks, int hidden, uint16_t* __restrict__ dgate_b,
-                                                    uint16_t* __restrict__ dup_b) {
-  const int c = (int)blockIdx.x * 256 + threadIdx.x;
-  if (c >= 2 * hidden) return;
-  float v = 0.f;
-  for (int i = 0; i < chunks; ++i) v += partial[(int64_t)i * 2 * hidden + c];
-  (c < hidden ? dgate_b + c : dup_b + (c - hidden))[0] = __builtin_bit_cast(uint16_t, (bf16)v);
-}
-
 struct BwdParams {
   const void *dg, *du;          // [rows, hidden]
   const void *gate_w, *up_w;    // [hidden, dim]
   const void* x;
   void *dx, *dgate_w, *dup_w;
+  const float* partial;         // [chunks][2 hidden]
+  uint16_t *dgate_b, *dup_b;
   int64_t rows, ldx, ld_dx;
-  int dim, hidden;
+  int dim, hidden, chunks;
 };
+
+// The tile's accumulators as rows row0 + ... of a [rows, cols] matrix.
+template <typename T, typename S>
+__device__ __forceinline__ void store_tile(const f32x4 (&acc)[S::MI][S::NJ], T* out, int64_t ld, int64_t row0, int64_t rows, int col0, int cols,
+                                           int lane) {
+  const int l16 = lane & 15, l4 = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < S::MI; ++i) {
+    const int64_t m = row0 + 16 * i + l16;
+    const bool valid = m < rows;
+    float v[S::NJ][4];
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[j][e] = acc[i][j][e];
+    store_row<T, S::NJ>(out + (valid ? m : 0) * ld, col0, cols, v, l4, valid);
+  }
+}
+
+template <typename S>
+__host__ __device__ constexpr int tiles_of(int64_t rows, int cols) {
+  return (int)((rows + S::BM - 1) / S::BM) * ((cols + S::BN - 1) / S::BN);
+}
 
 // dx = dg Wg + du Wu: the weights are read k by k (a row of W is one k).
 template <typename T, typename S>
-__global__ __launch_bounds__(S::NW * 64, 1) void k_gated_dx(BwdParams p) {
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[S::LDS];
-  const int tiles_n = (p.dim + S::BN - 1) / S::BN, tiles_m = (int)((p.rows + S::BM - 1) / S::BM);
+__device__ __forceinline__ void dx_tile(const BwdParams& p, int wg, uint8_t* smem, int wave, int lane, f32x4 (&acc)[S::MI][S::NJ]) {
   int tm, tn;
-  tile_of((int)blockIdx.x, tiles_m, tiles_n, 1024 / S::BM, &tm, &tn);
+  tile_of(wg, (int)((p.rows + S::BM - 1) / S::BM), (p.dim + S::BN - 1) / S::BN, 1024 / S::BM, &tm, &tn);
   const int64_t m0 = (int64_t)tm * S::BM;
-  const int n0 = tn * S::BN;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int steps = (p.hidden + 63) / 64;
+  const int n0 = tn * S::BN, steps = (p.hidden + 63) / 64;
   RowOperand<S::BM, S::NW> a;
   ColumnOperand<S::BN, S::NW> b;
   a.init((const T*)p.dg + m0 * p.hidden, (const T*)p.du + m0 * p.hidden, p.rows - m0, (int64_t)p.hidden * 2, p.hidden * 2, steps, wave, lane);
   b.init((const T*)p.gate_w + n0, (const T*)p.up_w + n0, p.dim - n0, (int64_t)p.dim * 2, p.hidden, steps, wave, lane);
-  f32x4 acc[S::MI][S::NJ];
-#pragma unroll
-  for (int i = 0; i < S::MI; ++i)
-#pragma unroll
-    for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   tile_products<S, T, ROWS, COLUMNS>(a, b, 2 * steps, smem, wave, lane, acc);
-  const int l16 = lane & 15, l4 = lane >> 4;
-#pragma unroll
-  for (int i = 0; i < S::MI; ++i) {
-    const int64_t m = m0 + wave / S::WNW * S::WR + 16 * i + l16;
-    const bool valid = m < p.rows;
-    float v[S::NJ][4];
-#pragma unroll
-    for (int j = 0; j < S::NJ; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[j][e] = acc[i][j][e];
-    store_row<T, S::NJ>((T*)p.dx + (valid ? m : 0) * p.ld_dx, n0 + wave % S::WNW * S::WC, p.dim, v, l4, valid);
-  }
+  store_tile<T, S>(acc, (T*)p.dx, p.ld_dx, m0 + wave / S::WNW * S::WR, p.rows, n0 + wave % S::WNW * S::WC, p.dim, lane);
 }
 
 // dWg = dg^T x and dWu = du^T x: both operands are read k (row) by k.
 template <typename T, typename S>
-__global__ __launch_bounds__(S::NW * 64, 1) void k_gated_dw(BwdParams p) {
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[S::LDS];
-  const int tiles_n = (p.dim + S::BN - 1) / S::BN, tiles_h = (p.hidden + S::BM - 1) / S::BM;
+__device__ __forceinline__ void dw_tile(const BwdParams& p, int wg, uint8_t* smem, int wave, int lane, f32x4 (&acc)[S::MI][S::NJ]) {
+  const int tiles_h = (p.hidden + S::BM - 1) / S::BM;
   int tm, tn;
-  tile_of((int)blockIdx.x, 2 * tiles_h, tiles_n, 1024 / S::BM, &tm, &tn);
+  tile_of(wg, 2 * tiles_h, (p.dim + S::BN - 1) / S::BN, 1024 / S::BM, &tm, &tn);
   const bool up = tm >= tiles_h;
   const int m0 = (up ? tm - tiles_h : tm) * S::BM, n0 = tn * S::BN;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   ColumnOperand<S::BM, S::NW> a;
   ColumnOperand<S::BN, S::NW> b;
   a.init((const T*)(up ? p.du : p.dg) + m0, nullptr, p.hidden - m0, (int64_t)p.hidden * 2, p.rows, 0x7fffffff, wave, lane);
   b.init((const T*)p.x + n0, nullptr, p.dim - n0, p.ldx * 2, p.rows, 0x7fffffff, wave, lane);
+  tile_products<S, T, COLUMNS, COLUMNS>(a, b, (int)((p.rows + 63) / 64), smem, wave, lane, acc);
+  store_tile<T, S>(acc, (T*)(up ? p.dup_w : p.dgate_w), p.dim, m0 + wave / S::WNW * S::WR, p.hidden, n0 + wave % S::WNW * S::WC, p.dim, lane);
+}
+
+// The products of the gradient in one launch: first dx's tiles, whose k is the
+// longer where rows are few, then those of the weights' gradients, then the
+// biases' (the chunks' column sums, in order), so that what each leaves idle
+// the next one takes.
+template <typename T, typename S>
+__global__ __launch_bounds__(S::NW * 64, 1) void k_gated_products(BwdParams p, int dx_tiles, int dw_tiles) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[S::LDS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wg = (int)blockIdx.x;
+  if (wg >= dx_tiles + dw_tiles) {
+    const int c = (wg - dx_tiles - dw_tiles) * S::NW * 64 + (int)threadIdx.x;
+    if (c >= 2 * p.hidden) return;
+    float v = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < p.chunks; ++i) v += p.partial[(int64_t)i * 2 * p.hidden + c];
+    (c < p.hidden ? p.dgate_b + c : p.dup_b + (c - p.hidden))[0] = __builtin_bit_cast(uint16_t, (bf16)v);
+    return;
+  }
   f32x4 acc[S::MI][S::NJ];
 #pragma unroll
   for (int i = 0; i < S::MI; ++i)
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  tile_products<S, T, COLUMNS, COLUMNS>(a, b, (int)((p.rows + 63) / 64), smem, wave, lane, acc);
-  T* out = (T*)(up ? p.dup_w : p.dgate_w);
-  const int l16 = lane & 15, l4 = lane >> 4;
-#pragma unroll
-  for (int i = 0; i < S::MI; ++i) {
-    const int m = m0 + wave / S::WNW * S::WR + 16 * i + l16;
-    const bool valid = m < p.hidden;
-    float v[S::NJ][4];
-#pragma unroll
-    for (int j = 0; j < S::NJ; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[j][e] = acc[i][j][e];
-    store_row<T, S::NJ>(out + (int64_t)(valid ? m : 0) * p.dim, n0 + wave % S::WNW * S::WC, p.dim, v, l4, valid);
-  }
+  if (wg < dx_tiles) dx_tile<T, S>(p, wg, smem, wave, lane, acc);
+  else dw_tile<T, S>(p, wg - dx_tiles, smem, wave, lane, acc);
 }
 
 template <typename T, typename S>
-hipError_t run_dx(const BwdParams& p, hipStream_t s) {
-  const int64_t tiles = (p.rows + S::BM - 1) / S::BM * ((p.dim + S::BN - 1) / S::BN);
-  hipLaunchKernelGGL((k_gated_dx<T, S>), dim3((unsigned)tiles), dim3(S::NW * 64), 0, s, p);
-  return hipGetLastError();
-}
-
-template <typename T, typename S>
-hipError_t run_dw(const BwdParams& p, hipStream_t s) {
-  const int64_t tiles = 2 * ((p.hidden + S::BM - 1) / S::BM) * ((p.dim + S::BN - 1) / S::BN);
-  hipLaunchKernelGGL((k_gated_dw<T, S>), dim3((unsigned)tiles), dim3(S::NW * 64), 0, s, p);
+hipError_t run_products(const BwdParams& p, bool dx, bool dw, bool db, hipStream_t s) {
+  const int dx_tiles = dx ? tiles_of<S>(p.rows, p.dim) : 0, dw_tiles = dw ? 2 * tiles_of<S>(p.hidden, p.dim) : 0;
+  const int db_wgs = db ? (2 * p.hidden + S::NW * 64 - 1) / (S::NW * 64) : 0;
+  if (!(dx_tiles + dw_tiles + db_wgs)) return hipSuccess;
+  hipLaunchKernelGGL((k_gated_products<T, S>), dim3((unsigned)(dx_tiles + dw_tiles + db_wgs)), dim3(S::NW * 64), 0, s, p, dx_tiles, dw_tiles);
   return hipGetLastError();
 }
 
@@ -388,21 +385,17 @@ hipError_t bwd_t(const xema_gated_ffn_bwd_args& a, hipStream_t s) {
                        a.rows, a.hidden, a.act, chunk, dg, du, partial);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (a.dgate_b) {
-    hipLaunchKernelGGL(k_gated_bias, dim3((2 * a.hidden + 255) / 256), dim3(256), 0, s, partial, a.rows > 0 ? chunks : 0, a.hidden,
-                       (uint16_t*)a.dgate_b, (uint16_t*)a.dup_b);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  const BwdParams p{dg, du, a.gate_w, a.up_w, a.x, a.dx, a.dgate_w, a.dup_w, a.rows, a.ldx, a.ld_dx, a.dim, a.hidden};
-  if (a.dx && a.rows > 0) {
-    e = with_tile(pick_tile(a.rows, a.dim, 2 * ((a.hidden + 63) / 64)), [&](auto shape) { return run_dx<T, decltype(shape)>(p, s); });
+  const BwdParams p{dg, du, a.gate_w, a.up_w, a.x, a.dx, a.dgate_w, a.dup_w, partial, (uint16_t*)a.dgate_b, (uint16_t*)a.dup_b,
+                    a.rows, a.ldx, a.ld_dx, a.dim, a.hidden, a.rows > 0 ? chunks : 0};
+  // one launch where both products take the same tile
+  const bool dx = a.dx && a.rows > 0, dw = a.dgate_w, db = a.dgate_b;
+  const FfnTile tx = pick_tile(a.rows, a.dim, 2 * ((a.hidden + 63) / 64)), tw = pick_tile(2 * (int64_t)a.hidden, a.dim, (a.rows + 63) / 64);
+  if (dx && dw && tx != tw) {
+    e = with_tile(tx, [&](auto shape) { return run_products<T, decltype(shape)>(p, true, false, false, s); });
     if (e != hipSuccess) return e;
+    return with_tile(tw, [&](auto shape) { return run_products<T, decltype(shape)>(p, false, true, db, s); });
   }
-  if (a.dgate_w) {
-    // (the two gradients' tiles are apart where hidden is no multiple of a tile's)
-    return with_tile(pick_tile(2 * (int64_t)a.hidden, a.dim, (a.rows + 63) / 64), [&](auto shape) { return run_dw<T, decltype(shape)>(p, s); });
-  }
-  return e;
+  return with_tile(dx ? tx : tw, [&](auto shape) { return run_products<T, decltype(shape)>(p, dx, dw, db, s); });
 }
 
 }  // namespace
@@ -414,7 +407,7 @@ hipError_t launch_gated_ffn(const xema_gated_ffn_args& a, hipStream_t s) {
   return a.dtype == XEMA_BF16 ? gated_t<bf16, bf16>(p, s) : gated_t<f16, f16>(p, s);
 }
 
-int64_t gated_bwd_row_chunks(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(64, (rows + 63) / 64)); }
+int64_t gated_bwd_row_chunks(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(64, (rows + 7) / 8)); }
 
 hipError_t launch_gated_ffn_bwd(const xema_gated_ffn_bwd_args& a, hipStream_t s) {
   return a.dtype == XEMA_BF16 ? bwd_t<bf16>(a, s) : bwd_t<f16>(a, s);

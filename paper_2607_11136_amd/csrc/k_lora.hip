@@ -72,7 +72,7 @@ __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p)
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int q = 0; q < RT; ++q) acc[i][q] = f32x4{0.f, 0.f, 0.f, 0.f};
-    constexpr int UNROLL = RT + MT <= 4 ? 2 : 1;
+    constexpr int UNROLL = RT + MT <= 5 ? 2 : 1;
     for (int k0 = begin; k0 < end; k0 += 64 * UNROLL) {
       frag fx[UNROLL][2][MT], fa[UNROLL][2][RT];
 #pragma unroll
@@ -169,13 +169,14 @@ __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce_rows(LoraPara
   store_reduced<T>((T*)p.t + r * 2 * p.rank, p.rank, (int)threadIdx.x * 8, s);
 }
 
-// The adapters of a wave's rows by blocks of 16: a block is pure where all its
-// rows that get a value have the same adapter.
+// The adapters of a wave's rows: the first PASSES different ones, each met by
+// all rows on MFMA, and the rows that have yet another.
+constexpr int PASSES = 3;
 template <int MI>
 struct WaveAdapters {
-  int id[MI];          // of this lane's row of each block
-  int block[MI];       // a pure block's adapter, -1 for a block without one, -2 for a mixed block (scalars)
-  int first, second;   // the first two pure blocks' adapters, -1 for none
+  int id[MI];          // of this lane's row of each block of 16
+  int one[PASSES];     // -1 for none (scalars)
+  int others;          // blocks with a row of a further adapter, a bit each (scalar)
   __device__ __forceinline__ void init(const LoraParams& p, int64_t m0, int lane) {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
@@ -183,56 +184,68 @@ struct WaveAdapters {
       id[i] = m < p.rows ? p.ids[m] : -2;
     }
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const uint64_t with = __ballot(has_adapter(p, id[i])), without = __ballot(id[i] == -1);
-      const int one = with ? __builtin_amdgcn_readlane(id[i], __builtin_ctzll(with)) : -1;
-      block[i] = !with ? -1 : without || __ballot(id[i] == one) != with ? -2 : one;
-    }
-    // (a third adapter within the wave's rows: its blocks count as mixed)
-    first = second = -1;
+    for (int n = 0; n < PASSES; ++n) {
+      one[n] = -1;
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      if (block[i] < 0 || block[i] == first) continue;
-      if (first < 0) first = block[i];
-      else if (second < 0) second = block[i];
-      else if (block[i] != second) block[i] = -2;
+      for (int i = 0; i < MI; ++i) {
+        const uint64_t left = __ballot(further(p, id[i], n));
+        if (left && one[n] < 0) one[n] = __builtin_amdgcn_readlane(id[i], __builtin_ctzll(left));
+      }
     }
+    others = 0;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) others |= __ballot(further(p, id[i], PASSES)) ? 1 << i : 0;
+  }
+  // a row's adapter, if it is none of the first n
+  __device__ __forceinline__ bool further(const LoraParams& p, int i, int n) const {
+    bool f = has_adapter(p, i);
+#pragma unroll
+    for (int k = 0; k < PASSES; ++k)
+      if (k < n) f = f && i != one[k];
+    return f;
   }
 };
 
-// acc += t[r] b[i]^T for the pure blocks with adapter `one` (-1: none): the
-// values' MFMA k-range and the remainders', over the same b.
+// acc += t[r] b[i]^T for the rows with adapter `one` (-1: none): the values'
+// MFMA k-range and the remainders', over the same b.  The products are formed
+// for all rows, and kept for those (a product with zeros in the place of
+// another row's t would not do: the adapter may hold infinities).
 template <typename T, typename S>
-__device__ __forceinline__ void add_to_pure(const LoraParams& p, int64_t m0, int n0, int lane, const WaveAdapters<S::MI>& who, int one,
+__device__ __forceinline__ void add_adapter(const LoraParams& p, int64_t m0, int n0, int lane, const WaveAdapters<S::MI>& who, int one,
                                             f32x4 (&acc)[S::MI][S::NJ]) {
   typedef typename Frag<T>::type frag;
   const int l16 = lane & 15, l4 = lane >> 4;
   const int slots = one >= 0 ? p.rank / 4 : 0, rs = p.rank / 8;    // 16-byte slots of a row of t and of a row of b
   const T* b = (const T*)p.b + (int64_t)one * p.out_dim * p.rank;
+  // k-steps loaded at once, as the registers beside acc allow (the latency is paid once for both)
+  constexpr int AHEAD = S::MI == 8 ? 1 : 2;
 #pragma unroll 1
-  for (int k = 0; k < slots; k += 4) {
-    const int at = k + l4;
-    const bool in = at < slots;
-    frag fb[S::NJ], ft[S::MI];
+  for (int k = 0; k < slots; k += 4 * AHEAD) {
+    frag fb[AHEAD][S::NJ], ft[AHEAD][S::MI];
 #pragma unroll
-    for (int j = 0; j < S::NJ; ++j) {
-      fb[j] = frag{};
-      if (in) fb[j] = *reinterpret_cast<const frag*>(b + min(n0 + 16 * j + l16, p.out_dim - 1) * p.rank + (at < rs ? at : at - rs) * 8);
-    }
-#pragma unroll
-    for (int i = 0; i < S::MI; ++i) {
-      const int64_t m = m0 + 16 * i + l16;
-      ft[i] = frag{};
-      if (in) ft[i] = *reinterpret_cast<const frag*>((const T*)p.t + (m < p.rows ? m : p.rows - 1) * 2 * p.rank + at * 8);
-    }
-    // (formed for every block and kept for those of this adapter: branches
-    // around the MFMAs would double the accumulators' registers)
-#pragma unroll
-    for (int i = 0; i < S::MI; ++i) {
-      const bool keep = who.block[i] == one;
+    for (int u = 0; u < AHEAD; ++u) {
+      const int at = k + 4 * u + l4;
+      const bool in = at < slots;
 #pragma unroll
       for (int j = 0; j < S::NJ; ++j) {
-        const f32x4 v = Frag<T>::run(fb[j], ft[i], acc[i][j]);
+        fb[u][j] = frag{};
+        if (in) fb[u][j] = *reinterpret_cast<const frag*>(b + min(n0 + 16 * j + l16, p.out_dim - 1) * p.rank + (at < rs ? at : at - rs) * 8);
+      }
+#pragma unroll
+      for (int i = 0; i < S::MI; ++i) {
+        const int64_t m = m0 + 16 * i + l16;
+        ft[u][i] = frag{};
+        if (in) ft[u][i] = *reinterpret_cast<const frag*>((const T*)p.t + (m < p.rows ? m : p.rows - 1) * 2 * p.rank + at * 8);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < S::MI; ++i) {
+      const bool keep = who.id[i] == one;
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) {
+        f32x4 v = acc[i][j];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) v = Frag<T>::run(fb[u][j], ft[u][i], v);
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[i][j][e] = keep ? v[e] : acc[i][j][e];
       }
@@ -244,7 +257,7 @@ __device__ __forceinline__ void add_to_pure(const LoraParams& p, int64_t m0, int
 template <typename T, int C>
 __device__ __forceinline__ void add_row(const LoraParams& p, const T* t, const T* const (&b)[C], float (&sum)[C]) {
   typedef T t8 __attribute__((ext_vector_type(8)));
-#pragma unroll(C <= 2 ? 4 : 1)
+#pragma unroll(C <= 2 ? 4 : 2)
   for (int q = 0; q < p.rank; q += 8) {
     const t8 hi = *reinterpret_cast<const t8*>(t + q), lo = *reinterpret_cast<const t8*>(t + p.rank + q);
     t8 v[C];
@@ -257,19 +270,18 @@ __device__ __forceinline__ void add_row(const LoraParams& p, const T* t, const T
   }
 }
 
-// acc += t[r] b[i]^T for the mixed blocks: every lane its own row's products,
-// so that no row meets another's adapter (which may hold infinities: a product
-// with a zero in its place would not do).
+// acc += t[r] b[i]^T for the rows with further adapters: every lane its own
+// row's products.
 template <typename T, typename S>
-__device__ __forceinline__ void add_to_mixed(const LoraParams& p, int64_t m0, int n0, int lane, const WaveAdapters<S::MI>& who,
+__device__ __forceinline__ void add_to_others(const LoraParams& p, int64_t m0, int n0, int lane, const WaveAdapters<S::MI>& who,
                                              f32x4 (&acc)[S::MI][S::NJ]) {
   constexpr int C = 8;      // columns at once: as many loads in flight as the registers beside acc allow
   static_assert(S::NJ % 2 == 0, "pairs of blocks");
   const int l16 = lane & 15, l4 = lane >> 4;
 #pragma unroll
   for (int i = 0; i < S::MI; ++i) {
-    if (who.block[i] != -2) continue;
-    if (!has_adapter(p, who.id[i])) continue;
+    if (!(who.others >> i & 1)) continue;
+    if (!who.further(p, who.id[i], PASSES)) continue;
     const T* bw = (const T*)p.b + (int64_t)who.id[i] * p.out_dim * p.rank;
 #pragma unroll
     for (int j = 0; j < S::NJ; j += 2) {
@@ -314,10 +326,10 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_lora_project(LoraParams p) {
     for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   tile_products<S, T, ROWS, ROWS>(a, b, (kbytes + KB - 1) / KB, smem, wave, lane, acc,
                                   [&] {
-                                    add_to_pure<T, S>(p, mw, nw, lane, who, who.first, acc);
-                                    add_to_pure<T, S>(p, mw, nw, lane, who, who.second, acc);
+#pragma unroll
+                                    for (int n = 0; n < PASSES; ++n) add_adapter<T, S>(p, mw, nw, lane, who, who.one[n], acc);
                                   });
-  add_to_mixed<T, S>(p, mw, nw, lane, who, acc);
+  add_to_others<T, S>(p, mw, nw, lane, who, acc);
 
   float bv[S::NJ][4];
 #pragma unroll
