@@ -65,6 +65,14 @@ __device__ __forceinline__ float load24(const uint32_t* upper, uint32_t low, int
   return __uint_as_float(hi | (low >> (8 * e) & 0xffu) << 8);
 }
 
+// Four floats from a 4-byte aligned address.
+__device__ __forceinline__ void load4_at4(const float* p, float v[4]) {
+  typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));
+  const f4 u = *reinterpret_cast<const f4*>(p);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = u[e];
+}
+
 struct GatedParams {
   const void* x; const float* x_scale;
   const void *gate_w, *up_w; const float *gate_scale, *up_scale;
@@ -102,19 +110,17 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_gated(GatedParams p) {
 
   const int l16 = lane & 15, l4 = lane >> 4;
   const int col0 = n0 + wave % S::WNW * (S::WC / 2);
-  float sg[NB][4], su[NB][4], bg[NB][4], bu[NB][4];
+  float sg[NB][4], su[NB][4], bg[NB][4] = {}, bu[NB][4] = {};
 #pragma unroll
-  for (int j = 0; j < NB; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int col = min(col0 + 16 * j + 4 * l4 + e, p.hidden - 1);
-      if (sizeof(T) == 1) {
-        sg[j][e] = p.gate_scale[col];
-        su[j][e] = p.up_scale[col];
-      }
-      bg[j][e] = p.gate_b ? bf16_bits_to_f32(p.gate_b[col]) : 0.f;
-      bu[j][e] = p.up_b ? bf16_bits_to_f32(p.up_b[col]) : 0.f;
+  for (int j = 0; j < NB; ++j) {
+    const int col = min(col0 + 16 * j + 4 * l4, p.hidden - 4);      // (units past the last are not stored)
+    if (sizeof(T) == 1) {
+      load4_at4(p.gate_scale + col, sg[j]);
+      load4_at4(p.up_scale + col, su[j]);
     }
+    if (p.gate_b) load4f<uint16_t>(p.gate_b + col, bg[j]);
+    if (p.up_b) load4f<uint16_t>(p.up_b + col, bu[j]);
+  }
 #pragma unroll
   for (int i = 0; i < S::MI; ++i) {
     const int64_t m = m0 + wave / S::WNW * S::WR + 16 * i + l16;

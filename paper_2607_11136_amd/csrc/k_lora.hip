@@ -331,11 +331,11 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_lora_project(LoraParams p) {
                                   });
   add_to_others<T, S>(p, mw, nw, lane, who, acc);
 
-  float bv[S::NJ][4];
+  float bv[S::NJ][4] = {};
+  if (p.bias) {
 #pragma unroll
-  for (int j = 0; j < S::NJ; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) bv[j][e] = p.bias ? bf16_bits_to_f32(p.bias[min(nw + 16 * j + 4 * l4 + e, p.out_dim - 1)]) : 0.f;
+    for (int j = 0; j < S::NJ; ++j) load4f<uint16_t>(p.bias + min(nw + 16 * j + 4 * l4, p.out_dim - 4), bv[j]);
+  }
 #pragma unroll
   for (int i = 0; i < S::MI; ++i) {
     const bool valid = who.id[i] >= -1;
