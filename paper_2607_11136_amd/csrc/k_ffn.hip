@@ -282,10 +282,11 @@ struct BwdParams {
   const void *gate_w, *up_w;    // [hidden, dim]
   const void* x;
   void *dx, *dgate_w, *dup_w;
+  float* dx_parts;              // [parts][rows][dim] where dx's k is split
   const float* partial;         // [chunks][2 hidden]
   uint16_t *dgate_b, *dup_b;
   int64_t rows, ldx, ld_dx;
-  int dim, hidden, chunks;
+  int dim, hidden, chunks, parts;
 };
 
 // The tile's accumulators as rows row0 + ... of a [rows, cols] matrix.
@@ -306,23 +307,61 @@ __device__ __forceinline__ void store_tile(const f32x4 (&acc)[S::MI][S::NJ], T* 
   }
 }
 
+// The same in fp32.
+template <typename S>
+__device__ __forceinline__ void store_sums(const f32x4 (&acc)[S::MI][S::NJ], float* out, int64_t ld, int64_t row0, int64_t rows, int col0, int cols,
+                                           int lane) {
+  const int l16 = lane & 15, l4 = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < S::MI; ++i) {
+    const int64_t m = row0 + 16 * i + l16;
+#pragma unroll
+    for (int j = 0; j < S::NJ; ++j) {
+      const int c = col0 + 16 * j + 4 * l4;
+      if (m < rows && c < cols) *reinterpret_cast<f32x4*>(out + m * ld + c) = acc[i][j];
+    }
+  }
+}
+
+// dx from its parts, in order.
+template <typename T>
+__global__ __launch_bounds__(256) void k_gated_dx_sum(BwdParams p) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, n = p.rows * p.dim;
+  if (at >= n) return;
+  f32x4 s = *reinterpret_cast<const f32x4*>(p.dx_parts + at);
+#pragma unroll 4
+  for (int i = 1; i < p.parts; ++i) s += *reinterpret_cast<const f32x4*>(p.dx_parts + i * n + at);
+  t4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = (T)s[e];
+  const int64_t r = at / p.dim;
+  *reinterpret_cast<t4*>((T*)p.dx + r * p.ld_dx + (at - r * p.dim)) = o;
+}
+
 template <typename S>
 __host__ __device__ constexpr int tiles_of(int64_t rows, int cols) {
   return (int)((rows + S::BM - 1) / S::BM) * ((cols + S::BN - 1) / S::BN);
 }
 
-// dx = dg Wg + du Wu: the weights are read k by k (a row of W is one k).
+// dx = dg Wg + du Wu: the weights are read k by k (a row of W is one k).  With
+// parts, workgroup wg has part wg / tiles of the steps, its sums kept in fp32.
 template <typename T, typename S>
 __device__ __forceinline__ void dx_tile(const BwdParams& p, int wg, uint8_t* smem, int wave, int lane, f32x4 (&acc)[S::MI][S::NJ]) {
+  const int tiles = tiles_of<S>(p.rows, p.dim), part = __builtin_amdgcn_readfirstlane(wg / tiles);
   int tm, tn;
-  tile_of(wg, (int)((p.rows + S::BM - 1) / S::BM), (p.dim + S::BN - 1) / S::BN, 1024 / S::BM, &tm, &tn);
+  tile_of(wg - part * tiles, (int)((p.rows + S::BM - 1) / S::BM), (p.dim + S::BN - 1) / S::BN, 1024 / S::BM, &tm, &tn);
   const int64_t m0 = (int64_t)tm * S::BM;
-  const int n0 = tn * S::BN, steps = (p.hidden + 63) / 64;
+  const int n0 = tn * S::BN, steps = (p.hidden + 63) / 64, each = (2 * steps + p.parts - 1) / p.parts, first = part * each;
   RowOperand<S::BM, S::NW> a;
   ColumnOperand<S::BN, S::NW> b;
-  a.init((const T*)p.dg + m0 * p.hidden, (const T*)p.du + m0 * p.hidden, p.rows - m0, (int64_t)p.hidden * 2, p.hidden * 2, steps, wave, lane);
-  b.init((const T*)p.gate_w + n0, (const T*)p.up_w + n0, p.dim - n0, (int64_t)p.dim * 2, p.hidden, steps, wave, lane);
-  tile_products<S, T, ROWS, COLUMNS>(a, b, 2 * steps, smem, wave, lane, acc);
+  a.init((const T*)p.dg + m0 * p.hidden, (const T*)p.du + m0 * p.hidden, p.rows - m0, (int64_t)p.hidden * 2, p.hidden * 2, steps, wave, lane, first);
+  b.init((const T*)p.gate_w + n0, (const T*)p.up_w + n0, p.dim - n0, (int64_t)p.dim * 2, p.hidden, steps, wave, lane, first);
+  tile_products<S, T, ROWS, COLUMNS>(a, b, min(each, 2 * steps - first), smem, wave, lane, acc);
+  if (p.parts > 1) {
+    store_sums<S>(acc, p.dx_parts + part * p.rows * p.dim, p.dim, m0 + wave / S::WNW * S::WR, p.rows, n0 + wave % S::WNW * S::WC, p.dim, lane);
+    return;
+  }
   store_tile<T, S>(acc, (T*)p.dx, p.ld_dx, m0 + wave / S::WNW * S::WR, p.rows, n0 + wave % S::WNW * S::WC, p.dim, lane);
 }
 
@@ -370,7 +409,7 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_gated_products(BwdParams p, i
 
 template <typename T, typename S>
 hipError_t run_products(const BwdParams& p, bool dx, bool dw, bool db, hipStream_t s) {
-  const int dx_tiles = dx ? tiles_of<S>(p.rows, p.dim) : 0, dw_tiles = dw ? 2 * tiles_of<S>(p.hidden, p.dim) : 0;
+  const int dx_tiles = dx ? tiles_of<S>(p.rows, p.dim) * p.parts : 0, dw_tiles = dw ? 2 * tiles_of<S>(p.hidden, p.dim) : 0;
   const int db_wgs = db ? (2 * p.hidden + S::NW * 64 - 1) / (S::NW * 64) : 0;
   if (!(dx_tiles + dw_tiles + db_wgs)) return hipSuccess;
   hipLaunchKernelGGL((k_gated_products<T, S>), dim3((unsigned)(dx_tiles + dw_tiles + db_wgs)), dim3(S::NW * 64), 0, s, p, dx_tiles, dw_tiles);
@@ -391,17 +430,22 @@ hipError_t bwd_t(const xema_gated_ffn_bwd_args& a, hipStream_t s) {
                        a.rows, a.hidden, a.act, chunk, dg, du, partial);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  const BwdParams p{dg, du, a.gate_w, a.up_w, a.x, a.dx, a.dgate_w, a.dup_w, partial, (uint16_t*)a.dgate_b, (uint16_t*)a.dup_b,
-                    a.rows, a.ldx, a.ld_dx, a.dim, a.hidden, a.rows > 0 ? chunks : 0};
-  // one launch where both products take the same tile
   const bool dx = a.dx && a.rows > 0, dw = a.dgate_w, db = a.dgate_b;
-  const FfnTile tx = pick_tile(a.rows, a.dim, 2 * ((a.hidden + 63) / 64)), tw = pick_tile(2 * (int64_t)a.hidden, a.dim, (a.rows + 63) / 64);
-  if (dx && dw && tx != tw) {
-    e = with_tile(tx, [&](auto shape) { return run_products<T, decltype(shape)>(p, true, false, false, s); });
-    if (e != hipSuccess) return e;
-    return with_tile(tw, [&](auto shape) { return run_products<T, decltype(shape)>(p, false, true, db, s); });
+  const FfnSplit sx = pick_split(a.rows, a.dim, 2 * ((a.hidden + 63) / 64));
+  const FfnTile tw = pick_tile(2 * (int64_t)a.hidden, a.dim, (a.rows + 63) / 64);
+  float* dx_parts = (float*)(ws + 2 * part + gated_bwd_row_chunks(a.rows) * 2 * a.hidden * 4);
+  const BwdParams p{dg, du, a.gate_w, a.up_w, a.x, a.dx, a.dgate_w, a.dup_w, dx_parts, partial, (uint16_t*)a.dgate_b, (uint16_t*)a.dup_b,
+                    a.rows, a.ldx, a.ld_dx, a.dim, a.hidden, a.rows > 0 ? chunks : 0, sx.parts};
+  // one launch where both products take the same tile
+  if (dx && dw && sx.tile != tw) {
+    e = with_tile(sx.tile, [&](auto shape) { return run_products<T, decltype(shape)>(p, true, false, false, s); });
+    if (e == hipSuccess) e = with_tile(tw, [&](auto shape) { return run_products<T, decltype(shape)>(p, false, true, db, s); });
+  } else {
+    e = with_tile(dx ? sx.tile : tw, [&](auto shape) { return run_products<T, decltype(shape)>(p, dx, dw, db, s); });
   }
-  return with_tile(dx ? tx : tw, [&](auto shape) { return run_products<T, decltype(shape)>(p, dx, dw, db, s); });
+  if (e != hipSuccess || !dx || sx.parts == 1) return e;
+  hipLaunchKernelGGL((k_gated_dx_sum<T>), dim3((unsigned)((a.rows * a.dim / 4 + 255) / 256)), dim3(256), 0, s, p);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -414,6 +458,11 @@ hipError_t launch_gated_ffn(const xema_gated_ffn_args& a, hipStream_t s) {
 }
 
 int64_t gated_bwd_row_chunks(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(64, (rows + 7) / 8)); }
+
+int64_t gated_bwd_dx_parts(int64_t rows, int dim, int hidden) {
+  const int parts = rows > 0 ? pick_split(rows, dim, 2 * ((hidden + 63) / 64)).parts : 1;
+  return parts > 1 ? parts * rows * dim : 0;
+}
 
 hipError_t launch_gated_ffn_bwd(const xema_gated_ffn_bwd_args& a, hipStream_t s) {
   return a.dtype == XEMA_BF16 ? bwd_t<bf16>(a, s) : bwd_t<f16>(a, s);

@@ -257,7 +257,8 @@ __device__ __forceinline__ void add_adapter(const LoraParams& p, int64_t m0, int
 template <typename T, int C>
 __device__ __forceinline__ void add_row(const LoraParams& p, const T* t, const T* const (&b)[C], float (&sum)[C]) {
   typedef T t8 __attribute__((ext_vector_type(8)));
-#pragma unroll(C <= 2 ? 4 : 2)
+  constexpr int UNROLL = C <= 2 ? 4 : 2;
+#pragma unroll UNROLL
   for (int q = 0; q < p.rank; q += 8) {
     const t8 hi = *reinterpret_cast<const t8*>(t + q), lo = *reinterpret_cast<const t8*>(t + p.rank + q);
     t8 v[C];

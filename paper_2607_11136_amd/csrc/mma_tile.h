@@ -104,17 +104,19 @@ struct RowOperand {
   RowLoads<N, NW> l;
   const uint8_t *p0, *p1;
   int64_t bytes;
-  int kbytes, steps0;
-  // rows from `part0` (and, from step `steps0` on, `part1`), `valid` of them
+  int kbytes, steps0, first;
+  // rows from `part0` (and, from step `steps0` on, `part1`), `valid` of them;
+  // the main loop's step 0 is step `first_`
   __device__ __forceinline__ void init(const void* part0, const void* part1, int64_t valid, int64_t ld_bytes, int kbytes_,
-                                       int steps0_, int wave, int lane) {
+                                       int steps0_, int wave, int lane, int first_ = 0) {
     const int v = valid < N ? (int)valid : N;
     l.init(v, (uint32_t)ld_bytes, kbytes_, wave, lane);
     p0 = (const uint8_t*)part0; p1 = (const uint8_t*)part1;
     bytes = v * ld_bytes;
-    kbytes = kbytes_; steps0 = steps0_;
+    kbytes = kbytes_; steps0 = steps0_; first = first_;
   }
-  __device__ __forceinline__ void issue(int kt, int c, uint8_t* st, int wave) const {
+  __device__ __forceinline__ void issue(int step, int c, uint8_t* st, int wave) const {
+    const int kt = step + first;
     const bool second = kt >= steps0;
     l.issue(make_rsrc(second ? p1 : p0, bytes), c, second ? kt - steps0 : kt, kbytes, st, wave);
   }
@@ -125,16 +127,17 @@ struct ColumnOperand {
   static constexpr int LOADS = ColumnLoads<N, NW>::LOADS;
   ColumnLoads<N, NW> l;
   const uint8_t *p0, *p1;
-  int k, steps0;
+  int k, steps0, first;
   uint32_t ld;
   __device__ __forceinline__ void init(const void* part0, const void* part1, int64_t valid, int64_t ld_bytes, int64_t k_,
-                                       int steps0_, int wave, int lane) {
+                                       int steps0_, int wave, int lane, int first_ = 0) {
     ld = (uint32_t)ld_bytes;
     l.init(valid < N ? (int)valid : N, ld, wave, lane);
     p0 = (const uint8_t*)part0; p1 = (const uint8_t*)part1;
-    k = (int)k_; steps0 = steps0_;
+    k = (int)k_; steps0 = steps0_; first = first_;
   }
-  __device__ __forceinline__ void issue(int kt, int c, uint8_t* st, int wave) const {
+  __device__ __forceinline__ void issue(int step, int c, uint8_t* st, int wave) const {
+    const int kt = step + first;
     const bool second = kt >= steps0;
     const int k0 = (second ? kt - steps0 : kt) * 64;
     l.issue((second ? p1 : p0) + (int64_t)k0 * ld, ld, k - k0, c, st, wave);

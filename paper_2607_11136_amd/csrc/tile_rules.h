@@ -124,8 +124,8 @@ constexpr FfnCost kFfnCost[FFN_TILES] = {{256, 256, 1.03, 1.41, 6.6, false}, {12
                                          {128, 128, 0.52, 0.97, 4.2, true},  {64, 128, 0.35, 0.56, 3.2, true},
                                          {64, 64, 0.265, 0.41, 2.7, true}};
 
-inline double ffn_tile_us(const FfnCost& c, int64_t m, int64_t n, int64_t steps) {
-  const int64_t tiles = (m + c.rows - 1) / c.rows * ((n + c.cols - 1) / c.cols);
+inline double ffn_tile_us(const FfnCost& c, int64_t m, int64_t n, int64_t steps, int64_t times = 1) {
+  const int64_t tiles = (m + c.rows - 1) / c.rows * ((n + c.cols - 1) / c.cols) * times;
   const int64_t slots = c.shares ? 2 * RULE_CUS : RULE_CUS, rounds = tiles / slots, rest = tiles % slots;
   // the last round runs at the few CUs' pace while half of them idle, and pairs
   // are faster by up to 15% while few CUs have one
@@ -150,6 +150,23 @@ inline FfnTile pick_tile(int64_t m, int64_t n, int64_t steps) {
     if (t == 0 || us < least) { best = t; least = us; }
   }
   return (FfnTile)best;
+}
+
+// A product whose k may be split: `parts` sums over consecutive steps, kept in
+// fp32 and added by a launch of their own (3 us, and the sums' bytes at about 4
+// TB/s there and back).  For few rows and long k (dx of a short batch), whose
+// tiles leave most CUs idle.  us whole and split: 333 x 512, 44 steps 16 and 8;
+// 64 x 4096, 344 steps 96 and 40.
+struct FfnSplit { FfnTile tile; int parts; };
+inline FfnSplit pick_split(int64_t m, int64_t n, int64_t steps) {
+  FfnSplit best{pick_tile(m, n, steps), 1};
+  double least = ffn_tile_us(kFfnCost[best.tile], m, n, steps);
+  for (int parts = 2; parts <= 16 && steps / parts >= 8 && m * n * parts <= ((int64_t)1 << 24); parts *= 2)   // (64 MiB of sums)
+    for (int t = 0; t < FFN_TILES; ++t) {
+      const double us = ffn_tile_us(kFfnCost[t], m, n, (steps + parts - 1) / parts, parts) + 3.0 + (double)m * n * 8 * parts / 4e6;
+      if (us < least) { best = {(FfnTile)t, parts}; least = us; }
+    }
+  return best;
 }
 
 // ---------------------------------------------------------------------------

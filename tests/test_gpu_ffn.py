@@ -318,7 +318,7 @@ def test_gated_ffn_extreme_gates(act):
 
 
 BWD_SIZES = [(1, 8, 8), (2, 64, 40), (17, 512, 1368), (63, 128, 64), (65, 136, 200), (130, 328, 520), (257, 1544, 264), (1100, 256, 1032),
-             (2100, 4104, 2056), (5000, 4104, 72)]
+             (2100, 4104, 2056), (5000, 4104, 72), (70, 136, 4104), (5, 1032, 2056)]
 
 
 def run_bwd(x, wg, wu, pre, dy, act, bias=True, dx=True, dw=True, gap=8, stream=None):
