@@ -24,7 +24,7 @@
  * their width, below 2^21, whose bytes are a multiple of 16 (so rows start
  * 16-byte aligned); widths are multiples of 8 (of 16 for XEMA_E4M3 rows) and
  * at most 131072; row counts are any from 0 (nothing is launched) to
- * 2^31 - 1024.  Outputs must not overlap inputs, workspaces or each other,
+ * 2^24 - 1.  Outputs must not overlap inputs, workspaces or each other,
  * except where an entry point allows it.
  *
  * Sums and statistics are fp32 (MFMA accumulators, row sums), each in one

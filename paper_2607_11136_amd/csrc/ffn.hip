@@ -10,7 +10,8 @@ using namespace xema;
 
 namespace {
 
-constexpr int64_t MAX_ROWS = ((int64_t)1 << 31) - 1024, MAX_LD = (int64_t)1 << 21, MAX_WIDTH = 131072;
+// (a launch has fewer than 2^32 threads, and a row up to 256)
+constexpr int64_t MAX_ROWS = ((int64_t)1 << 24) - 1, MAX_LD = (int64_t)1 << 21, MAX_WIDTH = 131072;
 
 bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 

@@ -161,11 +161,14 @@ struct FfnSplit { FfnTile tile; int parts; };
 inline FfnSplit pick_split(int64_t m, int64_t n, int64_t steps) {
   FfnSplit best{pick_tile(m, n, steps), 1};
   double least = ffn_tile_us(kFfnCost[best.tile], m, n, steps);
-  for (int parts = 2; parts <= 16 && steps / parts >= 8 && m * n * parts <= ((int64_t)1 << 24); parts *= 2)   // (64 MiB of sums)
+  for (int64_t want = 2; want <= 16 && steps / want >= 8; want *= 2) {
+    const int64_t each = (steps + want - 1) / want, parts = (steps + each - 1) / each;
+    if (m * n * parts > ((int64_t)1 << 24)) break;      // (64 MiB of sums)
     for (int t = 0; t < FFN_TILES; ++t) {
-      const double us = ffn_tile_us(kFfnCost[t], m, n, (steps + parts - 1) / parts, parts) + 3.0 + (double)m * n * 8 * parts / 4e6;
-      if (us < least) { best = {(FfnTile)t, parts}; least = us; }
+      const double us = ffn_tile_us(kFfnCost[t], m, n, each, parts) + 3.0 + (double)m * n * 8 * parts / 4e6;
+      if (us < least) { best = {(FfnTile)t, (int)parts}; least = us; }
     }
+  }
   return best;
 }
 

@@ -96,7 +96,7 @@ def test_accepted_with_no_rows(case):
 
 
 REFUSED = [
-    (norm(rows=-1), INVALID), (norm(rows=1 << 31), UNSUPPORTED), (norm(x=None), INVALID), (norm(y=None), INVALID), (norm(dim=0), INVALID),
+    (norm(rows=-1), INVALID), (norm(rows=1 << 24), UNSUPPORTED), (gated(rows=1 << 40), UNSUPPORTED), (lora(rows=1 << 24), UNSUPPORTED), (norm(x=None), INVALID), (norm(y=None), INVALID), (norm(dim=0), INVALID),
     (norm(eps=0.0), INVALID), (norm(eps=float("nan")), INVALID), (norm(dim=60), UNSUPPORTED), (norm(ldx=56), INVALID),
     (norm(dim=16392, ldx=16392, ld_resid=16392, ld_sum=16392, ldy=16392), UNSUPPORTED), (norm(x_dtype=3), UNSUPPORTED),
     (norm(resid_dtype=9), UNSUPPORTED), (norm(sum_dtype=3), UNSUPPORTED), (norm(y_dtype=2), UNSUPPORTED),

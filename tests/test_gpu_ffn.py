@@ -208,7 +208,7 @@ def test_rmsnorm_bwd_in_place(which):
 # -- gated feed-forward ------------------------------------------------------------------------------------------
 
 SIZES = [(1, 8, 8), (1, 4096, 1024), (2, 64, 40), (16, 72, 136), (17, 512, 1368), (32, 1096, 72), (33, 1096, 72), (63, 128, 64), (65, 136, 200), (130, 328, 520), (257, 1544, 264),
-         (700, 256, 2056), (1500, 192, 4104)]
+         (700, 256, 2056), (1500, 192, 4104), (582, 72, 3376), (2435, 88, 1552), (207, 64, 4208)]
 
 
 def gated_inputs(rows, dim, hidden, dtype, bias, seed):
@@ -267,13 +267,15 @@ def test_gated_ffn(rows, dim, hidden, dtype, act, bias):
     assert torch.equal(y2, y[:, :hidden])
 
 
+SIZES_8BIT = [(1, 16, 8), (1, 4096, 1024), (3, 144, 40), (16, 2064, 24), (31, 1040, 72), (65, 272, 200), (130, 336, 520), (700, 128, 2056),
+              (1500, 512, 4104), (582, 80, 3376), (2435, 144, 1552), (207, 64, 4208)]
+
 # A 16x16x128 MFMA of e4m3 values aligns its 128 products to the largest before
 # it adds them: off by up to 2^-14 of the sum of their magnitudes (measured 2^-14.8).
 E4M3_SUM = 2.0 ** -14
 
 
-@pytest.mark.parametrize("rows,dim,hidden", [(1, 16, 8), (1, 4096, 1024), (3, 144, 40), (16, 2064, 24), (31, 1040, 72), (65, 272, 200), (130, 336, 520), (700, 128, 2056),
-                                             (1500, 512, 4104)])
+@pytest.mark.parametrize("rows,dim,hidden", SIZES_8BIT)
 @pytest.mark.parametrize("yt,act,bias", [(BF16, 0, False), (F16, 1, True)])
 def test_gated_ffn_8bit(rows, dim, hidden, yt, act, bias):
     x, wg, wu, bg, bu = gated_inputs(rows, dim, hidden, F32, bias, rows + dim)
@@ -318,7 +320,9 @@ def test_gated_ffn_extreme_gates(act):
 
 
 BWD_SIZES = [(1, 8, 8), (2, 64, 40), (17, 512, 1368), (63, 128, 64), (65, 136, 200), (130, 328, 520), (257, 1544, 264), (1100, 256, 1032),
-             (2100, 4104, 2056), (5000, 4104, 72), (70, 136, 4104), (5, 1032, 2056)]
+             (2100, 4104, 2056), (5000, 4104, 72), (70, 136, 4104), (5, 1032, 2056),
+             (39, 280, 5456), (35, 544, 5504), (33, 528, 1816), (2711, 1456, 72), (1614, 1240, 2400),
+             (40, 1800, 2304), (69, 1136, 4120)]
 
 
 def run_bwd(x, wg, wu, pre, dy, act, bias=True, dx=True, dw=True, gap=8, stream=None):
@@ -437,7 +441,9 @@ def spread_ids(rows, n, how, seed):
 LORA_SIZES = [(1, 8, 8, 8, 1), (1, 4096, 1032, 16, 3), (5, 72, 136, 8, 2), (48, 512, 1024, 16, 20), (65, 136, 200, 24, 4), (130, 328, 520, 64, 7),
               (257, 1544, 264, 128, 5), (700, 256, 2056, 32, 40), (1500, 192, 4104, 8, 3), (9000, 256, 1544, 16, 4),
               (12500, 136, 520, 32, 5), (16, 2056, 72, 32, 3), (33, 1032, 88, 128, 2),
-              (7, 264, 4360, 16, 3), (20, 136, 4136, 24, 4), (47, 72, 8192, 8, 2), (64, 520, 4104, 40, 9), (64, 2056, 520, 16, 3), (30, 64, 8200, 8, 2)]
+              (7, 264, 4360, 16, 3), (20, 136, 4136, 24, 4), (47, 72, 8192, 8, 2), (64, 520, 4104, 40, 9), (64, 2056, 520, 16, 3), (30, 64, 8200, 8, 2),
+              (582, 72, 3376, 8, 2), (2100, 72, 136, 16, 6), (1100, 72, 136, 32, 6), (600, 136, 72, 64, 9), (4200, 136, 72, 64, 9),
+              (4200, 264, 72, 128, 3)]
 
 
 @pytest.mark.parametrize("rows,dim,out_dim,rank,n", LORA_SIZES)
