@@ -7,9 +7,9 @@
 //
 // 18432 x 4096 x 4096, rank 32, an adapter for each of four sequences: 50 us reducing
 // (x once from HBM: 29 us) and 485 us (the product alone 460, 1350 TFLOP/s);
-// 3204 x 1544 x 4104, rank 64, seven requests: 15 and 60 us (rows of 3088 bytes
+// 3204 x 1544 x 4104, rank 64, seven requests: 13 and 60 us (rows of 3088 bytes
 // straddle the 128-byte lines; the adapters' loads are bound by their latency,
-// 1.3 us a k-step); 48 single tokens of 4096 x 4096: 6 and 18 us (x from L2 for
+// 1.3 us a k-step); 48 single tokens of 4096 x 4096: 5 and 18 us (x from L2 for
 // every 16 columns).
 #include "device_common.h"
 #include "few_rows.h"
@@ -51,9 +51,12 @@ __device__ __forceinline__ void store_reduced(T* t, int rank, int q, const float
 }
 
 // t[r] = scale[i] x[r] a[i]^T as value and remainder.  A workgroup per block of
-// 16 MT rows multiplies all of them on MFMA with the adapter that they share,
-// its waves a part of k each; where a block has several adapters (requests
-// that meet in it), with one after the other, and a row keeps its own.
+// 16 MT rows and 16 RT ranks multiplies them on MFMA with the adapter that the
+// rows share, its waves a part of k each; where a block has several adapters
+// (requests that meet in it, or single tokens), with one after the other, and a
+// row keeps its own.  While the blocks are fewer than the CUs, what bounds it is
+// how fast one CU gets its part of a and x from L2 (256 KiB in 10 us): the ranks
+// are then dealt to several workgroups (run_reduce).
 template <typename T, int MT, int RT>
 __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p) {
   typedef typename Frag<T>::type frag;
@@ -61,6 +64,7 @@ __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p)
   __shared__ __attribute__((aligned(16))) float red[REDUCE_WAVES][RB][RR + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, l4 = lane >> 4;
   const int64_t m0 = (int64_t)blockIdx.x * RB;
+  const int q0 = (int)blockIdx.y * RR, ranks = min(p.rank - q0, RR);
   const int id = lane < RB && m0 + lane < p.rows ? p.ids[m0 + lane] : -2;
   const T* xr[MT];
 #pragma unroll
@@ -77,7 +81,7 @@ __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p)
     const float scale = p.scale[one];
     const T* ar[RT];
 #pragma unroll
-    for (int q = 0; q < RT; ++q) ar[q] = (const T*)p.a + ((int64_t)one * p.rank + min(16 * q + l16, p.rank - 1)) * p.dim;
+    for (int q = 0; q < RT; ++q) ar[q] = (const T*)p.a + ((int64_t)one * p.rank + min(q0 + 16 * q + l16, p.rank - 1)) * p.dim;
     f32x4 acc[MT][RT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -117,8 +121,8 @@ __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p)
 #pragma unroll
       for (int q = 0; q < RT; ++q) *reinterpret_cast<f32x4*>(&red[wave][16 * i + l16][16 * q + 4 * l4]) = acc[i][q];
     __syncthreads();
-    for (int at = threadIdx.x; at < RB * p.rank / 8; at += REDUCE_WAVES * 64) {
-      const int row = at / (p.rank / 8), q = at % (p.rank / 8) * 8;
+    for (int at = threadIdx.x; at < RB * ranks / 8; at += REDUCE_WAVES * 64) {
+      const int row = at / (ranks / 8), q = at % (ranks / 8) * 8;
       if (!(rows >> row & 1)) continue;
       float s[8];
 #pragma unroll
@@ -128,56 +132,58 @@ __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p)
         for (int w = 0; w < REDUCE_WAVES; ++w) s[e] += red[w][row][q + e];
         s[e] *= scale;
       }
-      store_reduced<T>((T*)p.t + (m0 + row) * 2 * p.rank, p.rank, q, s);
+      store_reduced<T>((T*)p.t + (m0 + row) * 2 * p.rank, p.rank, q0 + q, s);
     }
     if (todo) __syncthreads();
   }
 }
 
-// The same for few rows: a workgroup per row, four ranks a wave at a time;
-// where that leaves waves over, k in parts too.
+// The same for few rows: a workgroup per row and 32 ranks, four ranks a wave;
+// where that leaves waves over, k in parts too.  (All ranks of a row in one
+// workgroup: 64 rows of 4096, rank 128, 50 us with the product; so 40.)
+constexpr int ROW_RANKS = REDUCE_WAVES * 4;
 template <typename T>
 __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce_rows(LoraParams p) {
   typedef T t8 __attribute__((ext_vector_type(8)));
-  __shared__ float sums[REDUCE_WAVES * 16];                      // [parts][rank], at most 8 x 16 or 1 x 128
+  __shared__ float sums[REDUCE_WAVES * 4];                       // [parts][ranks of this workgroup]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t r = blockIdx.x;
   const int own = p.ids[r];
   if (!has_adapter(p, own)) return;
   const float scale = p.scale[own];
-  const int batches = min(p.rank / 4, REDUCE_WAVES), parts = REDUCE_WAVES / batches;
+  const int q0 = (int)blockIdx.y * ROW_RANKS, ranks = min(p.rank - q0, ROW_RANKS);
+  const int batches = ranks / 4, parts = REDUCE_WAVES / batches;
   const int batch = wave % batches, part = wave / batches;       // (part `parts`: waves that no batch needs)
   const T* x = (const T*)p.x + r * p.ldx;
-  const T* a = (const T*)p.a + (int64_t)own * p.rank * p.dim;
-  if (part < parts)
-    for (int q = batch * 4; q < p.rank; q += batches * 4) {
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
+  const T* a = (const T*)p.a + ((int64_t)own * p.rank + q0 + batch * 4) * p.dim;
+  if (part < parts) {
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-      for (int k = part * 512 + lane * 8; k < p.dim; k += parts * 512) {
-        const t8 u = *reinterpret_cast<const t8*>(x + k);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const t8 v = *reinterpret_cast<const t8*>(a + (int64_t)(q + i) * p.dim + k);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) s[i] = fmaf((float)u[e], (float)v[e], s[i]);
-        }
-      }
+    for (int k = part * 512 + lane * 8; k < p.dim; k += parts * 512) {
+      const t8 u = *reinterpret_cast<const t8*>(x + k);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[i] = wave_sum(s[i]);
-        if (lane == 0) sums[part * p.rank + q + i] = s[i];
+        const t8 v = *reinterpret_cast<const t8*>(a + (int64_t)i * p.dim + k);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[i] = fmaf((float)u[e], (float)v[e], s[i]);
       }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s[i] = wave_sum(s[i]);
+      if (lane == 0) sums[part * ranks + batch * 4 + i] = s[i];
+    }
+  }
   __syncthreads();
-  if ((int)threadIdx.x >= p.rank / 8) return;
+  if ((int)threadIdx.x >= ranks / 8) return;
   float s[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     s[e] = 0.f;
-    for (int w = 0; w < parts; ++w) s[e] += sums[w * p.rank + threadIdx.x * 8 + e];
+    for (int w = 0; w < parts; ++w) s[e] += sums[w * ranks + threadIdx.x * 8 + e];
     s[e] *= scale;
   }
-  store_reduced<T>((T*)p.t + r * 2 * p.rank, p.rank, (int)threadIdx.x * 8, s);
+  store_reduced<T>((T*)p.t + r * 2 * p.rank, p.rank, q0 + (int)threadIdx.x * 8, s);
 }
 
 // The adapters of a wave's rows: the first PASSES different ones, each met by
@@ -415,14 +421,25 @@ hipError_t run_project_few(const LoraParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <typename T, int MT, int RT>
+hipError_t run_reduce_rt(const LoraParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((k_lora_reduce<T, MT, RT>), dim3((unsigned)((p.rows + 16 * MT - 1) / (16 * MT)), (p.rank + 16 * RT - 1) / (16 * RT)),
+                     dim3(REDUCE_WAVES * 64), 0, s, p);
+  return hipGetLastError();
+}
+
+// The most ranks a workgroup that still give each CU one: each of them reads all
+// of its rows' x.  1000 rows of 4096, rank 64: 21 us with all ranks in one
+// workgroup, 10 in four; with 50 rows a request 39 and 19; with an adapter drawn
+// for every row 276 and 124.
 template <typename T, int MT>
 hipError_t run_reduce(const LoraParams& p, hipStream_t s) {
-  const dim3 grid((unsigned)((p.rows + 16 * MT - 1) / (16 * MT))), block(REDUCE_WAVES * 64);
-  if (p.rank <= 16) hipLaunchKernelGGL((k_lora_reduce<T, MT, 1>), grid, block, 0, s, p);
-  else if (p.rank <= 32) hipLaunchKernelGGL((k_lora_reduce<T, MT, 2>), grid, block, 0, s, p);
-  else if (p.rank <= 64) hipLaunchKernelGGL((k_lora_reduce<T, MT, 4>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((k_lora_reduce<T, MT, 8>), grid, block, 0, s, p);
-  return hipGetLastError();
+  const int64_t blocks = (p.rows + 16 * MT - 1) / (16 * MT);
+  auto enough = [&](int rt) { return blocks * ((p.rank + 16 * rt - 1) / (16 * rt)) >= RULE_CUS; };
+  if (p.rank > 64 && enough(8)) return run_reduce_rt<T, MT, 8>(p, s);
+  if (p.rank > 32 && enough(4)) return run_reduce_rt<T, MT, 4>(p, s);
+  if (p.rank > 16 && enough(2)) return run_reduce_rt<T, MT, 2>(p, s);
+  return run_reduce_rt<T, MT, 1>(p, s);
 }
 
 // A row by itself reads all of its adapter's a, which pays while the rows are
@@ -430,7 +447,7 @@ hipError_t run_reduce(const LoraParams& p, hipStream_t s) {
 template <typename T>
 hipError_t reduce(const LoraParams& p, hipStream_t s) {
   if (p.rows * p.rank <= 32768) {
-    hipLaunchKernelGGL((k_lora_reduce_rows<T>), dim3((unsigned)p.rows), dim3(REDUCE_WAVES * 64), 0, s, p);
+    hipLaunchKernelGGL((k_lora_reduce_rows<T>), dim3((unsigned)p.rows, (p.rank + ROW_RANKS - 1) / ROW_RANKS), dim3(REDUCE_WAVES * 64), 0, s, p);
     return hipGetLastError();
   }
   return p.rows > 4096 ? run_reduce<T, 2>(p, s) : run_reduce<T, 1>(p, s);
