@@ -44,7 +44,8 @@ __device__ __forceinline__ void store_reduced(T* t, int rank, int q, const float
     // conversion, may round to the other neighbour than the remainder is of)
     const float v = as_rounded_f32(s[e]);
     hi[e] = (T)v;
-    lo[e] = (T)(v - (float)hi[e]);
+    // (an infinity leaves no remainder: taken from itself it would be NaN)
+    lo[e] = __builtin_isinf((float)hi[e]) ? (T)0.f : (T)(v - (float)hi[e]);
   }
   *reinterpret_cast<t8*>(t + q) = hi;
   *reinterpret_cast<t8*>(t + rank + q) = lo;

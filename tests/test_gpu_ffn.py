@@ -484,6 +484,29 @@ def test_lora_adapters_do_not_touch_each_other():
             assert bool(torch.isnan(got[ids == 1][:, 7]).all())
 
 
+@pytest.mark.parametrize("rows,rank", [(1, 8), (40, 16), (300, 64), (5000, 8)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_lora_infinities_follow_the_formula(rows, rank, dtype):
+    """All weights positive: a row with an infinity is infinity in every column,
+    not NaN, and so is one whose x a^T leaves the type's range."""
+    d = lora_inputs(rows, 264, 392, rank, 2, dtype, rows)
+    for n in ("x", "w", "a", "b"):
+        d[n] = d[n].abs() + 2.0 ** -10
+    ids = spread_ids(rows, 2, "mixed", rows)
+    ids[0], ids[2:3] = 1, 0                    # (in both calls: a padding row would stay NaN)
+    good, got = empty(rows, 392, 0, dtype), empty(rows, 392, 0, dtype)
+    run_lora(d, ids, good)
+    d["x"][0, 5] = float("inf")
+    if rows > 2:
+        d["x"][2] = torch.finfo(dtype).max     # (264 of them against a's sum of 8 at least)
+    run_lora(d, ids, got)
+    for r in (0, 2)[:1 + (rows > 2)]:
+        assert bool((got[r] == float("inf")).all())
+        got[r] = good[r]
+    live = ids >= -1
+    assert torch.equal(got[live], good[live])
+
+
 def test_lora_without_adapters_is_the_projection():
     d = lora_inputs(70, 264, 392, 8, 1, F16, 4)
     y = empty(70, 392, 0, F16)
