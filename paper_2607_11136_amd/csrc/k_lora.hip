@@ -275,8 +275,7 @@ __device__ __forceinline__ void add_adapter(const LoraParams& p, int64_t m0, int
 template <typename T, int C>
 __device__ __forceinline__ void add_row(const LoraParams& p, const T* t, const T* const (&b)[C], float (&sum)[C]) {
   typedef T t8 __attribute__((ext_vector_type(8)));
-  constexpr int UNROLL = C <= 2 ? 4 : 2;
-#pragma unroll UNROLL
+#pragma unroll 4
   for (int q = 0; q < p.rank; q += 8) {
     const t8 hi = *reinterpret_cast<const t8*>(t + q), lo = *reinterpret_cast<const t8*>(t + p.rank + q);
     t8 v[C];
@@ -289,31 +288,61 @@ __device__ __forceinline__ void add_row(const LoraParams& p, const T* t, const T
   }
 }
 
-// acc += t[r] b[i]^T for the rows with further adapters: every lane its own
-// row's products.
+// acc += t[r] b[i]^T for the rows with further adapters: a block's adapters in
+// turn, TOGETHER of them at once as the registers beside acc allow, each on MFMA
+// over the block's 16 rows; bound by the latency of b's lines from L2.  A lane
+// per row would read each line of b in eight 16-byte pieces, from L2 again each
+// time.  With the reduction, that and this, us, adapters drawn per row of 24,
+// rank 64: 1000 x 4096 x 4096 268 and 221, 1000 x 2048 x 8192 303 and 219.
 template <typename T, typename S>
 __device__ __forceinline__ void add_to_others(const LoraParams& p, int64_t m0, int n0, int lane, const WaveAdapters<S::MI>& who,
                                              f32x4 (&acc)[S::MI][S::NJ]) {
-  constexpr int C = 8;      // columns at once: as many loads in flight as the registers beside acc allow
-  static_assert(S::NJ % 2 == 0, "pairs of blocks");
+  typedef typename Frag<T>::type frag;
+  constexpr int TOGETHER = S::MI == 8 ? 1 : 2;
   const int l16 = lane & 15, l4 = lane >> 4;
 #pragma unroll
   for (int i = 0; i < S::MI; ++i) {
     if (!(who.others >> i & 1)) continue;
-    if (!who.further(p, who.id[i], PASSES)) continue;
-    const T* bw = (const T*)p.b + (int64_t)who.id[i] * p.out_dim * p.rank;
+    const int64_t m = m0 + 16 * i + l16;
+    const T* t = (const T*)p.t + (m < p.rows ? m : p.rows - 1) * 2 * p.rank;
+    for (uint64_t todo = __ballot(who.further(p, who.id[i], PASSES)); todo;) {
+      int one[TOGETHER];
+      f32x4 v[TOGETHER][S::NJ];
 #pragma unroll
-    for (int j = 0; j < S::NJ; j += 2) {
-      const T* b[C];
-      float sum[C];
+      for (int u = 0; u < TOGETHER; ++u) {
+        one[u] = todo ? __builtin_amdgcn_readlane(who.id[i], __builtin_ctzll(todo)) : one[0];
+        todo &= ~__ballot(who.id[i] == one[u]);
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        b[c] = bw + min(n0 + (j + c / 4) * 16 + 4 * l4 + c % 4, p.out_dim - 1) * p.rank;
-        sum[c] = acc[i][j + c / 4][c % 4];
+        for (int j = 0; j < S::NJ; ++j) v[u][j] = acc[i][j];
       }
-      add_row<T, C>(p, (const T*)p.t + (m0 + 16 * i + l16) * 2 * p.rank, b, sum);
+      for (int k0 = 0; k0 < p.rank; k0 += 32) {
+        const int k = k0 + l4 * 8;
+        frag fb[TOGETHER][S::NJ], hi = {}, lo = {};
 #pragma unroll
-      for (int c = 0; c < C; ++c) acc[i][j + c / 4][c % 4] = sum[c];
+        for (int u = 0; u < TOGETHER; ++u)
+#pragma unroll
+          for (int j = 0; j < S::NJ; ++j) fb[u][j] = frag{};
+        if (k < p.rank) {
+#pragma unroll
+          for (int u = 0; u < TOGETHER; ++u) {
+            const T* b = (const T*)p.b + (int64_t)one[u] * p.out_dim * p.rank + k;
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j) fb[u][j] = *reinterpret_cast<const frag*>(b + min(n0 + 16 * j + l16, p.out_dim - 1) * p.rank);
+          }
+          hi = *reinterpret_cast<const frag*>(t + k);
+          lo = *reinterpret_cast<const frag*>(t + p.rank + k);
+        }
+#pragma unroll
+        for (int u = 0; u < TOGETHER; ++u)
+#pragma unroll
+          for (int j = 0; j < S::NJ; ++j) v[u][j] = Frag<T>::run(fb[u][j], lo, Frag<T>::run(fb[u][j], hi, v[u][j]));
+      }
+#pragma unroll
+      for (int u = 0; u < TOGETHER; ++u)
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = who.id[i] == one[u] ? v[u][j][e] : acc[i][j][e];
     }
   }
 }
