@@ -489,11 +489,14 @@ hipError_t lora_t(const LoraParams& p, hipStream_t s) {
     const hipError_t e = reduce<T>(p, s);
     if (e != hipSuccess) return e;
   }
-  // Few rows: one round of workgroups (one a CU), 16 or 32 columns each.  Past
-  // that, and past 64 rows, every workgroup's reading all of x costs more than
-  // the tiles (us, with the reduction; columns 16, 32, tiles):
-  //   48 x 4096 x 4096   25, 29, 31      48 x 4096 x 6144   41, 30, 31
-  //   16 x 4096 x 11008  35, 35, 31      48 x 4096 x 11008  59, 52, 34
+  // Few rows: one round of workgroups (one a CU), 16, 32 or 64 columns each, 64
+  // also where that takes more rounds.  Past that, and past 64 rows (32 beside 64
+  // columns), every workgroup's reading all of x costs more than the tiles (us,
+  // with the reduction; columns 16, 32, 64, tiles):
+  //   48 x 4096 x 4096   25, 29, -, 32     16 x 4096 x 11008  35, 34, 30, 33
+  //   48 x 4096 x 6144   41, 30, -, 33     1 x 4096 x 16384   35, 34, 34, 38
+  //   48 x 4096 x 11008  59, 52, -, 34     16 x 4096 x 32768  86, 69, 62, 75
+  //   24 x 4096 x 8192   31, 25, -, 32     32 x 4096 x 32768  -, 83, 70, 78
   if (p.rows <= 64 && p.out_dim <= 4096) {
     if (p.rows <= 16) return run_project_few<T, YT, 1, 1, 16, 4>(p, s);
     if (p.rows <= 32) return run_project_few<T, YT, 2, 1, 16, 4>(p, s);
@@ -506,6 +509,8 @@ hipError_t lora_t(const LoraParams& p, hipStream_t s) {
     if (p.rows <= 48) return run_project_few<T, YT, 3, 2, 16, 2>(p, s);
     return run_project_few<T, YT, 4, 2, 16, 1>(p, s);
   }
+  if (p.rows <= 16) return run_project_few<T, YT, 1, 4, 16, 1>(p, s);
+  if (p.rows <= 32) return run_project_few<T, YT, 2, 4, 16, 1>(p, s);
   return with_tile(pick_tile(p.rows, p.out_dim, (p.dim * 2 + KB - 1) / KB), [&](auto shape) { return run_project<T, YT, decltype(shape)>(p, s); });
 }
 
