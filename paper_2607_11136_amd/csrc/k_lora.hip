@@ -5,7 +5,7 @@
 // 16-bit values, a rounding and its remainder: b's MFMA then runs over 2 rank k's,
 // which for ranks to 16 is the one k-step that rank alone would take.
 //
-// 18432 x 4096 x 4096, rank 32, an adapter for each of four sequences: 50 us reducing
+// 18432 x 4096 x 4096, rank 32, an adapter for each of four sequences: 47 us reducing
 // (x once from HBM: 29 us) and 485 us (the product alone 460, 1350 TFLOP/s);
 // 3204 x 1544 x 4104, rank 64, seven requests: 13 and 60 us (rows of 3088 bytes
 // straddle the 128-byte lines; the adapters' loads are bound by their latency,
@@ -458,15 +458,14 @@ hipError_t run_reduce_rt(const LoraParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The most ranks a workgroup that still give each CU one: each of them reads all
-// of its rows' x.  1000 rows of 4096, rank 64: 21 us with all ranks in one
+// The most ranks a workgroup, to 64, that still give each CU one: each of them
+// reads all of its rows' x.  1000 rows of 4096, rank 64: 21 us with all ranks in one
 // workgroup, 10 in four; with 50 rows a request 39 and 19; with an adapter drawn
 // for every row 276 and 124.
 template <typename T, int MT>
 hipError_t run_reduce(const LoraParams& p, hipStream_t s) {
   const int64_t blocks = (p.rows + 16 * MT - 1) / (16 * MT);
   auto enough = [&](int rt) { return blocks * ((p.rank + 16 * rt - 1) / (16 * rt)) >= RULE_CUS; };
-  if (p.rank > 64 && enough(8)) return run_reduce_rt<T, MT, 8>(p, s);
   if (p.rank > 32 && enough(4)) return run_reduce_rt<T, MT, 4>(p, s);
   if (p.rank > 16 && enough(2)) return run_reduce_rt<T, MT, 2>(p, s);
   return run_reduce_rt<T, MT, 1>(p, s);
@@ -480,7 +479,10 @@ hipError_t reduce(const LoraParams& p, hipStream_t s) {
     hipLaunchKernelGGL((k_lora_reduce_rows<T>), dim3((unsigned)p.rows, (p.rank + ROW_RANKS - 1) / ROW_RANKS), dim3(REDUCE_WAVES * 64), 0, s, p);
     return hipGetLastError();
   }
-  return p.rows > 4096 ? run_reduce<T, 2>(p, s) : run_reduce<T, 1>(p, s);
+  // (the more rows share a's lines the better, while every CU has a workgroup:
+  // 18432 x 4096 from HBM, us, 32 and 48 rows each: rank 32 71 and 65, rank 128
+  // 144 and 110; 5000 x 4096, rank 16 32 and 41)
+  return p.rows > 48 * RULE_CUS ? run_reduce<T, 3>(p, s) : p.rows > 16 * RULE_CUS ? run_reduce<T, 2>(p, s) : run_reduce<T, 1>(p, s);
 }
 
 template <typename T, typename YT>

@@ -443,7 +443,8 @@ LORA_SIZES = [(1, 8, 8, 8, 1), (1, 4096, 1032, 16, 3), (5, 72, 136, 8, 2), (48, 
               (12500, 136, 520, 32, 5), (16, 2056, 72, 32, 3), (33, 1032, 88, 128, 2),
               (7, 264, 4360, 16, 3), (20, 136, 4136, 24, 4), (47, 72, 8192, 8, 2), (64, 520, 4104, 40, 9), (64, 2056, 520, 16, 3), (30, 64, 8200, 8, 2),
               (582, 72, 3376, 8, 2), (2100, 72, 136, 16, 6), (1100, 72, 136, 32, 6), (600, 136, 72, 64, 9), (4200, 136, 72, 64, 9),
-              (4200, 264, 72, 128, 3), (1, 136, 8200, 16, 2), (13, 1032, 8264, 64, 5), (16, 64, 16392, 8, 30), (32, 520, 8328, 128, 6)]
+              (4200, 264, 72, 128, 3), (1, 136, 8200, 16, 2), (13, 1032, 8264, 64, 5), (16, 64, 16392, 8, 30), (32, 520, 8328, 128, 6),
+              (12400, 72, 72, 72, 4)]
 
 
 @pytest.mark.parametrize("rows,dim,out_dim,rank,n", LORA_SIZES)
