@@ -255,8 +255,9 @@ extern "C" int xema_gated_ffn_bwd_workspace_bytes(int64_t rows, int32_t dim, int
   XEMA_CHECK(check_rows(rows));
   XEMA_CHECK(check_width(dim, XEMA_BF16));
   XEMA_CHECK(check_width(hidden, XEMA_BF16));
-  // dg, du in 16 bits, the partial column sums of both, and dx's partial sums
-  *bytes = 2 * round_up(rows * hidden * 2, kAlign) + gated_bwd_row_chunks(rows) * 2 * hidden * 4 + gated_bwd_dx_parts(rows, dim, hidden) * 4;
+  // dg, du in 16 bits, the partial column sums of both, and the partial sums of dx and of the weights' gradients
+  *bytes = 2 * round_up(rows * hidden * 2, kAlign) + gated_bwd_row_chunks(rows) * 2 * hidden * 4 +
+           (gated_bwd_dx_parts(rows, dim, hidden) + gated_bwd_dw_parts(rows, dim, hidden)) * 4;
   return XEMA_OK;
 }
 

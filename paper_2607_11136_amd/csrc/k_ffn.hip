@@ -6,7 +6,8 @@
 // 16384: 46 us, 5.8 TB/s).
 // Gradient: dg and du first, bound by HBM (1.08 GB in 222 us), as both products
 // need them in either order; then dx, the weights' and the biases' gradients in
-// one launch (8192 x 4096 x 11008: 2.2 ms, 1340 TFLOP/s), the weights and x read
+// one launch (8192 x 4096 x 11008: 2.2 ms, 1340 TFLOP/s) where they take the same
+// tile, and the sums of the parts where a product splits its k; the weights and x read
 // in place through transposing LDS reads: copies in the other order would cost
 // 0.9 GB of traffic a step.
 #include <algorithm>
@@ -293,10 +294,11 @@ struct BwdParams {
   const void* x;
   void *dx, *dgate_w, *dup_w;
   float* dx_parts;              // [parts][rows][dim] where dx's k is split
+  float* dw_parts;              // [w_parts][2][hidden][dim] where the weights' gradients' k (rows) is split
   const float* partial;         // [chunks][2 hidden]
   uint16_t *dgate_b, *dup_b;
   int64_t rows, ldx, ld_dx;
-  int dim, hidden, chunks, parts;
+  int dim, hidden, chunks, parts, w_parts;
 };
 
 // The tile's accumulators as rows row0 + ... of a [rows, cols] matrix.
@@ -333,20 +335,28 @@ __device__ __forceinline__ void store_sums(const f32x4 (&acc)[S::MI][S::NJ], flo
   }
 }
 
-// dx from its parts, in order.
+// Outputs from their parts, in order: n elements in rows of `width`, those from
+// `half` on belonging to out1.
 template <typename T>
-__global__ __launch_bounds__(256) void k_gated_dx_sum(BwdParams p) {
+__global__ __launch_bounds__(256) void k_gated_sum(const float* __restrict__ sums, int parts, int64_t n, int width, T* __restrict__ out0,
+                                                   T* __restrict__ out1, int64_t half, int64_t ld) {
   typedef T t4 __attribute__((ext_vector_type(4)));
-  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, n = p.rows * p.dim;
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
   if (at >= n) return;
-  f32x4 s = *reinterpret_cast<const f32x4*>(p.dx_parts + at);
+  f32x4 s = *reinterpret_cast<const f32x4*>(sums + at);
 #pragma unroll 4
-  for (int i = 1; i < p.parts; ++i) s += *reinterpret_cast<const f32x4*>(p.dx_parts + i * n + at);
+  for (int i = 1; i < parts; ++i) s += *reinterpret_cast<const f32x4*>(sums + i * n + at);
   t4 o;
 #pragma unroll
   for (int e = 0; e < 4; ++e) o[e] = (T)s[e];
-  const int64_t r = at / p.dim;
-  *reinterpret_cast<t4*>((T*)p.dx + r * p.ld_dx + (at - r * p.dim)) = o;
+  const int64_t in = at < half ? at : at - half, r = in / width;
+  *reinterpret_cast<t4*>((at < half ? out0 : out1) + r * ld + (in - r * width)) = o;
+}
+
+template <typename T>
+hipError_t run_sum(const float* sums, int parts, int64_t n, int width, T* out0, T* out1, int64_t half, int64_t ld, hipStream_t s) {
+  hipLaunchKernelGGL((k_gated_sum<T>), dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, s, sums, parts, n, width, out0, out1, half, ld);
+  return hipGetLastError();
 }
 
 template <typename S>
@@ -354,10 +364,20 @@ __host__ __device__ constexpr int tiles_of(int64_t rows, int cols) {
   return (int)((rows + S::BM - 1) / S::BM) * ((cols + S::BN - 1) / S::BN);
 }
 
+// Where a tile goes: rows row0 + ... of [rows, cols], to `out`, or its sums to
+// `sums` where it has a part of k alone.
+template <typename T>
+struct TileOut {
+  T* out;
+  float* sums;
+  int64_t ld, row0, rows;
+  int col0, cols;
+};
+
 // dx = dg Wg + du Wu: the weights are read k by k (a row of W is one k).  With
 // parts, workgroup wg has part wg / tiles of the steps, its sums kept in fp32.
 template <typename T, typename S>
-__device__ __forceinline__ void dx_tile(const BwdParams& p, int wg, uint8_t* smem, int wave, int lane, f32x4 (&acc)[S::MI][S::NJ]) {
+__device__ __forceinline__ TileOut<T> dx_tile(const BwdParams& p, int wg, uint8_t* smem, int wave, int lane, f32x4 (&acc)[S::MI][S::NJ]) {
   const int tiles = tiles_of<S>(p.rows, p.dim), part = __builtin_amdgcn_readfirstlane(wg / tiles);
   int tm, tn;
   tile_of(wg - part * tiles, (int)((p.rows + S::BM - 1) / S::BM), (p.dim + S::BN - 1) / S::BN, 1024 / S::BM, &tm, &tn);
@@ -368,27 +388,35 @@ __device__ __forceinline__ void dx_tile(const BwdParams& p, int wg, uint8_t* sme
   a.init((const T*)p.dg + m0 * p.hidden, (const T*)p.du + m0 * p.hidden, p.rows - m0, (int64_t)p.hidden * 2, p.hidden * 2, steps, wave, lane, first);
   b.init((const T*)p.gate_w + n0, (const T*)p.up_w + n0, p.dim - n0, (int64_t)p.dim * 2, p.hidden, steps, wave, lane, first);
   tile_products<S, T, ROWS, COLUMNS>(a, b, min(each, 2 * steps - first), smem, wave, lane, acc);
-  if (p.parts > 1) {
-    store_sums<S>(acc, p.dx_parts + part * p.rows * p.dim, p.dim, m0 + wave / S::WNW * S::WR, p.rows, n0 + wave % S::WNW * S::WC, p.dim, lane);
-    return;
-  }
-  store_tile<T, S>(acc, (T*)p.dx, p.ld_dx, m0 + wave / S::WNW * S::WR, p.rows, n0 + wave % S::WNW * S::WC, p.dim, lane);
+  return {(T*)p.dx, p.parts > 1 ? p.dx_parts + part * p.rows * p.dim : nullptr, p.parts > 1 ? p.dim : p.ld_dx,
+          m0 + wave / S::WNW * S::WR, p.rows, n0 + wave % S::WNW * S::WC, p.dim};
 }
 
-// dWg = dg^T x and dWu = du^T x: both operands are read k (row) by k.
+// dWg = dg^T x and dWu = du^T x: both operands are read k (row) by k.  With
+// w_parts, workgroup wg has part wg / tiles of the rows, its sums kept in fp32.
 template <typename T, typename S>
-__device__ __forceinline__ void dw_tile(const BwdParams& p, int wg, uint8_t* smem, int wave, int lane, f32x4 (&acc)[S::MI][S::NJ]) {
-  const int tiles_h = (p.hidden + S::BM - 1) / S::BM;
+__device__ __forceinline__ TileOut<T> dw_tile(const BwdParams& p, int wg, uint8_t* smem, int wave, int lane, f32x4 (&acc)[S::MI][S::NJ]) {
+  const int tiles_h = (p.hidden + S::BM - 1) / S::BM, tiles = 2 * tiles_of<S>(p.hidden, p.dim);
+  const int steps = (int)((p.rows + 63) / 64);
+  int part = 0, first = 0, count = steps;
+  if (p.w_parts > 1) {
+    const int each = (steps + p.w_parts - 1) / p.w_parts;
+    part = __builtin_amdgcn_readfirstlane(wg / tiles);
+    first = part * each;
+    count = min(each, steps - first);
+  }
   int tm, tn;
-  tile_of(wg, 2 * tiles_h, (p.dim + S::BN - 1) / S::BN, 1024 / S::BM, &tm, &tn);
+  tile_of(wg - part * tiles, 2 * tiles_h, (p.dim + S::BN - 1) / S::BN, 1024 / S::BM, &tm, &tn);
   const bool up = tm >= tiles_h;
+  const int64_t r0 = (int64_t)first * 64;
   const int m0 = (up ? tm - tiles_h : tm) * S::BM, n0 = tn * S::BN;
   ColumnOperand<S::BM, S::NW> a;
   ColumnOperand<S::BN, S::NW> b;
-  a.init((const T*)(up ? p.du : p.dg) + m0, nullptr, p.hidden - m0, (int64_t)p.hidden * 2, p.rows, 0x7fffffff, wave, lane);
-  b.init((const T*)p.x + n0, nullptr, p.dim - n0, p.ldx * 2, p.rows, 0x7fffffff, wave, lane);
-  tile_products<S, T, COLUMNS, COLUMNS>(a, b, (int)((p.rows + 63) / 64), smem, wave, lane, acc);
-  store_tile<T, S>(acc, (T*)(up ? p.dup_w : p.dgate_w), p.dim, m0 + wave / S::WNW * S::WR, p.hidden, n0 + wave % S::WNW * S::WC, p.dim, lane);
+  a.init((const T*)(up ? p.du : p.dg) + r0 * p.hidden + m0, nullptr, p.hidden - m0, (int64_t)p.hidden * 2, p.rows - r0, 0x7fffffff, wave, lane);
+  b.init((const T*)p.x + r0 * p.ldx + n0, nullptr, p.dim - n0, p.ldx * 2, p.rows - r0, 0x7fffffff, wave, lane);
+  tile_products<S, T, COLUMNS, COLUMNS>(a, b, count, smem, wave, lane, acc);
+  return {(T*)(up ? p.dup_w : p.dgate_w), p.w_parts > 1 ? p.dw_parts + ((int64_t)part * 2 + up) * p.hidden * p.dim : nullptr, p.dim,
+          m0 + wave / S::WNW * S::WR, p.hidden, n0 + wave % S::WNW * S::WC, p.dim};
 }
 
 // The products of the gradient in one launch: first dx's tiles, whose k is the
@@ -413,13 +441,14 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_gated_products(BwdParams p, i
   for (int i = 0; i < S::MI; ++i)
 #pragma unroll
     for (int j = 0; j < S::NJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (wg < dx_tiles) dx_tile<T, S>(p, wg, smem, wave, lane, acc);
-  else dw_tile<T, S>(p, wg - dx_tiles, smem, wave, lane, acc);
+  const TileOut<T> o = wg < dx_tiles ? dx_tile<T, S>(p, wg, smem, wave, lane, acc) : dw_tile<T, S>(p, wg - dx_tiles, smem, wave, lane, acc);
+  if (o.sums) store_sums<S>(acc, o.sums, o.ld, o.row0, o.rows, o.col0, o.cols, lane);
+  else store_tile<T, S>(acc, o.out, o.ld, o.row0, o.rows, o.col0, o.cols, lane);
 }
 
 template <typename T, typename S>
 hipError_t run_products(const BwdParams& p, bool dx, bool dw, bool db, hipStream_t s) {
-  const int dx_tiles = dx ? tiles_of<S>(p.rows, p.dim) * p.parts : 0, dw_tiles = dw ? 2 * tiles_of<S>(p.hidden, p.dim) : 0;
+  const int dx_tiles = dx ? tiles_of<S>(p.rows, p.dim) * p.parts : 0, dw_tiles = dw ? 2 * tiles_of<S>(p.hidden, p.dim) * p.w_parts : 0;
   const int db_wgs = db ? (2 * p.hidden + S::NW * 64 - 1) / (S::NW * 64) : 0;
   if (!(dx_tiles + dw_tiles + db_wgs)) return hipSuccess;
   hipLaunchKernelGGL((k_gated_products<T, S>), dim3((unsigned)(dx_tiles + dw_tiles + db_wgs)), dim3(S::NW * 64), 0, s, p, dx_tiles, dw_tiles);
@@ -442,20 +471,25 @@ hipError_t bwd_t(const xema_gated_ffn_bwd_args& a, hipStream_t s) {
   }
   const bool dx = a.dx && a.rows > 0, dw = a.dgate_w, db = a.dgate_b;
   const FfnSplit sx = pick_split(a.rows, a.dim, 2 * ((a.hidden + 63) / 64));
-  const FfnTile tw = pick_tile(2 * (int64_t)a.hidden, a.dim, (a.rows + 63) / 64);
+  const FfnSplit sw = pick_split(2 * (int64_t)a.hidden, a.dim, (a.rows + 63) / 64);
   float* dx_parts = (float*)(ws + 2 * part + gated_bwd_row_chunks(a.rows) * 2 * a.hidden * 4);
-  const BwdParams p{dg, du, a.gate_w, a.up_w, a.x, a.dx, a.dgate_w, a.dup_w, dx_parts, partial, (uint16_t*)a.dgate_b, (uint16_t*)a.dup_b,
-                    a.rows, a.ldx, a.ld_dx, a.dim, a.hidden, a.rows > 0 ? chunks : 0, sx.parts};
+  float* dw_parts = dx_parts + gated_bwd_dx_parts(a.rows, a.dim, a.hidden);
+  const BwdParams p{dg, du, a.gate_w, a.up_w, a.x, a.dx, a.dgate_w, a.dup_w, dx_parts, dw_parts, partial, (uint16_t*)a.dgate_b, (uint16_t*)a.dup_b,
+                    a.rows, a.ldx, a.ld_dx, a.dim, a.hidden, a.rows > 0 ? chunks : 0, sx.parts, sw.parts};
   // one launch where both products take the same tile
-  if (dx && dw && sx.tile != tw) {
+  if (dx && dw && sx.tile != sw.tile) {
     e = with_tile(sx.tile, [&](auto shape) { return run_products<T, decltype(shape)>(p, true, false, false, s); });
-    if (e == hipSuccess) e = with_tile(tw, [&](auto shape) { return run_products<T, decltype(shape)>(p, false, true, db, s); });
+    if (e == hipSuccess) e = with_tile(sw.tile, [&](auto shape) { return run_products<T, decltype(shape)>(p, false, true, db, s); });
   } else {
-    e = with_tile(dx ? sx.tile : tw, [&](auto shape) { return run_products<T, decltype(shape)>(p, dx, dw, db, s); });
+    e = with_tile(dx ? sx.tile : sw.tile, [&](auto shape) { return run_products<T, decltype(shape)>(p, dx, dw, db, s); });
   }
-  if (e != hipSuccess || !dx || sx.parts == 1) return e;
-  hipLaunchKernelGGL((k_gated_dx_sum<T>), dim3((unsigned)((a.rows * a.dim / 4 + 255) / 256)), dim3(256), 0, s, p);
-  return hipGetLastError();
+  if (e == hipSuccess && dx && sx.parts > 1)
+    e = run_sum<T>(dx_parts, sx.parts, a.rows * a.dim, a.dim, (T*)a.dx, (T*)a.dx, a.rows * a.dim, a.ld_dx, s);
+  if (e == hipSuccess && dw && sw.parts > 1) {
+    const int64_t one = (int64_t)a.hidden * a.dim;
+    e = run_sum<T>(dw_parts, sw.parts, 2 * one, a.dim, (T*)a.dgate_w, (T*)a.dup_w, one, a.dim, s);
+  }
+  return e;
 }
 
 }  // namespace
@@ -472,6 +506,11 @@ int64_t gated_bwd_row_chunks(int64_t rows) { return std::max<int64_t>(1, std::mi
 int64_t gated_bwd_dx_parts(int64_t rows, int dim, int hidden) {
   const int parts = rows > 0 ? pick_split(rows, dim, 2 * ((hidden + 63) / 64)).parts : 1;
   return parts > 1 ? parts * rows * dim : 0;
+}
+
+int64_t gated_bwd_dw_parts(int64_t rows, int dim, int hidden) {
+  const int parts = pick_split(2 * (int64_t)hidden, dim, (rows + 63) / 64).parts;
+  return parts > 1 ? (int64_t)parts * 2 * hidden * dim : 0;
 }
 
 hipError_t launch_gated_ffn_bwd(const xema_gated_ffn_bwd_args& a, hipStream_t s) {

@@ -154,9 +154,10 @@ inline FfnTile pick_tile(int64_t m, int64_t n, int64_t steps) {
 
 // A product whose k may be split: `parts` sums over consecutive steps, kept in
 // fp32 and added by a launch of their own (3 us, and the sums' bytes at about 4
-// TB/s there and back).  For few rows and long k (dx of a short batch), whose
-// tiles leave most CUs idle.  us whole and split: 333 x 512, 44 steps 16 and 8;
-// 64 x 4096, 344 steps 96 and 40.
+// TB/s there and back).  For small results of long k (dx of a short batch, the
+// weights' gradients of a narrow layer), whose tiles leave most CUs idle.  us whole
+// and split: 333 x 512, 44 steps 16 and 8; 64 x 4096, 344 steps 96 and 40; 2 1024 x
+// 512, 469 steps 141 and 69.
 struct FfnSplit { FfnTile tile; int parts; };
 inline FfnSplit pick_split(int64_t m, int64_t n, int64_t steps) {
   FfnSplit best{pick_tile(m, n, steps), 1};

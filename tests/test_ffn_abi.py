@@ -155,7 +155,10 @@ def test_null_arguments():
 def test_workspace_sizes():
     # dg and du in 16 bits, 256-byte aligned, and up to 64 partial sums of 2 x hidden floats
     assert X.xema_gated_ffn_bwd_workspace_bytes(3, 64, 40) == 2 * 256 + 2 * 40 * 4
-    assert X.xema_gated_ffn_bwd_workspace_bytes(100000, 64, 4096) == 2 * 100000 * 4096 * 2 + 64 * 2 * 4096 * 4
+    assert X.xema_gated_ffn_bwd_workspace_bytes(100000, 4096, 4096) == 2 * 100000 * 4096 * 2 + 64 * 2 * 4096 * 4
+    # and two or more fp32 sums of the weights' gradients where they have few tiles
+    more = X.xema_gated_ffn_bwd_workspace_bytes(100000, 64, 4096) - (2 * 100000 * 4096 * 2 + 64 * 2 * 4096 * 4)
+    assert more % (2 * 4096 * 64 * 4) == 0 and 2 <= more // (2 * 4096 * 64 * 4) <= 16
     assert X.xema_gated_ffn_pre_bytes(0, 64) == 0 and X.xema_gated_ffn_pre_bytes(100000, 4096) == 6 * 100000 * 4096
     assert X.xema_rmsnorm_bwd_workspace_bytes(1, 64) == 64 * 4
     assert X.xema_rmsnorm_bwd_workspace_bytes(100000, 64) == 1024 * 64 * 4

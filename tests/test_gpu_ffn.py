@@ -319,7 +319,7 @@ def test_gated_ffn_extreme_gates(act):
     R.within(dub, a, R.rounded(a, 64 * R.U * a.abs() + 1e-30, BF16), "act again")
 
 
-BWD_SIZES = [(1, 8, 8), (2, 64, 40), (17, 512, 1368), (63, 128, 64), (65, 136, 200), (130, 328, 520), (257, 1544, 264), (1100, 256, 1032),
+BWD_SIZES = [(4500, 64, 72), (9000, 72, 328), (2100, 264, 392), (1, 8, 8), (2, 64, 40), (17, 512, 1368), (63, 128, 64), (65, 136, 200), (130, 328, 520), (257, 1544, 264), (1100, 256, 1032),
              (2100, 4104, 2056), (5000, 4104, 72), (70, 136, 4104), (5, 1032, 2056),
              (39, 280, 5456), (35, 544, 5504), (33, 528, 1816), (2711, 1456, 72), (1614, 1240, 2400),
              (40, 1800, 2304), (69, 1136, 4120)]
