@@ -153,11 +153,11 @@ inline FfnTile pick_tile(int64_t m, int64_t n, int64_t steps) {
 }
 
 // A product whose k may be split: `parts` sums over consecutive steps, kept in
-// fp32 and added by a launch of their own (3 us, and the sums' bytes at about 4
-// TB/s there and back).  For small results of long k (dx of a short batch, the
-// weights' gradients of a narrow layer), whose tiles leave most CUs idle.  us whole
-// and split: 333 x 512, 44 steps 16 and 8; 64 x 4096, 344 steps 96 and 40; 2 1024 x
-// 512, 469 steps 141 and 69.
+// fp32 and added by a launch of their own (3 us, and the sums' bytes at about 7
+// TB/s there and back, for most stay in the caches).  For small results of long k
+// (dx of a short batch, the weights' gradients of a narrow layer), whose tiles leave
+// most CUs idle.  us whole and split: 333 x 512, 44 steps 16 and 8; 64 x 4096, 344
+// steps 96 and 40; 2 1024 x 512, 469 steps 141 and 69.
 struct FfnSplit { FfnTile tile; int parts; };
 inline FfnSplit pick_split(int64_t m, int64_t n, int64_t steps) {
   FfnSplit best{pick_tile(m, n, steps), 1};
@@ -166,7 +166,7 @@ inline FfnSplit pick_split(int64_t m, int64_t n, int64_t steps) {
     const int64_t each = (steps + want - 1) / want, parts = (steps + each - 1) / each;
     if (m * n * parts > ((int64_t)1 << 24)) break;      // (64 MiB of sums)
     for (int t = 0; t < FFN_TILES; ++t) {
-      const double us = ffn_tile_us(kFfnCost[t], m, n, each, parts) + 3.0 + (double)m * n * 8 * parts / 4e6;
+      const double us = ffn_tile_us(kFfnCost[t], m, n, each, parts) + 3.0 + (double)m * n * 8 * parts / 7e6;
       if (us < least) { best = {(FfnTile)t, (int)parts}; least = us; }
     }
   }
