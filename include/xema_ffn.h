@@ -189,7 +189,9 @@ XEMA_API int xema_op_gated_ffn_bwd(const xema_gated_ffn_bwd_args* args, void* st
  * x[r] a[i]^T is summed in fp32, scaled, and carried as two values of `dtype`,
  * its rounding and the rounding of what that leaves (16 significant bits in
  * bf16; an infinity past fp16's range), through the workspace (256-byte
- * aligned, at least xema_lora_workspace_bytes(rows, rank) bytes).           */
+ * aligned, at least xema_lora_workspace_bytes(rows, rank) bytes).  Infinities
+ * and NaN of b meet the first of the two alone, so that they give the formula's
+ * infinities and NaN.                                                       */
 typedef struct {
   int32_t dtype;
   int64_t rows; int32_t dim, out_dim;

@@ -224,6 +224,25 @@ struct WaveAdapters {
   }
 };
 
+// b as the remainders meet it: zeros in place of infinities and NaN (16-bit
+// elements whose exponent is all ones), which the values have met with t's sign
+// already: a remainder, zero or of the other sign, would make NaN of infinity.
+// (A full exponent and its own lowest bit carry into the sign's place.)  us
+// without and with it and the second pass of add_to_others: 1000 x 4096 x 4096,
+// rank 64, mixed rows 211 and 213; 128 rows, rank 16, mixed 33 and 35; 3204 x 1544 x
+// 4104, rank 64, seven requests 75 and 75.
+template <typename T>
+__device__ __forceinline__ typename Frag<T>::type finite_only(typename Frag<T>::type f) {
+  constexpr uint32_t EXP = std::is_same_v<T, bf16> ? 0x7f807f80u : 0x7c007c00u, LOW = std::is_same_v<T, bf16> ? 0x00800080u : 0x04000400u;
+  u32x4 w = __builtin_bit_cast(u32x4, f);
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const uint32_t full = ((w[d] & EXP) + LOW) >> 15 & 0x00010001u;
+    w[d] &= ~((full << 16) - full);
+  }
+  return __builtin_bit_cast(typename Frag<T>::type, w);
+}
+
 // acc += t[r] b[i]^T for the rows with adapter `one` (-1: none): the values'
 // MFMA k-range and the remainders', over the same b.  The products are formed
 // for all rows, and kept for those (a product with zeros in the place of
@@ -256,6 +275,11 @@ __device__ __forceinline__ void add_adapter(const LoraParams& p, int64_t m0, int
         if (in) ft[u][i] = *reinterpret_cast<const frag*>((const T*)p.t + (m < p.rows ? m : p.rows - 1) * 2 * p.rank + at * 8);
       }
     }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (k + 4 * u + 3 >= rs)                 // (a step that no remainder is in is left as it is)
+#pragma unroll
+        for (int j = 0; j < S::NJ; ++j) fb[u][j] = k + 4 * u + l4 >= rs ? finite_only<T>(fb[u][j]) : fb[u][j];
 #pragma unroll
     for (int i = 0; i < S::MI; ++i) {
       const bool keep = who.id[i] == one;
@@ -305,44 +329,69 @@ __device__ __forceinline__ void add_to_others(const LoraParams& p, int64_t m0, i
     if (!(who.others >> i & 1)) continue;
     const int64_t m = m0 + 16 * i + l16;
     const T* t = (const T*)p.t + (m < p.rows ? m : p.rows - 1) * 2 * p.rank;
-    for (uint64_t todo = __ballot(who.further(p, who.id[i], PASSES)); todo;) {
-      int one[TOGETHER];
-      f32x4 v[TOGETHER][S::NJ];
+    const bool further = who.further(p, who.id[i], PASSES);
+    f32x4 before[S::NJ];
 #pragma unroll
-      for (int u = 0; u < TOGETHER; ++u) {
-        one[u] = todo ? __builtin_amdgcn_readlane(who.id[i], __builtin_ctzll(todo)) : one[0];
-        todo &= ~__ballot(who.id[i] == one[u]);
+    for (int j = 0; j < S::NJ; ++j) before[j] = acc[i][j];
+    // Where a sum comes out infinite or NaN all are formed again with finite_only
+    // (in every pass that took 3 to 10% of the whole call, and where all is finite
+    // it changes nothing).
+    for (bool again = false;; again = true) {
+      for (uint64_t todo = __ballot(further); todo;) {
+        int one[TOGETHER];
+        f32x4 v[TOGETHER][S::NJ];
 #pragma unroll
-        for (int j = 0; j < S::NJ; ++j) v[u][j] = acc[i][j];
-      }
-      for (int k0 = 0; k0 < p.rank; k0 += 32) {
-        const int k = k0 + l4 * 8;
-        frag fb[TOGETHER][S::NJ], hi = {}, lo = {};
+        for (int u = 0; u < TOGETHER; ++u) {
+          one[u] = todo ? __builtin_amdgcn_readlane(who.id[i], __builtin_ctzll(todo)) : one[0];
+          todo &= ~__ballot(who.id[i] == one[u]);
 #pragma unroll
-        for (int u = 0; u < TOGETHER; ++u)
+          for (int j = 0; j < S::NJ; ++j) v[u][j] = acc[i][j];
+        }
+        for (int k0 = 0; k0 < p.rank; k0 += 32) {
+          const int k = k0 + l4 * 8;
+          frag fb[TOGETHER][S::NJ], hi = {}, lo = {};
 #pragma unroll
-          for (int j = 0; j < S::NJ; ++j) fb[u][j] = frag{};
-        if (k < p.rank) {
+          for (int u = 0; u < TOGETHER; ++u)
 #pragma unroll
-          for (int u = 0; u < TOGETHER; ++u) {
-            const T* b = (const T*)p.b + (int64_t)one[u] * p.out_dim * p.rank + k;
+            for (int j = 0; j < S::NJ; ++j) fb[u][j] = frag{};
+          if (k < p.rank) {
 #pragma unroll
-            for (int j = 0; j < S::NJ; ++j) fb[u][j] = *reinterpret_cast<const frag*>(b + min(n0 + 16 * j + l16, p.out_dim - 1) * p.rank);
+            for (int u = 0; u < TOGETHER; ++u) {
+              const T* b = (const T*)p.b + (int64_t)one[u] * p.out_dim * p.rank + k;
+#pragma unroll
+              for (int j = 0; j < S::NJ; ++j) fb[u][j] = *reinterpret_cast<const frag*>(b + min(n0 + 16 * j + l16, p.out_dim - 1) * p.rank);
+            }
+            hi = *reinterpret_cast<const frag*>(t + k);
+            lo = *reinterpret_cast<const frag*>(t + p.rank + k);
           }
-          hi = *reinterpret_cast<const frag*>(t + k);
-          lo = *reinterpret_cast<const frag*>(t + p.rank + k);
+#pragma unroll
+          for (int u = 0; u < TOGETHER; ++u)
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j) {
+              v[u][j] = Frag<T>::run(fb[u][j], hi, v[u][j]);
+              if (again) fb[u][j] = finite_only<T>(fb[u][j]);
+            }
+#pragma unroll
+          for (int u = 0; u < TOGETHER; ++u)
+#pragma unroll
+            for (int j = 0; j < S::NJ; ++j) v[u][j] = Frag<T>::run(fb[u][j], lo, v[u][j]);
         }
 #pragma unroll
         for (int u = 0; u < TOGETHER; ++u)
 #pragma unroll
-          for (int j = 0; j < S::NJ; ++j) v[u][j] = Frag<T>::run(fb[u][j], lo, Frag<T>::run(fb[u][j], hi, v[u][j]));
+          for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = who.id[i] == one[u] ? v[u][j][e] : acc[i][j][e];
       }
+      if (again) break;
+      float zero = 0.f;                        // (an infinity or NaN makes NaN of it)
 #pragma unroll
-      for (int u = 0; u < TOGETHER; ++u)
+      for (int j = 0; j < S::NJ; ++j)
 #pragma unroll
-        for (int j = 0; j < S::NJ; ++j)
+        for (int e = 0; e < 4; ++e) zero = fmaf(acc[i][j][e], 0.f, zero);
+      if (!__ballot(further && zero != 0.f)) break;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][j][e] = who.id[i] == one[u] ? v[u][j][e] : acc[i][j][e];
+      for (int j = 0; j < S::NJ; ++j) acc[i][j] = further ? before[j] : acc[i][j];
     }
   }
 }
