@@ -25,7 +25,9 @@
  * 16-byte aligned); widths are multiples of 8 (of 16 for XEMA_E4M3 rows) and
  * at most 131072; row counts are any from 0 (nothing is launched) to
  * 2^24 - 1.  Outputs must not overlap inputs, workspaces or each other,
- * except where an entry point allows it.
+ * except where an entry point allows it (XEMA_ERR_INVALID_ARG).  Column ranges
+ * of one buffer, and vectors between its rows, do not overlap; matrices whose
+ * rows interleave at unlike distances are refused as if they did.
  *
  * Sums and statistics are fp32 (MFMA accumulators, row sums), each in one
  * fixed order, with no atomics: the same call gives the same bytes.  What

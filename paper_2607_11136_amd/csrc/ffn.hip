@@ -1,9 +1,8 @@
 // Host entry points of the feed-forward sub-block's operators (xema_ffn.h):
 // argument validation, then the launches of k_norm.hip, k_ffn.hip and
 // k_lora.hip.
-#include <initializer_list>
-
 #include "ffn.h"
+#include "spans.h"
 #include "xema_internal.h"
 
 using namespace xema;
@@ -21,23 +20,8 @@ int64_t elem(int dtype) { return dtype == XEMA_F32 ? 4 : dtype == XEMA_E4M3 ? 1 
 bool is16(int d) { return d == XEMA_BF16 || d == XEMA_F16; }
 bool is_norm_type(int d) { return is16(d) || d == XEMA_F32; }
 
-// A matrix or vector argument: the bytes it spans.
-struct Span {
-  const void* p;
-  int64_t bytes;
-};
 Span matrix(const void* p, int dtype, int64_t rows, int64_t width, int64_t ld) {
-  return {p, p && rows > 0 ? ((rows - 1) * ld + width) * elem(dtype) : 0};
-}
-bool overlaps(const Span& a, const Span& b) {
-  if (!a.p || !b.p || !a.bytes || !b.bytes) return false;
-  const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
-  return a0 < b0 + (uintptr_t)b.bytes && b0 < a0 + (uintptr_t)a.bytes;
-}
-bool any_overlap(const Span& out, std::initializer_list<Span> others) {
-  for (const Span& o : others)
-    if (overlaps(out, o)) return true;
-  return false;
+  return span_rows(p, width * elem(dtype), rows, ld * elem(dtype));
 }
 
 int check_rows(int64_t rows) {
