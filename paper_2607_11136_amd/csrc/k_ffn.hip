@@ -220,10 +220,9 @@ hipError_t run_gated(const GatedParams& p, hipStream_t s) {
 
 template <typename T, typename YT>
 hipError_t gated_t(const GatedParams& p, hipStream_t s) {
-  // (weights from HBM, us, this kernel and the best tile: 16 x 2 4096 x 4096 17
-  // and 21, 32 rows 20 and 22; 16 x 2 11008 x 4096 40 and 39, 32 rows 51 and 40)
-  if (p.rows <= 16) return run_gated_few<T, YT, 1, 4>(p, s);
-  if (p.rows <= 32 && p.hidden <= 8192) return run_gated_few<T, YT, 2, 2>(p, s);
+  const FewPick few = pick_gated_few(p.rows, p.hidden);
+  if (few.rows16 == 1) return run_gated_few<T, YT, 1, 4>(p, s);
+  if (few.rows16 == 2) return run_gated_few<T, YT, 2, 2>(p, s);
   return with_tile(pick_tile(p.rows, 2 * (int64_t)p.hidden, ((int64_t)p.dim * sizeof(T) + KB - 1) / KB),
                    [&](auto shape) { return run_gated<T, YT, decltype(shape)>(p, s); });
 }

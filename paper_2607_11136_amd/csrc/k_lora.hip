@@ -57,7 +57,7 @@ __device__ __forceinline__ void store_reduced(T* t, int rank, int q, const float
 // (requests that meet in it, or single tokens), with one after the other, and a
 // row keeps its own.  While the blocks are fewer than the CUs, what bounds it is
 // how fast one CU gets its part of a and x from L2 (256 KiB in 10 us): the ranks
-// are then dealt to several workgroups (run_reduce).
+// are then dealt to several workgroups (pick_reduce).
 template <typename T, int MT, int RT>
 __global__ __launch_bounds__(REDUCE_WAVES * 64) void k_lora_reduce(LoraParams p) {
   typedef typename Frag<T>::type frag;
@@ -507,31 +507,22 @@ hipError_t run_reduce_rt(const LoraParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The most ranks a workgroup, to 64, that still give each CU one: each of them
-// reads all of its rows' x.  1000 rows of 4096, rank 64: 21 us with all ranks in one
-// workgroup, 10 in four; with 50 rows a request 39 and 19; with an adapter drawn
-// for every row 276 and 124.
 template <typename T, int MT>
-hipError_t run_reduce(const LoraParams& p, hipStream_t s) {
-  const int64_t blocks = (p.rows + 16 * MT - 1) / (16 * MT);
-  auto enough = [&](int rt) { return blocks * ((p.rank + 16 * rt - 1) / (16 * rt)) >= RULE_CUS; };
-  if (p.rank > 32 && enough(4)) return run_reduce_rt<T, MT, 4>(p, s);
-  if (p.rank > 16 && enough(2)) return run_reduce_rt<T, MT, 2>(p, s);
-  return run_reduce_rt<T, MT, 1>(p, s);
+hipError_t run_reduce(const LoraParams& p, int ranks16, hipStream_t s) {
+  return ranks16 == 4 ? run_reduce_rt<T, MT, 4>(p, s) : ranks16 == 2 ? run_reduce_rt<T, MT, 2>(p, s) : run_reduce_rt<T, MT, 1>(p, s);
 }
 
-// A row by itself reads all of its adapter's a, which pays while the rows are
-// few (and then likely single tokens, each with an adapter of its own).
 template <typename T>
 hipError_t reduce(const LoraParams& p, hipStream_t s) {
-  if (p.rows * p.rank <= 32768) {
-    hipLaunchKernelGGL((k_lora_reduce_rows<T>), dim3((unsigned)p.rows, (p.rank + ROW_RANKS - 1) / ROW_RANKS), dim3(REDUCE_WAVES * 64), 0, s, p);
-    return hipGetLastError();
+  const ReducePick pick = pick_reduce(p.rows, p.rank);
+  switch (pick.rows16) {
+    case 0:
+      hipLaunchKernelGGL((k_lora_reduce_rows<T>), dim3((unsigned)p.rows, (p.rank + ROW_RANKS - 1) / ROW_RANKS), dim3(REDUCE_WAVES * 64), 0, s, p);
+      return hipGetLastError();
+    case 1: return run_reduce<T, 1>(p, pick.ranks16, s);
+    case 2: return run_reduce<T, 2>(p, pick.ranks16, s);
+    default: return run_reduce<T, 3>(p, pick.ranks16, s);
   }
-  // (the more rows share a's lines the better, while every CU has a workgroup:
-  // 18432 x 4096 from HBM, us, 32 and 48 rows each: rank 32 71 and 65, rank 128
-  // 144 and 110; 5000 x 4096, rank 16 32 and 41)
-  return p.rows > 48 * RULE_CUS ? run_reduce<T, 3>(p, s) : p.rows > 16 * RULE_CUS ? run_reduce<T, 2>(p, s) : run_reduce<T, 1>(p, s);
 }
 
 template <typename T, typename YT>
@@ -540,28 +531,20 @@ hipError_t lora_t(const LoraParams& p, hipStream_t s) {
     const hipError_t e = reduce<T>(p, s);
     if (e != hipSuccess) return e;
   }
-  // Few rows: one round of workgroups (one a CU), 16, 32 or 64 columns each, 64
-  // also where that takes more rounds.  Past that, and past 64 rows (32 beside 64
-  // columns), every workgroup's reading all of x costs more than the tiles (us,
-  // with the reduction; columns 16, 32, 64, tiles):
-  //   48 x 4096 x 4096   25, 29, -, 32     16 x 4096 x 11008  35, 34, 30, 33
-  //   48 x 4096 x 6144   41, 30, -, 33     1 x 4096 x 16384   35, 34, 34, 38
-  //   48 x 4096 x 11008  59, 52, -, 34     16 x 4096 x 32768  86, 69, 62, 75
-  //   24 x 4096 x 8192   31, 25, -, 32     32 x 4096 x 32768  -, 83, 70, 78
-  if (p.rows <= 64 && p.out_dim <= 4096) {
-    if (p.rows <= 16) return run_project_few<T, YT, 1, 1, 16, 4>(p, s);
-    if (p.rows <= 32) return run_project_few<T, YT, 2, 1, 16, 4>(p, s);
-    if (p.rows <= 48) return run_project_few<T, YT, 3, 1, 16, 2>(p, s);
+  const FewPick few = pick_lora_few(p.rows, p.out_dim);
+  if (few.cols16 == 1) {
+    if (few.rows16 == 1) return run_project_few<T, YT, 1, 1, 16, 4>(p, s);
+    if (few.rows16 == 2) return run_project_few<T, YT, 2, 1, 16, 4>(p, s);
+    if (few.rows16 == 3) return run_project_few<T, YT, 3, 1, 16, 2>(p, s);
     return run_project_few<T, YT, 4, 1, 16, 2>(p, s);
   }
-  if (p.rows <= 64 && p.out_dim <= 8192) {
-    if (p.rows <= 16) return run_project_few<T, YT, 1, 2, 16, 4>(p, s);
-    if (p.rows <= 32) return run_project_few<T, YT, 2, 2, 16, 2>(p, s);
-    if (p.rows <= 48) return run_project_few<T, YT, 3, 2, 16, 2>(p, s);
+  if (few.cols16 == 2) {
+    if (few.rows16 == 1) return run_project_few<T, YT, 1, 2, 16, 4>(p, s);
+    if (few.rows16 == 2) return run_project_few<T, YT, 2, 2, 16, 2>(p, s);
+    if (few.rows16 == 3) return run_project_few<T, YT, 3, 2, 16, 2>(p, s);
     return run_project_few<T, YT, 4, 2, 16, 1>(p, s);
   }
-  if (p.rows <= 16) return run_project_few<T, YT, 1, 4, 16, 1>(p, s);
-  if (p.rows <= 32) return run_project_few<T, YT, 2, 4, 16, 1>(p, s);
+  if (few.cols16 == 4) return few.rows16 == 1 ? run_project_few<T, YT, 1, 4, 16, 1>(p, s) : run_project_few<T, YT, 2, 4, 16, 1>(p, s);
   return with_tile(pick_tile(p.rows, p.out_dim, (p.dim * 2 + KB - 1) / KB), [&](auto shape) { return run_project<T, YT, decltype(shape)>(p, s); });
 }
 

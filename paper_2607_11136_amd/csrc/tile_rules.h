@@ -173,6 +173,51 @@ inline FfnSplit pick_split(int64_t m, int64_t n, int64_t steps) {
   return best;
 }
 
+// Few rows (few_rows.h), in blocks of 16 rows and of 16 columns a workgroup; no
+// blocks: tiles.  The gated feed-forward's workgroups have 16 hidden units (weights
+// from HBM, us, that kernel and the best tile: 16 x 2 4096 x 4096 17 and 21, 32 rows
+// 20 and 22; 16 x 2 11008 x 4096 40 and 39, 32 rows 51 and 40).
+struct FewPick { int rows16, cols16; };
+inline FewPick pick_gated_few(int64_t rows, int hidden) {
+  if (rows <= 16) return {1, 1};
+  if (rows <= 32 && hidden <= 8192) return {2, 1};
+  return {0, 0};
+}
+// The projection with adapters: one round of workgroups (one a CU), 16, 32 or 64
+// columns each, 64 also where that takes more rounds.  Past that, and past 64
+// rows (32 beside 64 columns), every workgroup's reading all of x costs more
+// than the tiles (us, with the reduction; columns 16, 32, 64, tiles):
+//   48 x 4096 x 4096   25, 29, -, 32     16 x 4096 x 11008  35, 34, 30, 33
+//   48 x 4096 x 6144   41, 30, -, 33     1 x 4096 x 16384   35, 34, 34, 38
+//   48 x 4096 x 11008  59, 52, -, 34     16 x 4096 x 32768  86, 69, 62, 75
+//   24 x 4096 x 8192   31, 25, -, 32     32 x 4096 x 32768  -, 83, 70, 78
+inline FewPick pick_lora_few(int64_t rows, int out_dim) {
+  const int rows16 = (int)((rows + 15) / 16);
+  if (rows <= 64 && out_dim <= 4096) return {rows16, 1};
+  if (rows <= 64 && out_dim <= 8192) return {rows16, 2};
+  if (rows <= 32) return {rows16, 4};
+  return {0, 0};
+}
+
+// The adapters' reduction, in blocks of 16 rows and of 16 ranks a workgroup; no
+// blocks: a workgroup per row.  A row by itself reads all of its adapter's a,
+// which pays while the rows are few (and then likely single tokens, each with an
+// adapter of its own).  The more rows share a's lines the better, while every CU
+// has a workgroup (18432 x 4096 from HBM, us, 32 and 48 rows each: rank 32 71 and
+// 65, rank 128 144 and 110; 5000 x 4096, rank 16 32 and 41).  Then the most ranks,
+// to 64, that still give each CU a workgroup, as each reads all of its rows' x
+// (1000 rows of 4096, rank 64: 21 us with all ranks in one workgroup, 10 in four;
+// with 50 rows a request 39 and 19; with an adapter drawn for every row 276 and 124).
+struct ReducePick { int rows16, ranks16; };
+inline ReducePick pick_reduce(int64_t rows, int rank) {
+  if (rows * rank <= 32768) return {0, 0};
+  const int rows16 = rows > 48 * RULE_CUS ? 3 : rows > 16 * RULE_CUS ? 2 : 1;
+  const int64_t blocks = (rows + 16 * rows16 - 1) / (16 * rows16);
+  for (int ranks16 = 4; ranks16 > 1; ranks16 /= 2)
+    if (rank > 8 * ranks16 && blocks * ((rank + 16 * ranks16 - 1) / (16 * ranks16)) >= RULE_CUS) return {rows16, ranks16};
+  return {rows16, 1};
+}
+
 // ---------------------------------------------------------------------------
 // k_upconv.  A tile is RG R fragments of 16 corners (a corner: the four outputs
 // between four source pixels) and 128 / RG channels.
