@@ -192,12 +192,14 @@ XEMA_API int xema_op_gated_ffn_bwd(const xema_gated_ffn_bwd_args* args, void* st
  *   n_adapters or more    is a mistake: its y becomes NaN.
  * rank is a multiple of 8 up to 128 (smaller ranks are padded with zeros, in
  * a or in b); n_adapters may be 0 (a, b and scale are then not read).
- * x[r] a[i]^T is summed in fp32, scaled, and carried as two values of `dtype`,
- * its rounding and the rounding of what that leaves (16 significant bits in
- * bf16; an infinity past fp16's range), through the workspace (256-byte
- * aligned, at least xema_lora_workspace_bytes(rows, rank) bytes).  Infinities
- * and NaN of b meet the first of the two alone, so that they give the formula's
- * infinities and NaN.                                                       */
+ * t = scale x[r] a[i]^T is summed in fp32 and carried as two values of `dtype`,
+ * its rounding and the rounding of what that leaves, through the workspace
+ * (256-byte aligned, at least xema_lora_workspace_bytes(rows, rank) bytes).  In
+ * bf16 that keeps 16 significant bits at fp32's range; in fp16 22, but no finer
+ * than 2^-24 (t is off by up to 2^-25 where it is small), and t is an infinity
+ * from 65520 on, also where y would be finite: such adapters are for bf16.
+ * Infinities and NaN of b meet the first of the two alone, so that they give
+ * the formula's infinities and NaN, but NaN beside a t that is rounded to 0.   */
 typedef struct {
   int32_t dtype;
   int64_t rows; int32_t dim, out_dim;
