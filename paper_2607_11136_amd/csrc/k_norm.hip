@@ -162,7 +162,7 @@ __global__ __launch_bounds__(NORM_WAVES * 64) void k_rmsnorm(xema_rmsnorm_args a
   // (an infinity in s gives NaN and zeros: the largest magnitude is NaN too)
   const float scale = e4m3_scale(row_max<WPR>(top, red_max, wave));
   if (in_row == 0) a.y_scale[r] = scale;
-  // 2^-k: exact for every k from -126 to 120, also as a subnormal
+  // 2^-k: exact, and a normal number for every k from -126 to 120
   const float inv = 1.0f / scale;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {

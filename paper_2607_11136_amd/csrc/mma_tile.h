@@ -201,8 +201,9 @@ typedef __attribute__((address_space(3))) i16x4* lds_i16x4_t;
 
 // The transposing LDS read.  The restrict parameter gives it an alias scope:
 // without one the compiler takes it to depend on every load into LDS in flight
-// and waits for all of them before each read (dW 2.9 -> 1.3 ms); what it does
-// depend on, the main loops wait for themselves.
+// and waits for all of them before each read (the weights' gradients of 8192 x
+// 4096 x 2 11008 2.9 ms, with it 1.15); what it does depend on, the main loops
+// wait for themselves.
 __device__ __forceinline__ i16x4 read_transposed(lds_i16x4_t __restrict__ p) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
 }

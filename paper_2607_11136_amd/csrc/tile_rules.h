@@ -202,7 +202,16 @@ inline FewPick pick_lora_few(int64_t rows, int out_dim) {
 // The adapters' reduction, in blocks of 16 rows and of 16 ranks a workgroup; no
 // blocks: a workgroup per row.  A row by itself reads all of its adapter's a,
 // which pays while the rows are few (and then likely single tokens, each with an
-// adapter of its own).  The more rows share a's lines the better, while every CU
+// adapter of its own): rows of 4096, with a projection to 72, us, row by row and in
+// blocks,
+//                          one adapter   50 rows a request   drawn of 24 per row
+//   4096 rows, rank 8         44, 29           45, 37              53, 128
+//   1024 rows, rank 32        37, 30           39, 39              51, 139
+//   256 rows, rank 128        40, 33           46, 44              93, 170
+// and past the limit
+//   2048 rows, rank 32        49, 30           51, 39              66, 156
+//   512 rows, rank 128        52, 33           59, 45              111, 171
+// The more rows share a's lines the better, while every CU
 // has a workgroup (18432 x 4096 from HBM, us, 32 and 48 rows each: rank 32 71 and
 // 65, rank 128 144 and 110; 5000 x 4096, rank 16 32 and 41).  Then the most ranks,
 // to 64, that still give each CU a workgroup, as each reads all of its rows' x
