@@ -16,8 +16,9 @@
  * Conventions are those of xema.h and xema_ops.h: status return, host-side
  * validation before any launch, caller-owned device buffers, no allocation,
  * no state between calls, asynchronous on `stream` (a hipStream_t of the
- * current device, NULL = default stream; XEMA_ERR_INVALID_ARG for a stream of
- * another device), 16-byte aligned pointers unless stated.  Every entry point
+ * current device, NULL or hipStreamLegacy = default stream, hipStreamPerThread;
+ * XEMA_ERR_INVALID_ARG for a stream of another device), 16-byte aligned pointers
+ * unless stated.  Every entry point
  * can be captured into a graph; workspaces are scratch memory whose contents
  * on entry are ignored, and calls that may overlap need one each.  Matrices
  * are row-major with a leading dimension ("ld", in elements) of at least

@@ -40,12 +40,17 @@ int check_matrix(const void* p, int dtype, int64_t width, int64_t ld, bool optio
   return !aligned(p, 16) || ld * elem(dtype) % 16 ? XEMA_ERR_MISALIGNED : XEMA_OK;
 }
 
-// The stream must belong to the current device, where the launches go.
-int check_stream(void* stream) {
-  if (!stream) return XEMA_OK;
+// The stream of a call, which must belong to the current device, where the
+// launches go.  The two handles that are no streams of their own, the default
+// stream's and the calling thread's, do by their meaning, and are not asked about
+// (hipStreamGetDevice follows the former as an address).
+int take_stream(void* stream, hipStream_t* s) {
+  *s = (hipStream_t)stream;
+  if (*s == hipStreamLegacy) *s = nullptr;
+  if (!*s || *s == hipStreamPerThread) return XEMA_OK;
   int device = 0;
   hipDevice_t of = 0;
-  if (hipGetDevice(&device) != hipSuccess || hipStreamGetDevice((hipStream_t)stream, &of) != hipSuccess) return XEMA_ERR_HIP;
+  if (hipGetDevice(&device) != hipSuccess || hipStreamGetDevice(*s, &of) != hipSuccess) return XEMA_ERR_HIP;
   return of == device ? XEMA_OK : XEMA_ERR_INVALID_ARG;
 }
 
@@ -199,8 +204,9 @@ int check_lora(const xema_lora_args* a) {
 extern "C" int xema_op_rmsnorm(const xema_rmsnorm_args* args, void* stream) {
   XEMA_CHECK(check_rmsnorm(args));
   if (args->rows == 0) return XEMA_OK;
-  XEMA_CHECK(check_stream(stream));
-  return hip_status(launch_rmsnorm(*args, (hipStream_t)stream));
+  hipStream_t s;
+  XEMA_CHECK(take_stream(stream, &s));
+  return hip_status(launch_rmsnorm(*args, s));
 }
 
 extern "C" int xema_rmsnorm_bwd_workspace_bytes(int64_t rows, int32_t dim, int64_t* bytes) {
@@ -215,15 +221,17 @@ extern "C" int xema_rmsnorm_bwd_workspace_bytes(int64_t rows, int32_t dim, int64
 extern "C" int xema_op_rmsnorm_bwd(const xema_rmsnorm_bwd_args* args, void* stream) {
   XEMA_CHECK(check_rmsnorm_bwd(args));
   if (args->rows == 0 && !args->dgamma) return XEMA_OK;
-  XEMA_CHECK(check_stream(stream));
-  return hip_status(launch_rmsnorm_bwd(*args, (hipStream_t)stream));
+  hipStream_t s;
+  XEMA_CHECK(take_stream(stream, &s));
+  return hip_status(launch_rmsnorm_bwd(*args, s));
 }
 
 extern "C" int xema_op_gated_ffn(const xema_gated_ffn_args* args, void* stream) {
   XEMA_CHECK(check_gated(args));
   if (args->rows == 0) return XEMA_OK;
-  XEMA_CHECK(check_stream(stream));
-  return hip_status(launch_gated_ffn(*args, (hipStream_t)stream));
+  hipStream_t s;
+  XEMA_CHECK(take_stream(stream, &s));
+  return hip_status(launch_gated_ffn(*args, s));
 }
 
 extern "C" int xema_gated_ffn_pre_bytes(int64_t rows, int32_t hidden, int64_t* bytes) {
@@ -248,8 +256,9 @@ extern "C" int xema_gated_ffn_bwd_workspace_bytes(int64_t rows, int32_t dim, int
 extern "C" int xema_op_gated_ffn_bwd(const xema_gated_ffn_bwd_args* args, void* stream) {
   XEMA_CHECK(check_gated_bwd(args));
   if (args->rows == 0 && !args->dgate_w && !args->dgate_b) return XEMA_OK;
-  XEMA_CHECK(check_stream(stream));
-  return hip_status(launch_gated_ffn_bwd(*args, (hipStream_t)stream));
+  hipStream_t s;
+  XEMA_CHECK(take_stream(stream, &s));
+  return hip_status(launch_gated_ffn_bwd(*args, s));
 }
 
 extern "C" int xema_lora_workspace_bytes(int64_t rows, int32_t rank, int64_t* bytes) {
@@ -263,6 +272,7 @@ extern "C" int xema_lora_workspace_bytes(int64_t rows, int32_t rank, int64_t* by
 extern "C" int xema_op_lora_linear(const xema_lora_args* args, void* stream) {
   XEMA_CHECK(check_lora(args));
   if (args->rows == 0) return XEMA_OK;
-  XEMA_CHECK(check_stream(stream));
-  return hip_status(launch_lora_linear(*args, (hipStream_t)stream));
+  hipStream_t s;
+  XEMA_CHECK(take_stream(stream, &s));
+  return hip_status(launch_lora_linear(*args, s));
 }

@@ -106,3 +106,19 @@ def test_the_marks_are_seen():
         call(None)
         torch.cuda.synchronize()
         assert any(not torch.equal(t.view(torch.uint8), w.view(torch.uint8)) for t, w in zip(outputs, want)), case
+
+
+@pytest.mark.parametrize("case", CASES)
+@pytest.mark.parametrize("handle", [0, 1, 2])
+def test_handles_of_implicit_streams(case, handle):
+    """NULL, hipStreamLegacy and hipStreamPerThread."""
+    inputs, outputs, _, call = CASES[case]()
+    call(None)
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outputs]
+    for t in outputs:
+        t.view(torch.uint8).fill_(0xFF)
+    torch.cuda.synchronize()
+    call(handle)
+    torch.cuda.synchronize()
+    assert all(torch.equal(t.view(torch.uint8), w.view(torch.uint8)) for t, w in zip(outputs, want))
