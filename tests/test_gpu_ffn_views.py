@@ -1,5 +1,6 @@
-"""Inputs and outputs that are column ranges of one buffer: the same bytes as
-from tensors of their own, and nothing written beside the output's columns."""
+"""Inputs and outputs that are column ranges of one buffer, or that are each
+other where the header allows it: the same bytes as from tensors of their own,
+and nothing written beside the output's columns."""
 import pytest
 import torch
 
@@ -93,3 +94,30 @@ def test_columns_that_do_overlap_are_refused(shift):
     with pytest.raises(X.XemaError) as e:
         run_norm(buf[:, 128:256], None, None, 1e-6, buf[:, 128 + shift:256 + shift], 128)
     assert e.value.status == X.XEMA_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("rows,dim", [(5, 512), (130, 2064), (3, 16384)])
+@pytest.mark.parametrize("dtype,other", [(BF16, None), (torch.float32, BF16), (F16, F16)])
+@pytest.mark.parametrize("out", [F16, E4M3])
+def test_the_sum_in_place_of_x(rows, dim, dtype, other, out):
+    g = gen(dim)
+    x, resid = normal(g, (rows, dim + 8), 1.0, dtype), normal(g, (rows, dim), 2.0, other) if other else None
+    scales = [torch.empty(rows, device=DEV) if out == E4M3 else None for _ in range(2)]
+    y, y2 = empty(rows, dim, 0, out), empty(rows, dim, 0, out)
+    want, kept = empty(rows, dim, 0, dtype), x.clone()
+    run_norm(kept[:, :dim], resid, None, 1e-6, y, dim, want, scales[0])
+    run_norm(x[:, :dim], resid, None, 1e-6, y2, dim, x[:, :dim], scales[1])
+    assert torch.equal(x[:, :dim], want) and torch.equal(x[:, dim:], kept[:, dim:]) and torch.equal(y.view(torch.uint8), y2.view(torch.uint8))
+    assert out != E4M3 or torch.equal(*scales)
+
+
+@pytest.mark.parametrize("rows,dim", [(5, 512), (5000, 264), (1030, 4096)])
+def test_one_gradient_for_both_paths_in_place(rows, dim):
+    """dy, dsum and dx one tensor: a row is read whole before it is written."""
+    g = gen(rows)
+    s, d, gamma = normal(g, (rows, dim)), normal(g, (rows, dim)), normal(g, (dim,), 0.2, mean=1.0)
+    ws = [torch.empty(X.xema_rmsnorm_bwd_workspace_bytes(rows, dim), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    dg, dx = [torch.empty(dim, device=DEV) for _ in range(2)], empty(rows, dim, 0, BF16)
+    X.xema_op_rmsnorm_bwd(X.rmsnorm_bwd_args(s, 0, rows, dim, gamma, 1e-6, d, 0, dx, 0, dg[0], ws[0], ws[0].numel(), dsum=d, dsum_dtype=0))
+    X.xema_op_rmsnorm_bwd(X.rmsnorm_bwd_args(s, 0, rows, dim, gamma, 1e-6, d, 0, d, 0, dg[1], ws[1], ws[1].numel(), dsum=d, dsum_dtype=0))
+    assert torch.equal(d, dx) and torch.equal(*dg)
