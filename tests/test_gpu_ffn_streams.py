@@ -68,31 +68,36 @@ def test_launches_follow_the_work_of_their_stream(case, how):
     call(None)
     torch.cuda.synchronize()
     want, real = [t.clone() for t in outputs], [t.clone() for t in inputs]
-    # NaN in every type, and rows without an adapter: any launch that does not wait leaves its mark
-    for t in inputs:
-        t.view(torch.uint8).fill_(0xFF) if t.dtype != torch.int32 else t.fill_(-1)
-    for t in (*outputs, *scratch):
-        t.view(torch.uint8).fill_(0xFF)
     long = torch.ones((8192, 8192), device=DEV, dtype=BF16)
-    s, reached = torch.cuda.Stream(), torch.cuda.Event()
     torch.mm(long, long)
-    torch.cuda.synchronize()
-    with torch.cuda.stream(s):
-        for _ in range(200):
-            torch.mm(long, long)
-        for t, r in zip(inputs, real):
-            t.copy_(r)
-        reached.record()
-        if how == "current stream":
-            call(None)
-    if how == "stream argument":
-        call(s)
-    assert not reached.query()                # (or the call would prove nothing)
-    with torch.cuda.stream(s):
-        got = [t.clone() for t in outputs]
-    s.synchronize()
-    for g, w in zip(got, want):
-        assert torch.equal(g.view(torch.uint8), w.view(torch.uint8)), case
+    s = torch.cuda.Stream()
+    for products in (200, 1000, 4000):        # (more where the host was slow, or the call would prove nothing)
+        # NaN in every type, and rows without an adapter: any launch that does not wait leaves its mark
+        for t in inputs:
+            t.view(torch.uint8).fill_(0xFF) if t.dtype != torch.int32 else t.fill_(-1)
+        for t in (*outputs, *scratch):
+            t.view(torch.uint8).fill_(0xFF)
+        torch.cuda.synchronize()
+        reached = torch.cuda.Event()
+        with torch.cuda.stream(s):
+            for _ in range(products):
+                torch.mm(long, long)
+            for t, r in zip(inputs, real):
+                t.copy_(r)
+            reached.record()
+            if how == "current stream":
+                call(None)
+        if how == "stream argument":
+            call(s)
+        running = not reached.query()
+        with torch.cuda.stream(s):
+            got = [t.clone() for t in outputs]
+        s.synchronize()
+        for g, w in zip(got, want):
+            assert torch.equal(g.view(torch.uint8), w.view(torch.uint8)), case
+        if running:
+            return
+    raise AssertionError("the work was always done before the call returned")
 
 
 def test_the_marks_are_seen():
