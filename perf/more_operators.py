@@ -196,7 +196,7 @@ def prepare(case, seed):
         st["y"] = torch.empty((c["rows"], c["out_dim"]), dtype=TYPES[c["y"]], device=DEV)
         if c["kind"] == "linear_train":
             if c["act"] != "none":
-                st["pre"] = torch.empty_like(st["y"])
+                st["pre"] = torch.empty(3 * c["rows"] * c["out_dim"], dtype=torch.uint8, device=DEV)   # z in 24 bits
             for n in ("x", "w") + (("bias",) if c["bias"] else ()):
                 st["d" + n] = torch.empty_like(st[n])
     else:
