@@ -116,7 +116,8 @@ typedef struct {
 XEMA_API int xema_rmsnorm_bwd_workspace_bytes(int64_t rows, int32_t dim, int64_t* bytes);
 XEMA_API int xema_op_rmsnorm_bwd(const xema_rmsnorm_bwd_args* args, void* stream);
 
-typedef enum { XEMA_ACT_SILU = 0, XEMA_ACT_GELU_TANH = 1 } xema_act;
+/* (XEMA_ACT_NONE: the linear layer of xema_cross.h alone) */
+typedef enum { XEMA_ACT_SILU = 0, XEMA_ACT_GELU_TANH = 1, XEMA_ACT_NONE = 2 } xema_act;
 
 /* Gated feed-forward, both projections, the activation and the product in
  * one kernel:

@@ -1,7 +1,6 @@
 """Python binding of libxema, the MI355X (gfx950) DiT block forward.
 
-A thin ctypes layer over the C ABI declared in include/xema.h and
-include/xema_ops.h: the functions keep the C names, take torch tensors (device
+A thin ctypes layer over the C ABI declared in include/: the functions keep the C names, take torch tensors (device
 memory) or plain integers, and raise XemaError on a non-zero status.  Every
 step of the block runs in the library's HIP kernels; torch only provides device
 memory and the stream.  The shared library is loaded from this directory on
@@ -143,7 +142,7 @@ class RmsnormBwdArgs(ctypes.Structure):
                 ("workspace", _P), ("workspace_bytes", _I64)]
 
 
-XEMA_ACT_SILU, XEMA_ACT_GELU_TANH = 0, 1
+XEMA_ACT_SILU, XEMA_ACT_GELU_TANH, XEMA_ACT_NONE = 0, 1, 2
 
 
 class GatedFfnArgs(ctypes.Structure):
@@ -165,6 +164,46 @@ class LoraArgs(ctypes.Structure):
                 ("w", _P), ("bias", _P), ("a", _P), ("b", _P), ("scale", _P), ("rank", _I32), ("n_adapters", _I32),
                 ("row_adapter", _P), ("y", _P), ("y_dtype", _I32), ("ldy", _I64),
                 ("workspace", _P), ("workspace_bytes", _I64)]
+
+
+class LayernormArgs(ctypes.Structure):
+    _fields_ = [("rows", _I64), ("dim", _I32), ("x", _P), ("x_dtype", _I32), ("ldx", _I64),
+                ("resid", _P), ("resid_dtype", _I32), ("ld_resid", _I64), ("sum", _P), ("sum_dtype", _I32), ("ld_sum", _I64),
+                ("gamma", _P), ("beta", _P), ("eps", _F32), ("y", _P), ("y_dtype", _I32), ("ldy", _I64)]
+
+
+class LayernormBwdArgs(ctypes.Structure):
+    _fields_ = [("rows", _I64), ("dim", _I32), ("s", _P), ("s_dtype", _I32), ("ld_s", _I64),
+                ("dy", _P), ("dy_dtype", _I32), ("ld_dy", _I64),
+                ("dsum", _P), ("dsum_dtype", _I32), ("ld_dsum", _I64), ("gamma", _P), ("eps", _F32),
+                ("dx", _P), ("dx_dtype", _I32), ("ld_dx", _I64), ("dgamma", _P), ("dbeta", _P),
+                ("workspace", _P), ("workspace_bytes", _I64)]
+
+
+class LinearArgs(ctypes.Structure):
+    _fields_ = [("dtype", _I32), ("act", _I32), ("rows", _I64), ("dim", _I32), ("out_dim", _I32), ("x", _P), ("ldx", _I64),
+                ("w", _P), ("bias", _P), ("resid", _P), ("resid_dtype", _I32), ("ld_resid", _I64),
+                ("y", _P), ("y_dtype", _I32), ("ldy", _I64), ("pre", _P)]
+
+
+class LinearBwdArgs(ctypes.Structure):
+    _fields_ = [("dtype", _I32), ("act", _I32), ("rows", _I64), ("dim", _I32), ("out_dim", _I32), ("x", _P), ("ldx", _I64),
+                ("w", _P), ("pre", _P), ("dy", _P), ("dy_dtype", _I32), ("ld_dy", _I64), ("dx", _P), ("ld_dx", _I64),
+                ("dw", _P), ("dbias", _P), ("workspace", _P), ("workspace_bytes", _I64)]
+
+
+_CROSS_SIZES = [(n, _I32) for n in ("dtype", "batch", "heads", "kv_heads", "head_dim", "q_len", "kv_len")]
+
+
+class CrossAttnArgs(ctypes.Structure):
+    _fields_ = _CROSS_SIZES + [("q", _P), ("ldq", _I64), ("k", _P), ("ldk", _I64), ("v", _P), ("ldv", _I64), ("kv_lens", _P), ("scale", _F32),
+                               ("o", _P), ("ldo", _I64), ("lse", _P), ("workspace", _P), ("workspace_bytes", _I64)]
+
+
+class CrossAttnBwdArgs(ctypes.Structure):
+    _fields_ = _CROSS_SIZES + [("q", _P), ("ldq", _I64), ("k", _P), ("ldk", _I64), ("v", _P), ("ldv", _I64), ("kv_lens", _P), ("scale", _F32),
+                               ("o", _P), ("ldo", _I64), ("lse", _P), ("dout", _P), ("ld_do", _I64), ("dq", _P), ("ld_dq", _I64),
+                               ("dk", _P), ("ld_dk", _I64), ("dv", _P), ("ld_dv", _I64), ("workspace", _P), ("workspace_bytes", _I64)]
 
 
 _SIGNATURES = {
@@ -236,6 +275,22 @@ _FFN_SIGNATURES = {
 }
 EXPORTED_FFN = tuple(_FFN_SIGNATURES)
 
+# the cross-attention sub-block's operators (include/xema_cross.h)
+_CROSS_SIGNATURES = {
+    "xema_op_layernorm": (ctypes.c_int, [ctypes.POINTER(LayernormArgs), _P]),
+    "xema_layernorm_bwd_workspace_bytes": (ctypes.c_int, [_I64, _I32, ctypes.POINTER(_I64)]),
+    "xema_op_layernorm_bwd": (ctypes.c_int, [ctypes.POINTER(LayernormBwdArgs), _P]),
+    "xema_linear_pre_bytes": (ctypes.c_int, [_I64, _I32, ctypes.POINTER(_I64)]),
+    "xema_op_linear": (ctypes.c_int, [ctypes.POINTER(LinearArgs), _P]),
+    "xema_linear_bwd_workspace_bytes": (ctypes.c_int, [_I64, _I32, _I32, ctypes.POINTER(_I64)]),
+    "xema_op_linear_bwd": (ctypes.c_int, [ctypes.POINTER(LinearBwdArgs), _P]),
+    "xema_cross_attn_workspace_bytes": (ctypes.c_int, [_I32] * 6 + [ctypes.POINTER(_I64)]),
+    "xema_op_cross_attn": (ctypes.c_int, [ctypes.POINTER(CrossAttnArgs), _P]),
+    "xema_cross_attn_bwd_workspace_bytes": (ctypes.c_int, [_I32] * 6 + [ctypes.POINTER(_I64)]),
+    "xema_op_cross_attn_bwd": (ctypes.c_int, [ctypes.POINTER(CrossAttnBwdArgs), _P]),
+}
+EXPORTED_CROSS = tuple(_CROSS_SIGNATURES)
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -247,7 +302,7 @@ def lib() -> ctypes.CDLL:
             raise RuntimeError(f"{LIB_PATH} is missing: build it with "
                                "`python -m paper_2607_11136_amd.build` (needs hipcc)")
         l = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in {**_SIGNATURES, **_FFN_SIGNATURES}.items():
+        for name, (res, args) in {**_SIGNATURES, **_FFN_SIGNATURES, **_CROSS_SIGNATURES}.items():
             f = getattr(l, name)
             f.restype = res
             f.argtypes = args
@@ -672,3 +727,112 @@ def xema_lora_workspace_bytes(rows: int, rank: int) -> int:
 
 def xema_op_lora_linear(args: LoraArgs, stream=None) -> None:
     _check(lib().xema_op_lora_linear(ctypes.byref(args), _stream(stream)), "xema_op_lora_linear")
+
+
+# -- the cross-attention sub-block's operators (include/xema_cross.h) ------------------------------
+
+
+def layernorm_args(x, x_dtype: int, rows: int, dim: int, gamma, beta, eps: float, y, y_dtype: int, resid=None,
+                   resid_dtype: int = XEMA_BF16, sum=None, sum_dtype: int = XEMA_BF16, ldx: int = 0, ld_resid: int = 0, ld_sum: int = 0,
+                   ldy: int = 0) -> LayernormArgs:
+    """Leading dimensions of 0 stand for dim."""
+    return LayernormArgs(rows, dim, _ptr(x), x_dtype, ldx or dim, _ptr(resid), resid_dtype, ld_resid or dim, _ptr(sum), sum_dtype,
+                         ld_sum or dim, _ptr(gamma), _ptr(beta), eps, _ptr(y), y_dtype, ldy or dim)
+
+
+def xema_op_layernorm(args: LayernormArgs, stream=None) -> None:
+    _check(lib().xema_op_layernorm(ctypes.byref(args), _stream(stream)), "xema_op_layernorm")
+
+
+def layernorm_bwd_args(s, s_dtype: int, rows: int, dim: int, gamma, eps: float, dy, dy_dtype: int, dx, dx_dtype: int, dgamma=None,
+                       dbeta=None, workspace=None, workspace_bytes: int = 0, dsum=None, dsum_dtype: int = XEMA_BF16, ld_s: int = 0,
+                       ld_dy: int = 0, ld_dsum: int = 0, ld_dx: int = 0) -> LayernormBwdArgs:
+    """Leading dimensions of 0 stand for dim."""
+    return LayernormBwdArgs(rows, dim, _ptr(s), s_dtype, ld_s or dim, _ptr(dy), dy_dtype, ld_dy or dim, _ptr(dsum), dsum_dtype,
+                            ld_dsum or dim, _ptr(gamma), eps, _ptr(dx), dx_dtype, ld_dx or dim, _ptr(dgamma), _ptr(dbeta), _ptr(workspace),
+                            int(workspace_bytes))
+
+
+def xema_layernorm_bwd_workspace_bytes(rows: int, dim: int) -> int:
+    n = _I64()
+    _check(lib().xema_layernorm_bwd_workspace_bytes(rows, dim, ctypes.byref(n)), "xema_layernorm_bwd_workspace_bytes")
+    return n.value
+
+
+def xema_op_layernorm_bwd(args: LayernormBwdArgs, stream=None) -> None:
+    _check(lib().xema_op_layernorm_bwd(ctypes.byref(args), _stream(stream)), "xema_op_layernorm_bwd")
+
+
+def linear_args(dtype: int, x, rows: int, dim: int, w, out_dim: int, bias, act: int, y, y_dtype: int, resid=None,
+                resid_dtype: int = XEMA_BF16, pre=None, ldx: int = 0, ld_resid: int = 0, ldy: int = 0) -> LinearArgs:
+    """Leading dimensions of 0 stand for the width."""
+    return LinearArgs(dtype, act, rows, dim, out_dim, _ptr(x), ldx or dim, _ptr(w), _ptr(bias), _ptr(resid), resid_dtype, ld_resid or out_dim,
+                      _ptr(y), y_dtype, ldy or out_dim, _ptr(pre))
+
+
+def xema_linear_pre_bytes(rows: int, out_dim: int) -> int:
+    n = _I64()
+    _check(lib().xema_linear_pre_bytes(rows, out_dim, ctypes.byref(n)), "xema_linear_pre_bytes")
+    return n.value
+
+
+def xema_op_linear(args: LinearArgs, stream=None) -> None:
+    _check(lib().xema_op_linear(ctypes.byref(args), _stream(stream)), "xema_op_linear")
+
+
+def linear_bwd_args(dtype: int, act: int, x, rows: int, dim: int, w, out_dim: int, pre, dy, dy_dtype: int, dx, dw, dbias, workspace,
+                    workspace_bytes: int, ldx: int = 0, ld_dy: int = 0, ld_dx: int = 0) -> LinearBwdArgs:
+    """Leading dimensions of 0 stand for the width."""
+    return LinearBwdArgs(dtype, act, rows, dim, out_dim, _ptr(x), ldx or dim, _ptr(w), _ptr(pre), _ptr(dy), dy_dtype, ld_dy or out_dim,
+                         _ptr(dx), ld_dx or dim, _ptr(dw), _ptr(dbias), _ptr(workspace), int(workspace_bytes))
+
+
+def xema_linear_bwd_workspace_bytes(rows: int, dim: int, out_dim: int) -> int:
+    n = _I64()
+    _check(lib().xema_linear_bwd_workspace_bytes(rows, dim, out_dim, ctypes.byref(n)), "xema_linear_bwd_workspace_bytes")
+    return n.value
+
+
+def xema_op_linear_bwd(args: LinearBwdArgs, stream=None) -> None:
+    _check(lib().xema_op_linear_bwd(ctypes.byref(args), _stream(stream)), "xema_op_linear_bwd")
+
+
+def cross_attn_args(dtype: int, batch: int, heads: int, kv_heads: int, head_dim: int, q_len: int, kv_len: int, q, k, v, scale: float, o,
+                    workspace=None, workspace_bytes: int = 0, lse=None, kv_lens=None, ldq: int = 0, ldk: int = 0, ldv: int = 0,
+                    ldo: int = 0) -> CrossAttnArgs:
+    """Leading dimensions of 0 stand for the width."""
+    nq, nk = heads * head_dim, kv_heads * head_dim
+    return CrossAttnArgs(dtype, batch, heads, kv_heads, head_dim, q_len, kv_len, _ptr(q), ldq or nq, _ptr(k), ldk or nk, _ptr(v), ldv or nk,
+                         _ptr(kv_lens), scale, _ptr(o), ldo or nq, _ptr(lse), _ptr(workspace), int(workspace_bytes))
+
+
+def xema_cross_attn_workspace_bytes(batch: int, heads: int, kv_heads: int, head_dim: int, q_len: int, kv_len: int) -> int:
+    n = _I64()
+    _check(lib().xema_cross_attn_workspace_bytes(batch, heads, kv_heads, head_dim, q_len, kv_len, ctypes.byref(n)),
+           "xema_cross_attn_workspace_bytes")
+    return n.value
+
+
+def xema_op_cross_attn(args: CrossAttnArgs, stream=None) -> None:
+    _check(lib().xema_op_cross_attn(ctypes.byref(args), _stream(stream)), "xema_op_cross_attn")
+
+
+def cross_attn_bwd_args(dtype: int, batch: int, heads: int, kv_heads: int, head_dim: int, q_len: int, kv_len: int, q, k, v, scale: float, o,
+                        lse, dout, dq, dk, dv, workspace, workspace_bytes: int, kv_lens=None, ldq: int = 0, ldk: int = 0, ldv: int = 0,
+                        ldo: int = 0, ld_do: int = 0, ld_dq: int = 0, ld_dk: int = 0, ld_dv: int = 0) -> CrossAttnBwdArgs:
+    """Leading dimensions of 0 stand for the width."""
+    nq, nk = heads * head_dim, kv_heads * head_dim
+    return CrossAttnBwdArgs(dtype, batch, heads, kv_heads, head_dim, q_len, kv_len, _ptr(q), ldq or nq, _ptr(k), ldk or nk, _ptr(v), ldv or nk,
+                            _ptr(kv_lens), scale, _ptr(o), ldo or nq, _ptr(lse), _ptr(dout), ld_do or nq, _ptr(dq), ld_dq or nq, _ptr(dk),
+                            ld_dk or nk, _ptr(dv), ld_dv or nk, _ptr(workspace), int(workspace_bytes))
+
+
+def xema_cross_attn_bwd_workspace_bytes(batch: int, heads: int, kv_heads: int, head_dim: int, q_len: int, kv_len: int) -> int:
+    n = _I64()
+    _check(lib().xema_cross_attn_bwd_workspace_bytes(batch, heads, kv_heads, head_dim, q_len, kv_len, ctypes.byref(n)),
+           "xema_cross_attn_bwd_workspace_bytes")
+    return n.value
+
+
+def xema_op_cross_attn_bwd(args: CrossAttnBwdArgs, stream=None) -> None:
+    _check(lib().xema_op_cross_attn_bwd(ctypes.byref(args), _stream(stream)), "xema_op_cross_attn_bwd")

@@ -1,0 +1,407 @@
+// Attention to an encoder's states (xema_cross.h), forward, on gfx950 MFMA:
+// one pass over the states with a running reference maximum and sum.
+//
+// k_cross: a wave holds QB blocks of 32 queries of one head; the workgroup's
+// four waves share tiles of 64 states, two stages in LDS.  S^T = K Q^T leaves a
+// lane with one query's scores, whose exponentials feed O^T = V^T P^T from their
+// registers (cross_tile.h).  The reference maximum moves only when a tile's sum
+// of exponentials passes PMAX, so the common path takes no maximum: P stays
+// below PMAX, and the largest weight is at least 1 against the sum.
+//
+// k_cross_few: single tokens.  The tokens of all heads that share a state's head
+// are one block of up to 32 queries, and the workgroup's waves take tiles of 32
+// states in turn, each with stages of its own and no barrier, so that the states
+// stream from HBM; the waves' sums meet in LDS at the end.
+//
+// Where a call has too few workgroups for the CUs, its states are split into
+// parts, each workgroup's sums kept in fp32 with their maximum, and k_cross_join
+// joins them.
+#include "cross.h"
+#include "cross_tile.h"
+
+namespace xema {
+
+namespace {
+
+constexpr int KT = 64;                 // states per tile
+constexpr int CROSS_WAVES = 4;
+constexpr float PMAX = 4096.f;         // (fp16 P stays finite; 2^12 beside sums in fp32 loses nothing)
+constexpr float LOWEST = -1e30f;       // a reference below every score, so that -infinity less it stays one
+
+struct CrossParams {
+  const void *q, *k, *v;
+  void* o;
+  float* lse;
+  const int32_t* kv_lens;
+  float* part_o;                       // [parts][rows][head_dim]
+  float2* part_ml;                     // [parts][rows]: maximum (log2 units), sum
+  int64_t ldq, ldk, ldv, ldo;
+  int64_t rows;                        // batch * heads * q_len
+  int batch, heads, kv_heads, head_dim, q_len, kv_len, parts, blocks;     // blocks of queries of a head
+  float c;                             // scale * log2(e)
+};
+
+// The running softmax of a lane's column, and its sum over V.
+template <int ND>
+struct Column {
+  float m, l;                          // reference (log2 units); this lane's share of the sum
+  f32x16 o[ND];
+  __device__ __forceinline__ void init() {
+    m = LOWEST;
+    l = 0.f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
+  }
+  // scores (of NB blocks of 32 states) to weights 2^(c s - m)
+  template <int NB>
+  __device__ __forceinline__ void weigh(f32x16 (&s)[NB], float c, bool first) {
+    f32x16 p[NB];
+    float sum = first ? 0.f : exps<NB>(s, p, c);
+    const bool grow = first || !(pair_max(sum) <= PMAX);
+    if (__builtin_amdgcn_ballot_w64(grow)) {
+      float top = s[0][0] * c;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r] * c);
+      top = fmaxf(pair_max(top), m);
+      const float to = grow ? top : m, f = __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= f;
+      sum = exps<NB>(s, p, c);
+    }
+    l += sum;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) s[b] = p[b];
+  }
+  template <int NB>
+  __device__ __forceinline__ float exps(const f32x16 (&s)[NB], f32x16 (&p)[NB], float c) const {
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        p[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, -m));
+        part[r & 3] += p[b][r];
+      }
+    return (part[0] + part[1]) + (part[2] + part[3]);
+  }
+};
+
+// Scores of states at or past `left` become -infinity: block b's register r is state 32 b + 8 (r / 4) + 4 hi + r % 4.
+template <int NB>
+__device__ __forceinline__ void mask_from(f32x16 (&s)[NB], int left, int hi) {
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (32 * b + 8 * (r >> 2) + 4 * hi + (r & 3) >= left) s[b][r] = -INFINITY;
+}
+
+// What a lane's column leaves: o and lse, or its part of them.  `row` is the
+// column's among all (batch, head, token); o_at the address of its output.
+template <typename T, int ND>
+__device__ __forceinline__ void finish(const CrossParams& p, const Column<ND>& col, float l, int64_t row, T* o_at, int part, int hi, bool valid) {
+  if (p.parts > 1) {
+    const int64_t at = part * p.rows + row;
+    store_column_f32<ND>(p.part_o + at * p.head_dim, p.head_dim, col.o, 1.f, hi, valid);
+    if (valid && !hi) p.part_ml[at] = float2{col.m, l};
+    return;
+  }
+  store_column<T, ND>(o_at, p.head_dim, col.o, l == 0.f ? 0.f : 1.f / l, hi, valid);
+  // (v_log_f32 is log2)
+  if (p.lse && valid && !hi) p.lse[row] = l == 0.f ? -INFINITY : (col.m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+template <typename T, int HDP, int QB>
+__global__ __launch_bounds__(CROSS_WAVES * 64, 2) void k_cross(CrossParams p) {
+  typedef Rows<HDP> R;
+  typedef typename Mfma<T>::frag frag;
+  constexpr int KK = R::KK, ND = R::ND, TILE = KT * R::RB;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2 * TILE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c32 = lane & 31, hi = lane >> 5;
+  // workgroup -> (batch, head, part, block of queries)
+  const int t = xcd_order((int)blockIdx.x, (int)gridDim.x);
+  const int block = t % p.blocks, part = t / p.blocks % p.parts, bh = t / p.blocks / p.parts;
+  const int b = bh / p.heads, h = bh - b * p.heads, kvh = h / (p.heads / p.kv_heads);
+  const int n = states_of(p.kv_lens, b, p.kv_len), tiles = (n + KT - 1) / KT;
+  int first, count;
+  part_of(tiles, part, p.parts, &first, &count);
+
+  const int64_t kv_row = (int64_t)b * p.kv_len + (int64_t)first * KT;
+  const uint8_t* kb = (const uint8_t*)((const T*)p.k + kv_row * p.ldk + kvh * p.head_dim);
+  const uint8_t* vb = (const uint8_t*)((const T*)p.v + kv_row * p.ldv + kvh * p.head_dim);
+  const uint32_t ldk = (uint32_t)p.ldk * 2, ldv = (uint32_t)p.ldv * 2;
+  TileLoads<HDP, KT, CROSS_WAVES> lk, lv;
+  lk.init(ldk, p.head_dim, wave, lane);
+  lv.init(ldv, p.head_dim, wave, lane);
+  int left = n - first * KT;                     // states from the next tile to load on
+  auto issue = [&](int stage) {
+    lk.issue(kb, ldk, left, smem[stage], wave);
+    lv.issue(vb, ldv, left, smem[stage] + TILE, wave);
+    kb += (int64_t)KT * ldk;
+    vb += (int64_t)KT * ldv;
+    left -= KT;
+  };
+  if (count > 0) issue(0);
+
+  // (queries past the last repeat it and are not stored)
+  const int q0 = (block * CROSS_WAVES + wave) * QB * 32;
+  const T* const qh = (const T*)p.q + (int64_t)b * p.q_len * p.ldq + (int64_t)h * p.head_dim;
+  frag qf[QB][KK];
+  Column<ND> col[QB];
+#pragma unroll
+  for (int c = 0; c < QB; ++c) {
+    load_column<T, HDP>(qh + (int64_t)min(q0 + 32 * c + c32, p.q_len - 1) * p.ldq, p.head_dim, hi, qf[c]);
+    col[c].init();
+  }
+  AlongRows<T, HDP> rk;
+  AcrossRows<T, HDP> rv;
+  rk.init(lane);
+  rv.init(lane);
+
+  for (int i = 0; i < count; ++i) {
+    // tile i has landed (this wave's part: vmcnt; the others': the barrier), and
+    // every wave has read tile i - 1, whose stage tile i + 1 takes
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    __syncthreads();
+    if (i + 1 < count) issue((i + 1) & 1);
+    const uint8_t *ks = smem[i & 1], *vs = ks + TILE;
+    f32x16 s[QB][2];
+#pragma unroll
+    for (int kb2 = 0; kb2 < 2; ++kb2)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const frag f = rk.read(ks, 32 * kb2, kk, hi);
+#pragma unroll
+        for (int c = 0; c < QB; ++c) s[c][kb2] = Mfma<T>::run(f, qf[c][kk], kk ? s[c][kb2] : f32x16{});
+      }
+    const int here = n - (first + i) * KT;
+#pragma unroll
+    for (int c = 0; c < QB; ++c) {
+      if (here < KT) mask_from<2>(s[c], here, hi);
+      col[c].template weigh<2>(s[c], p.c, i == 0);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      frag pf[QB];
+#pragma unroll
+      for (int c = 0; c < QB; ++c) pf[c] = pack8<T>(s[c][u >> 1], u & 1);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const frag f = rv.read(vs, 16 * u, d);
+#pragma unroll
+        for (int c = 0; c < QB; ++c) col[c].o[d] = Mfma<T>::run(f, pf[c], col[c].o[d]);
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < QB; ++c) {
+    const int q = q0 + 32 * c + c32;
+    const bool valid = q < p.q_len;
+    const int64_t token = valid ? q : 0;
+    finish<T, ND>(p, col[c], pair_sum(col[c].l), ((int64_t)b * p.heads + h) * p.q_len + token,
+                  (T*)p.o + ((int64_t)b * p.q_len + token) * p.ldo + (int64_t)h * p.head_dim, part, hi, valid);
+  }
+}
+
+constexpr int FT = 32;                 // states per tile of a wave of k_cross_few
+
+template <typename T, int HDP>
+__global__ __launch_bounds__(CROSS_WAVES * 64) void k_cross_few(CrossParams p) {
+  typedef Rows<HDP> R;
+  typedef typename Mfma<T>::frag frag;
+  constexpr int KK = R::KK, ND = R::ND, TILE = FT * R::RB, STAGE = 2 * TILE, LOADS = 2 * TileLoads<HDP, FT, 1>::LOADS;
+  constexpr int ROW = HDP + 4;                   // fp32 of a column where the waves' sums meet (padded against bank conflicts)
+  constexpr int LDS = CROSS_WAVES * (2 * STAGE > 32 * ROW * 4 ? 2 * STAGE : 32 * ROW * 4);
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS];
+  __shared__ float2 ml[CROSS_WAVES][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c32 = lane & 31, hi = lane >> 5;
+  // workgroup -> (batch, state head, block of queries, part)
+  const int t = (int)blockIdx.x;
+  const int part = t % p.parts, block = t / p.parts % p.blocks, bk = t / p.parts / p.blocks;
+  const int b = bk / p.kv_heads, kvh = bk - b * p.kv_heads, group = p.heads / p.kv_heads;
+  const int n = states_of(p.kv_lens, b, p.kv_len), tiles = (n + FT - 1) / FT;
+  int first, count;
+  part_of(tiles, part, p.parts, &first, &count);
+  // this wave's tiles: first + wave, first + wave + CROSS_WAVES, ...
+  const int mine = (count - wave + CROSS_WAVES - 1) / CROSS_WAVES;
+
+  uint8_t* const stages = smem + wave * 2 * STAGE;
+  const uint32_t ldk = (uint32_t)p.ldk * 2, ldv = (uint32_t)p.ldv * 2;
+  const int64_t kv_row = (int64_t)b * p.kv_len;
+  const T* const kh = (const T*)p.k + kv_row * p.ldk + kvh * p.head_dim;
+  const T* const vh = (const T*)p.v + kv_row * p.ldv + kvh * p.head_dim;
+  TileLoads<HDP, FT, 1> lk, lv;
+  lk.init(ldk, p.head_dim, 0, lane);
+  lv.init(ldv, p.head_dim, 0, lane);
+  // (tiles past the wave's last have no states: their loads read nothing)
+  auto issue = [&](int i) {
+    const int64_t at = i < mine ? (int64_t)(first + wave + i * CROSS_WAVES) * FT : n;
+    uint8_t* const st = stages + (i & 1) * STAGE;
+    lk.issue((const uint8_t*)(kh + at * p.ldk), ldk, n - (int)at, st, 0);
+    lv.issue((const uint8_t*)(vh + at * p.ldv), ldv, n - (int)at, st + TILE, 0);
+  };
+  issue(0);
+  issue(1);
+
+  // query r of the block: token r / group of the head kvh * group + r % group
+  const int r0 = block * 32 + c32, rows = p.q_len * group;
+  const int rq = min(r0, rows - 1), token = rq / group, h = kvh * group + rq - token * group;
+  frag qf[KK];
+  load_column<T, HDP>((const T*)p.q + ((int64_t)b * p.q_len + token) * p.ldq + (int64_t)h * p.head_dim, p.head_dim, hi, qf);
+  Column<ND> col;
+  col.init();
+  AlongRows<T, HDP> rk;
+  AcrossRows<T, HDP> rv;
+  rk.init(lane);
+  rv.init(lane);
+  for (int i = 0; i < mine; ++i) {
+    // the wave's tile i has landed, tile i + 1 may be in flight
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(LOADS));
+    asm volatile("" ::: "memory");
+    const uint8_t *ks = stages + (i & 1) * STAGE, *vs = ks + TILE;
+    f32x16 s[1];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) s[0] = Mfma<T>::run(rk.read(ks, 0, kk, hi), qf[kk], kk ? s[0] : f32x16{});
+    const int here = n - (first + wave + i * CROSS_WAVES) * FT;
+    if (here < FT) mask_from<1>(s, here, hi);
+    col.template weigh<1>(s, p.c, i == 0);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const frag pf = pack8<T>(s[0], u);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) col.o[d] = Mfma<T>::run(rv.read(vs, 16 * u, d), pf, col.o[d]);
+    }
+    // its reads are done: tile i + 2 takes its stage
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xc07f);          // lgkmcnt(0)
+    issue(i + 2);
+  }
+  // the loads that ran ahead write to LDS: let them finish, then the waves' sums meet
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+  const float l = pair_sum(col.l);
+  if (!hi) ml[wave][c32] = float2{col.m, l};
+  __syncthreads();
+  float* const sums = (float*)smem;
+  float top = LOWEST;
+#pragma unroll
+  for (int w = 0; w < CROSS_WAVES; ++w) top = fmaxf(top, ml[w][c32].x);
+  store_column_f32<ND>(sums + (wave * 32 + c32) * ROW, HDP, col.o, __builtin_amdgcn_exp2f(col.m - top), hi, true);
+  __syncthreads();
+  // eight threads a query, four columns each at a time
+  const int q = (int)threadIdx.x / 8, at = block * 32 + q;
+  if (at >= rows) return;
+  float m = LOWEST, sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < CROSS_WAVES; ++w) m = fmaxf(m, ml[w][q].x);
+#pragma unroll
+  for (int w = 0; w < CROSS_WAVES; ++w) sum += ml[w][q].y * __builtin_amdgcn_exp2f(ml[w][q].x - m);
+  const int tq = at / group, hq = kvh * group + at - tq * group;
+  const int64_t row = ((int64_t)b * p.heads + hq) * p.q_len + tq, prow = part * p.rows + row;
+  T* const orow = (T*)p.o + ((int64_t)b * p.q_len + tq) * p.ldo + (int64_t)hq * p.head_dim;
+  const float f = p.parts > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+  for (int e = ((int)threadIdx.x & 7) * 4; e < p.head_dim; e += 32) {
+    f32x4 v = *reinterpret_cast<const f32x4*>(sums + q * ROW + e);
+#pragma unroll
+    for (int w = 1; w < CROSS_WAVES; ++w) v += *reinterpret_cast<const f32x4*>(sums + (w * 32 + q) * ROW + e);
+    if (p.parts > 1) {
+      *reinterpret_cast<f32x4*>(p.part_o + prow * p.head_dim + e) = v;
+    } else {
+      typedef T t4 __attribute__((ext_vector_type(4)));
+      t4 o;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[x] = (T)(v[x] * f);
+      *reinterpret_cast<t4*>(orow + e) = o;
+    }
+  }
+  if (threadIdx.x & 7) return;
+  if (p.parts > 1) p.part_ml[prow] = float2{m, sum};
+  else if (p.lse) p.lse[row] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+}
+
+// The parts of a (batch, head, token)'s sums, joined in order: 16 threads a row, eight columns each.
+template <typename T>
+__global__ __launch_bounds__(256) void k_cross_join(CrossParams p) {
+  const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+  if (row >= p.rows) return;
+  float m = LOWEST, sum = 0.f;
+  for (int i = 0; i < p.parts; ++i) m = fmaxf(m, p.part_ml[i * p.rows + row].x);
+  for (int i = 0; i < p.parts; ++i) {
+    const float2 ml = p.part_ml[i * p.rows + row];
+    sum += ml.y * __builtin_amdgcn_exp2f(ml.x - m);
+  }
+  const int64_t bh = row / p.q_len, token = row - bh * p.q_len, b = bh / p.heads, h = bh - b * p.heads;
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
+  const int e = ((int)threadIdx.x & 15) * 8;
+  if (e == 0 && p.lse) p.lse[row] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  if (e >= p.head_dim) return;
+  f32x4 v[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll 4
+  for (int i = 0; i < p.parts; ++i) {
+    const float w = __builtin_amdgcn_exp2f(p.part_ml[i * p.rows + row].x - m);
+    const f32x4* const at = reinterpret_cast<const f32x4*>(p.part_o + (i * p.rows + row) * p.head_dim + e);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) v[x] += at[x] * w;
+  }
+  typedef T t8 __attribute__((ext_vector_type(8)));
+  t8 o;
+#pragma unroll
+  for (int x = 0; x < 8; ++x) o[x] = (T)(v[x / 4][x % 4] * f);
+  *reinterpret_cast<t8*>((T*)p.o + (b * p.q_len + token) * p.ldo + h * p.head_dim + e) = o;
+}
+
+template <typename T, int HDP>
+hipError_t run_cross(CrossParams p, const CrossPick& pick, hipStream_t s) {
+  constexpr int QB = HDP <= 64 ? 2 : 1;
+  p.blocks = pick.blocks;
+  const unsigned wgs = (unsigned)((int64_t)p.batch * (pick.few ? p.kv_heads : p.heads) * pick.blocks * pick.parts);
+  if (pick.few) hipLaunchKernelGGL((k_cross_few<T, HDP>), dim3(wgs), dim3(CROSS_WAVES * 64), 0, s, p);
+  else hipLaunchKernelGGL((k_cross<T, HDP, QB>), dim3(wgs), dim3(CROSS_WAVES * 64), 0, s, p);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t cross_t(const CrossParams& p, const CrossPick& pick, hipStream_t s) {
+  hipError_t e;
+  if (p.head_dim <= 32) e = run_cross<T, 32>(p, pick, s);
+  else if (p.head_dim <= 64) e = run_cross<T, 64>(p, pick, s);
+  else if (p.head_dim <= 96) e = run_cross<T, 96>(p, pick, s);
+  else e = run_cross<T, 128>(p, pick, s);
+  if (e != hipSuccess || p.parts == 1) return e;
+  hipLaunchKernelGGL((k_cross_join<T>), dim3((unsigned)((p.rows + 15) / 16)), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
+CrossPick pick_of(const CrossShape& c) { return pick_cross(c.batch, c.heads, c.kv_heads, c.head_dim, c.q_len, c.kv_len); }
+
+}  // namespace
+
+int64_t cross_attn_workspace(const CrossShape& c) {
+  const int64_t rows = (int64_t)c.batch * c.heads * c.q_len;
+  const int parts = rows ? pick_of(c).parts : 1;
+  return parts > 1 ? parts * rows * (c.head_dim * 4 + 8) : 0;
+}
+
+hipError_t launch_cross_attn(const xema_cross_attn_args& a, hipStream_t s) {
+  const CrossPick pick = pick_of({a.batch, a.heads, a.kv_heads, a.head_dim, a.q_len, a.kv_len});
+  const int64_t rows = (int64_t)a.batch * a.heads * a.q_len;
+  float* const part_o = (float*)a.workspace;
+  const CrossParams p{a.q, a.k, a.v, a.o, a.lse, a.kv_lens, part_o, (float2*)(part_o + pick.parts * rows * a.head_dim),
+                      a.ldq, a.ldk, a.ldv, a.ldo, rows, a.batch, a.heads, a.kv_heads, a.head_dim, a.q_len, a.kv_len, pick.parts, 0,
+                      a.scale * LOG2E_F};
+  return a.dtype == XEMA_BF16 ? cross_t<bf16>(p, pick, s) : cross_t<f16>(p, pick, s);
+}
+
+}  // namespace xema

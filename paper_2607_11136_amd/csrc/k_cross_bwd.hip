@@ -1,0 +1,358 @@
+// Gradient of the attention to an encoder's states (xema_cross.h) on gfx950
+// MFMA, in two passes that each form the scores again from q, k and lse:
+//
+// k_cross_dq: a wave holds 32 queries of one head (q, dout and dq in registers),
+// the workgroup's four waves share tiles of 64 states.  It forms D from dout and
+// o first, and leaves lse and D for the other pass.
+//
+// k_cross_dkv: a wave holds 32 states (k, v, dk and dv in registers), the
+// workgroup's four waves share tiles of 64 tokens, those of all heads that share
+// the states' head one after another, so that their sum needs no exchange.  An
+// encoder has few states beside the tokens: the tokens are split over workgroups,
+// whose sums k_cross_sums adds in order.
+//
+// Products are formed transposed (cross_tile.h): a column's scores and their
+// gradients feed the last product from their registers.
+#include "cross.h"
+#include "cross_tile.h"
+
+namespace xema {
+
+namespace {
+
+constexpr int KT = 64;                 // states (dq) or tokens (dk, dv) per tile
+constexpr int BWD_WAVES = 4;
+
+// fp16 keeps p as 2^14 p: its bits last to p = 2^-28, and 2^14 (1 + rounding) is in range.
+template <typename T>
+constexpr float P_EXP = std::is_same_v<T, f16> ? 14.f : 0.f;
+template <typename T>
+constexpr float P_UNIT = std::is_same_v<T, f16> ? 0x1p-14f : 1.f;
+
+struct CrossBwd {
+  const void *q, *k, *v, *o, *dout;
+  const float* lse;
+  const int32_t* kv_lens;
+  void *dq, *dk, *dv;
+  float *stat_l, *stat_d;              // [batch, heads, q_len]: lse in log2 units less P_EXP (+infinity: no states), P_UNIT D
+  float* dq_parts;                     // [parts][batch * q_len][heads * head_dim]
+  float* dkv_parts;                    // [parts][dk, dv][batch * kv_len][kv_heads * head_dim]
+  int64_t ldq, ldk, ldv, ldo, ld_do, ld_dq, ld_dk, ld_dv;
+  int batch, heads, kv_heads, head_dim, q_len, kv_len, q_parts, kv_parts;
+  float c, scale;                      // scale * log2(e), scale
+};
+
+template <typename T, int HDP>
+__global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
+  typedef Rows<HDP> R;
+  typedef typename Mfma<T>::frag frag;
+  constexpr int KK = R::KK, ND = R::ND, TILE = KT * R::RB;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2 * TILE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c32 = lane & 31, hi = lane >> 5;
+  const int blocks = (p.q_len + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES);
+  const int t = xcd_order((int)blockIdx.x, (int)gridDim.x);
+  const int block = t % blocks, part = t / blocks % p.q_parts, bh = t / blocks / p.q_parts;
+  const int b = bh / p.heads, h = bh - b * p.heads, kvh = h / (p.heads / p.kv_heads);
+  const int n = states_of(p.kv_lens, b, p.kv_len), tiles = (n + KT - 1) / KT;
+  int first, count;
+  part_of(tiles, part, p.q_parts, &first, &count);
+  if (!p.dq) count = 0;
+
+  const int64_t kv_row = (int64_t)b * p.kv_len + (int64_t)first * KT;
+  const uint8_t* kb = (const uint8_t*)((const T*)p.k + kv_row * p.ldk + kvh * p.head_dim);
+  const uint8_t* vb = (const uint8_t*)((const T*)p.v + kv_row * p.ldv + kvh * p.head_dim);
+  const uint32_t ldk = (uint32_t)p.ldk * 2, ldv = (uint32_t)p.ldv * 2;
+  TileLoads<HDP, KT, BWD_WAVES> lk, lv;
+  lk.init(ldk, p.head_dim, wave, lane);
+  lv.init(ldv, p.head_dim, wave, lane);
+  int left = n - first * KT;
+  auto issue = [&](int stage) {
+    lk.issue(kb, ldk, left, smem[stage], wave);
+    lv.issue(vb, ldv, left, smem[stage] + TILE, wave);
+    kb += (int64_t)KT * ldk;
+    vb += (int64_t)KT * ldv;
+    left -= KT;
+  };
+  if (count > 0) issue(0);
+
+  const int q = (block * BWD_WAVES + wave) * 32 + c32;
+  const bool valid = q < p.q_len;
+  const int64_t token = min(q, p.q_len - 1), tok_row = (int64_t)b * p.q_len + token, row = ((int64_t)b * p.heads + h) * p.q_len + token;
+  const int64_t at = (int64_t)h * p.head_dim;
+  frag qf[KK], df[KK];
+  load_column<T, HDP>((const T*)p.q + tok_row * p.ldq + at, p.head_dim, hi, qf);
+  load_column<T, HDP>((const T*)p.dout + tok_row * p.ld_do + at, p.head_dim, hi, df);
+  float D = 0.f;
+  {
+    frag of[KK];
+    load_column<T, HDP>((const T*)p.o + tok_row * p.ldo + at, p.head_dim, hi, of);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) D = fmaf((float)df[kk][e], (float)of[kk][e], D);
+  }
+  D = pair_sum(D);
+  const float lse = p.lse[row];
+  const float L = lse == -INFINITY ? INFINITY : lse * LOG2E_F;
+  if (part == 0 && valid && !hi) {
+    p.stat_l[row] = L - P_EXP<T>;
+    p.stat_d[row] = D * P_UNIT<T>;
+  }
+  if (!p.dq) return;
+
+  f32x16 acc[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
+  AlongRows<T, HDP> ra;
+  AcrossRows<T, HDP> rx;
+  ra.init(lane);
+  rx.init(lane);
+  for (int i = 0; i < count; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    __syncthreads();
+    if (i + 1 < count) issue((i + 1) & 1);
+    const uint8_t *ks = smem[i & 1], *vs = ks + TILE;
+    const int here = n - (first + i) * KT;
+#pragma unroll
+    for (int blk = 0; blk < 2; ++blk) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) s = Mfma<T>::run(ra.read(ks, 32 * blk, kk, hi), qf[kk], kk ? s : f32x16{});
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) dp = Mfma<T>::run(ra.read(vs, 32 * blk, kk, hi), df[kk], kk ? dp : f32x16{});
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.c, -L)) * (dp[r] - D);
+      if (here < KT) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * blk + 8 * (r >> 2) + 4 * hi + (r & 3) >= here) s[r] = 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const frag f = pack8<T>(s, u);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[d] = Mfma<T>::run(rx.read(ks, 32 * blk + 16 * u, d), f, acc[d]);
+      }
+    }
+  }
+  if (p.q_parts > 1)
+    store_column_f32<ND>(p.dq_parts + (part * (int64_t)p.batch * p.q_len + tok_row) * p.heads * p.head_dim + at, p.head_dim, acc, p.scale, hi, valid);
+  else
+    store_column<T, ND>((T*)p.dq + tok_row * p.ld_dq + at, p.head_dim, acc, p.scale, hi, valid);
+}
+
+template <typename T, int HDP>
+__global__ __launch_bounds__(BWD_WAVES * 64, 1) void k_cross_dkv(CrossBwd p) {
+  typedef Rows<HDP> R;
+  typedef typename Mfma<T>::frag frag;
+  constexpr int KK = R::KK, ND = R::ND, TILE = KT * R::RB;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2 * TILE];
+  __shared__ __attribute__((aligned(16))) float stats[2][2][KT];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c32 = lane & 31, hi = lane >> 5;
+  const int blocks = (p.kv_len + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES);
+  const int t = xcd_order((int)blockIdx.x, (int)gridDim.x);
+  const int block = t % blocks, part = t / blocks % p.kv_parts, bk = t / blocks / p.kv_parts;
+  const int b = bk / p.kv_heads, kvh = bk - b * p.kv_heads, group = p.heads / p.kv_heads;
+  const int n = states_of(p.kv_lens, b, p.kv_len);
+  const int state0 = (block * BWD_WAVES + wave) * 32, state = state0 + c32;
+  // tiles: those of the first head's tokens, the second's, ...
+  const int per_head = (p.q_len + KT - 1) / KT;
+  int first, count;
+  part_of(group * per_head, part, p.kv_parts, &first, &count);
+  if (block * BWD_WAVES * 32 >= n) count = 0;       // (no states here: zeros)
+
+  const uint32_t ldq = (uint32_t)p.ldq * 2, ld_do = (uint32_t)p.ld_do * 2;
+  TileLoads<HDP, KT, BWD_WAVES> lq, ld;
+  lq.init(ldq, p.head_dim, wave, lane);
+  ld.init(ld_do, p.head_dim, wave, lane);
+  int g = per_head ? __builtin_amdgcn_readfirstlane(first / per_head) : 0, tile = first - g * per_head;      // of the next tile to load
+  auto issue = [&](int stage) {
+    const int h = kvh * group + g, t0 = tile * KT, rows = p.q_len - t0;
+    const int64_t at = (int64_t)b * p.q_len + t0;
+    lq.issue((const uint8_t*)((const T*)p.q + at * p.ldq + (int64_t)h * p.head_dim), ldq, rows, smem[stage], wave);
+    ld.issue((const uint8_t*)((const T*)p.dout + at * p.ld_do + (int64_t)h * p.head_dim), ld_do, rows, smem[stage] + TILE, wave);
+    // (zeros for tokens past the last, whose weights are not kept)
+    if (wave < 2) {
+      const float* const st = (wave ? p.stat_d : p.stat_l) + ((int64_t)b * p.heads + h) * p.q_len + t0;
+      load_lds4(make_rsrc(st, 4 * min(rows, KT)), (uint8_t*)stats[stage][wave], lane * 4);
+    }
+    if (++tile == per_head) {
+      tile = 0;
+      ++g;
+    }
+  };
+  int now = tile;
+  if (count > 0) issue(0);
+
+  frag kf[KK], vf[KK];
+  const int64_t kv_row = (int64_t)b * p.kv_len + min(state, p.kv_len - 1), at = (int64_t)kvh * p.head_dim;
+  // (states behind the last one: their columns are not kept, whatever they hold)
+  load_column<T, HDP>((const T*)p.k + kv_row * p.ldk + at, p.head_dim, hi, kf);
+  load_column<T, HDP>((const T*)p.v + kv_row * p.ldv + at, p.head_dim, hi, vf);
+  f32x16 dk[ND], dv[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.f;
+  AlongRows<T, HDP> ra;
+  AcrossRows<T, HDP> rx;
+  ra.init(lane);
+  rx.init(lane);
+  const bool busy = state0 < n;
+  for (int i = 0; i < count; ++i) {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    __syncthreads();
+    const int here = p.q_len - now * KT;             // tokens of this tile on
+    now = now + 1 == per_head ? 0 : now + 1;
+    if (i + 1 < count) issue((i + 1) & 1);
+    if (!busy) continue;
+    const uint8_t *qs = smem[i & 1], *ds = qs + TILE;
+    const float *sl = stats[i & 1][0], *sd = stats[i & 1][1];
+#pragma unroll
+    for (int blk = 0; blk < 2; ++blk) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) s = Mfma<T>::run(ra.read(qs, 32 * blk, kk, hi), kf[kk], kk ? s : f32x16{});
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) dp = Mfma<T>::run(ra.read(ds, 32 * blk, kk, hi), vf[kk], kk ? dp : f32x16{});
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 L = *reinterpret_cast<const f32x4*>(sl + 32 * blk + 8 * r4 + 4 * hi);
+        const f32x4 D = *reinterpret_cast<const f32x4*>(sd + 32 * blk + 8 * r4 + 4 * hi);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * r4 + e;
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.c, -L[e]));
+          dp[r] = s[r] * fmaf(dp[r], P_UNIT<T>, -D[e]);
+        }
+      }
+      // (rows past the last token are zeros, which make NaN of an infinite k)
+      if (here < KT) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * blk + 8 * (r >> 2) + 4 * hi + (r & 3) >= here) s[r] = dp[r] = 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const frag pf = pack8<T>(s, u), df = pack8<T>(dp, u);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          dv[d] = Mfma<T>::run(rx.read(ds, 32 * blk + 16 * u, d), pf, dv[d]);
+          dk[d] = Mfma<T>::run(rx.read(qs, 32 * blk + 16 * u, d), df, dk[d]);
+        }
+      }
+    }
+  }
+  if (state >= n) {
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.f;
+  }
+  const bool valid = state < p.kv_len;
+  if (p.kv_parts > 1) {
+    const int64_t width = (int64_t)p.kv_heads * p.head_dim, one = (int64_t)p.batch * p.kv_len * width;
+    float* const out = p.dkv_parts + part * 2 * one + kv_row * width + at;
+    store_column_f32<ND>(out, p.head_dim, dk, p.scale, hi, valid);
+    store_column_f32<ND>(out + one, p.head_dim, dv, P_UNIT<T>, hi, valid);
+  } else {
+    store_column<T, ND>((T*)p.dk + kv_row * p.ld_dk + at, p.head_dim, dk, p.scale, hi, valid);
+    store_column<T, ND>((T*)p.dv + kv_row * p.ld_dv + at, p.head_dim, dv, P_UNIT<T>, hi, valid);
+  }
+}
+
+// Outputs from their parts, in order: matrix blockIdx.y of up to two, n elements
+// in rows of `width`; part i of it lies i `stride` past its first.
+template <typename T>
+__global__ __launch_bounds__(256) void k_cross_sums(const float* __restrict__ sums, int parts, int64_t stride, int64_t n, int width, T* out0, T* out1,
+                                                    int64_t ld0, int64_t ld1) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (at >= n) return;
+  const bool second = blockIdx.y;
+  const float* const from = sums + (second ? n : 0) + at;
+  f32x4 s = *reinterpret_cast<const f32x4*>(from);
+#pragma unroll 4
+  for (int i = 1; i < parts; ++i) s += *reinterpret_cast<const f32x4*>(from + i * stride);
+  t4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = (T)s[e];
+  const int64_t r = at / width;
+  *reinterpret_cast<t4*>((second ? out1 : out0) + r * (second ? ld1 : ld0) + (at - r * width)) = o;
+}
+
+template <typename T, int HDP>
+hipError_t run_cross_bwd(const CrossBwd& p, hipStream_t s) {
+  const int64_t q_wgs = (int64_t)p.batch * p.heads * ((p.q_len + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES)) * p.q_parts;
+  const int64_t kv_wgs = (int64_t)p.batch * p.kv_heads * ((p.kv_len + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES)) * p.kv_parts;
+  hipError_t e = hipSuccess;
+  if (q_wgs) {
+    hipLaunchKernelGGL((k_cross_dq<T, HDP>), dim3((unsigned)q_wgs), dim3(BWD_WAVES * 64), 0, s, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (p.dq && p.q_parts > 1) {
+      const int width = p.heads * p.head_dim;
+      const int64_t n = (int64_t)p.batch * p.q_len * width;
+      hipLaunchKernelGGL((k_cross_sums<T>), dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, s, p.dq_parts, p.q_parts, n, n, width, (T*)p.dq, (T*)p.dq,
+                         p.ld_dq, p.ld_dq);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  if (p.dk && kv_wgs) {
+    hipLaunchKernelGGL((k_cross_dkv<T, HDP>), dim3((unsigned)kv_wgs), dim3(BWD_WAVES * 64), 0, s, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (p.kv_parts > 1) {
+      const int width = p.kv_heads * p.head_dim;
+      const int64_t n = (int64_t)p.batch * p.kv_len * width;
+      hipLaunchKernelGGL((k_cross_sums<T>), dim3((unsigned)((n / 4 + 255) / 256), 2), dim3(256), 0, s, p.dkv_parts, p.kv_parts, 2 * n, n, width, (T*)p.dk,
+                         (T*)p.dv, p.ld_dk, p.ld_dv);
+      e = hipGetLastError();
+    }
+  }
+  return e;
+}
+
+template <typename T>
+hipError_t cross_bwd_t(const CrossBwd& p, hipStream_t s) {
+  if (p.head_dim <= 32) return run_cross_bwd<T, 32>(p, s);
+  if (p.head_dim <= 64) return run_cross_bwd<T, 64>(p, s);
+  return p.head_dim <= 96 ? run_cross_bwd<T, 96>(p, s) : run_cross_bwd<T, 128>(p, s);
+}
+
+// The workspace, in floats: lse and D, then the parts of dq, then those of dk and dv.
+struct BwdSpace {
+  int q_parts, kv_parts;
+  int64_t stats, dq, dkv;
+};
+BwdSpace bwd_space(const CrossShape& c) {
+  const int64_t q_rows = (int64_t)c.batch * c.q_len, kv_rows = (int64_t)c.batch * c.kv_len;
+  BwdSpace w{cross_dq_parts(c.batch, c.heads, c.q_len, c.kv_len),
+             cross_dkv_parts(c.batch, c.heads, c.kv_heads, c.head_dim, c.q_len, c.kv_len), 0, 0, 0};
+  w.stats = (q_rows * c.heads + 3) / 4 * 4;
+  w.dq = w.q_parts > 1 ? w.q_parts * q_rows * c.heads * c.head_dim : 0;
+  w.dkv = w.kv_parts > 1 ? w.kv_parts * 2 * kv_rows * c.kv_heads * c.head_dim : 0;
+  return w;
+}
+
+}  // namespace
+
+int64_t cross_attn_bwd_workspace(const CrossShape& c) {
+  const BwdSpace w = bwd_space(c);
+  return (2 * w.stats + w.dq + w.dkv) * 4;
+}
+
+hipError_t launch_cross_attn_bwd(const xema_cross_attn_bwd_args& a, hipStream_t s) {
+  const BwdSpace w = bwd_space({a.batch, a.heads, a.kv_heads, a.head_dim, a.q_len, a.kv_len});
+  float* const ws = (float*)a.workspace;
+  const CrossBwd p{a.q, a.k, a.v, a.o, a.dout, a.lse, a.kv_lens, a.dq, a.dk, a.dv, ws, ws + w.stats, ws + 2 * w.stats, ws + 2 * w.stats + w.dq,
+                   a.ldq, a.ldk, a.ldv, a.ldo, a.ld_do, a.ld_dq, a.ld_dk, a.ld_dv, a.batch, a.heads, a.kv_heads, a.head_dim, a.q_len, a.kv_len,
+                   w.q_parts, w.kv_parts, a.scale * LOG2E_F, a.scale};
+  return a.dtype == XEMA_BF16 ? cross_bwd_t<bf16>(p, s) : cross_bwd_t<f16>(p, s);
+}
+
+}  // namespace xema

@@ -228,6 +228,43 @@ inline ReducePick pick_reduce(int64_t rows, int rank) {
 }
 
 // ---------------------------------------------------------------------------
+// Attention to an encoder's states (k_cross.hip, k_cross_bwd.hip)
+// ---------------------------------------------------------------------------
+// few: the kernel of single tokens, whose blocks are 32 queries of all heads that
+// share a state's head; otherwise blocks of a head's queries, 256 to a workgroup
+// at head dims to 64 and 128 past that.  parts: of the states.
+struct CrossPick { bool few; int blocks, parts; };
+inline CrossPick pick_cross(int batch, int heads, int kv_heads, int head_dim, int q_len, int kv_len) {
+  const int64_t rows = (int64_t)q_len * (heads / kv_heads);
+  CrossPick pick{rows <= 64, 0, 1};
+  if (pick.few) {
+    pick.blocks = (int)((rows + 31) / 32);
+    const int64_t wgs = (int64_t)batch * kv_heads * pick.blocks, most = ((int64_t)kv_len + 255) / 256;
+    const int64_t want = (RULE_CUS * (head_dim <= 64 ? 2 : 1) + wgs - 1) / wgs;
+    pick.parts = (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 64}));
+    return pick;
+  }
+  const int per = head_dim <= 64 ? 256 : 128;
+  pick.blocks = (q_len + per - 1) / per;
+  const int64_t wgs = (int64_t)batch * heads * pick.blocks, tiles = ((int64_t)kv_len + 63) / 64;
+  pick.parts = (int)std::max<int64_t>(1, std::min<int64_t>({2 * RULE_CUS / wgs, tiles / 4, 16}));
+  return pick;
+}
+
+// The gradient: parts of the states for dq (workgroups of 128 queries of a head),
+// and of the tokens of all heads that share a state's head for dk and dv
+// (workgroups of 128 states).
+inline int cross_dq_parts(int batch, int heads, int q_len, int kv_len) {
+  const int64_t wgs = (int64_t)batch * heads * ((q_len + 127) / 128), tiles = ((int64_t)kv_len + 63) / 64;
+  return wgs ? (int)std::max<int64_t>(1, std::min<int64_t>({2 * RULE_CUS / wgs, tiles / 4, 16})) : 1;
+}
+inline int cross_dkv_parts(int batch, int heads, int kv_heads, int head_dim, int q_len, int kv_len) {
+  const int64_t wgs = (int64_t)batch * kv_heads * ((kv_len + 127) / 128), tiles = (int64_t)heads / kv_heads * ((q_len + 63) / 64);
+  const int64_t sums = 2 * (int64_t)batch * kv_len * kv_heads * head_dim;
+  return wgs ? (int)std::max<int64_t>(1, std::min<int64_t>({2 * RULE_CUS / wgs, tiles / 4, 32, ((int64_t)1 << 26) / sums})) : 1;
+}
+
+// ---------------------------------------------------------------------------
 // k_upconv.  A tile is RG R fragments of 16 corners (a corner: the four outputs
 // between four source pixels) and 128 / RG channels.
 // ---------------------------------------------------------------------------
