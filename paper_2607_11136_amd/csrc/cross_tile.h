@@ -63,19 +63,34 @@ struct TileLoads {
 #pragma unroll
     for (int c = 0; c < LOADS; ++c) load_lds16(r, st + (wave * LOADS + c) * 1024, off[c], 0);
   }
+  // The same, rows past the last (rows >= 1) repeating it.
+  __device__ __forceinline__ void issue_repeated(const uint8_t* base, uint32_t ld_bytes, int rows, uint8_t* st, int wave, int lane) const {
+    if (rows >= N) return issue(base, ld_bytes, N, st, wave);
+    TileLoads last;
+#pragma unroll
+    for (int c = 0; c < LOADS; ++c) {
+      const int row = (wave * LOADS + c) * RPL + lane / (RB / 16);
+      last.off[c] = off[c] == OUT_OF_RANGE ? OUT_OF_RANGE : off[c] - (uint32_t)max(row - (rows - 1), 0) * ld_bytes;
+    }
+    last.issue(base, ld_bytes, rows, st, wave);
+  }
 };
+
+// Keeps the compiler from holding every address that it forms from x: they are formed again where they are used.
+__device__ __forceinline__ void forget(uint32_t& x) { asm volatile("" : "+v"(x)); }
 
 // Fragments along rows: rows row0 + lane % 32, elements 16 kk + 8 (lane / 32) + 0..7.
 template <typename T, int HDP>
 struct AlongRows {
   typedef typename Mfma<T>::frag frag;
-  uint32_t base, swz;
+  uint32_t base;
   __device__ __forceinline__ void init(int lane) {
-    base = (lane & 31) * Rows<HDP>::RB;
-    swz = Rows<HDP>::swz(lane & 31);       // (the same for rows 32 apart)
+    // (the swizzle of a row is that of the rows 32 from it)
+    base = (lane & 31) * Rows<HDP>::RB + (((lane >> 5) ^ Rows<HDP>::swz(lane & 31)) << 4);
   }
-  __device__ __forceinline__ frag read(const uint8_t* st, int row0, int kk, int hi) const {
-    return *reinterpret_cast<const frag*>(st + row0 * Rows<HDP>::RB + base + (((kk * 2 + hi) ^ swz) << 4));
+  // row0 a multiple of 32
+  __device__ __forceinline__ frag read(const uint8_t* st, int row0, int kk) const {
+    return *reinterpret_cast<const frag*>(st + row0 * Rows<HDP>::RB + (base ^ (kk << 5)));
   }
 };
 

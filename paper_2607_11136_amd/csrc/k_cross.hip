@@ -180,7 +180,7 @@ __global__ __launch_bounds__(CROSS_WAVES * 64, 2) void k_cross(CrossParams p) {
     for (int kb2 = 0; kb2 < 2; ++kb2)
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
-        const frag f = rk.read(ks, 32 * kb2, kk, hi);
+        const frag f = rk.read(ks, 32 * kb2, kk);
 #pragma unroll
         for (int c = 0; c < QB; ++c) s[c][kb2] = Mfma<T>::run(f, qf[c][kk], kk ? s[c][kb2] : f32x16{});
       }
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(CROSS_WAVES * 64) void k_cross_few(CrossParams p) {
     const uint8_t *ks = stages + (i & 1) * STAGE, *vs = ks + TILE;
     f32x16 s[1];
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) s[0] = Mfma<T>::run(rk.read(ks, 0, kk, hi), qf[kk], kk ? s[0] : f32x16{});
+    for (int kk = 0; kk < KK; ++kk) s[0] = Mfma<T>::run(rk.read(ks, 0, kk), qf[kk], kk ? s[0] : f32x16{});
     const int here = n - (first + wave + i * CROSS_WAVES) * FT;
     if (here < FT) mask_from<1>(s, here, hi);
     col.template weigh<1>(s, p.c, i == 0);

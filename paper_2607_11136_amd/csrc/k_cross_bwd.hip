@@ -34,7 +34,7 @@ struct CrossBwd {
   const float* lse;
   const int32_t* kv_lens;
   void *dq, *dk, *dv;
-  float *stat_l, *stat_d;              // [batch, heads, q_len]: lse in log2 units less P_EXP (+infinity: no states), P_UNIT D
+  float *stat_l, *stat_d;              // [batch, heads, q_len rounded up to KT]: lse in log2 units less P_EXP (+infinity: no states, no token), P_UNIT D
   float* dq_parts;                     // [parts][batch * q_len][heads * head_dim]
   float* dkv_parts;                    // [parts][dk, dv][batch * kv_len][kv_heads * head_dim]
   int64_t ldq, ldk, ldv, ldo, ld_do, ld_dq, ld_dk, ld_dv;
@@ -95,9 +95,11 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
   D = pair_sum(D);
   const float lse = p.lse[row];
   const float L = lse == -INFINITY ? INFINITY : lse * LOG2E_F;
-  if (part == 0 && valid && !hi) {
-    p.stat_l[row] = L - P_EXP<T>;
-    p.stat_d[row] = D * P_UNIT<T>;
+  const int padded = (p.q_len + KT - 1) / KT * KT;
+  if (part == 0 && q < padded && !hi) {
+    const int64_t st = (int64_t)bh * padded + q;
+    p.stat_l[st] = valid ? L - P_EXP<T> : INFINITY;
+    p.stat_d[st] = valid ? D * P_UNIT<T> : 0.f;
   }
   if (!p.dq) return;
 
@@ -121,9 +123,9 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
     for (int blk = 0; blk < 2; ++blk) {
       f32x16 s, dp;
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) s = Mfma<T>::run(ra.read(ks, 32 * blk, kk, hi), qf[kk], kk ? s : f32x16{});
+      for (int kk = 0; kk < KK; ++kk) s = Mfma<T>::run(ra.read(ks, 32 * blk, kk), qf[kk], kk ? s : f32x16{});
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) dp = Mfma<T>::run(ra.read(vs, 32 * blk, kk, hi), df[kk], kk ? dp : f32x16{});
+      for (int kk = 0; kk < KK; ++kk) dp = Mfma<T>::run(ra.read(vs, 32 * blk, kk), df[kk], kk ? dp : f32x16{});
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.c, -L)) * (dp[r] - D);
       if (here < KT) {
@@ -146,7 +148,7 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
 }
 
 template <typename T, int HDP>
-__global__ __launch_bounds__(BWD_WAVES * 64, 1) void k_cross_dkv(CrossBwd p) {
+__global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dkv(CrossBwd p) {
   typedef Rows<HDP> R;
   typedef typename Mfma<T>::frag frag;
   constexpr int KK = R::KK, ND = R::ND, TILE = KT * R::RB;
@@ -174,19 +176,18 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 1) void k_cross_dkv(CrossBwd p) {
   auto issue = [&](int stage) {
     const int h = kvh * group + g, t0 = tile * KT, rows = p.q_len - t0;
     const int64_t at = (int64_t)b * p.q_len + t0;
-    lq.issue((const uint8_t*)((const T*)p.q + at * p.ldq + (int64_t)h * p.head_dim), ldq, rows, smem[stage], wave);
-    ld.issue((const uint8_t*)((const T*)p.dout + at * p.ld_do + (int64_t)h * p.head_dim), ld_do, rows, smem[stage] + TILE, wave);
-    // (zeros for tokens past the last, whose weights are not kept)
+    // (tokens past the last repeat it, and weigh 0 by their lse: rows of zeros would make NaN of an infinite k)
+    lq.issue_repeated((const uint8_t*)((const T*)p.q + at * p.ldq + (int64_t)h * p.head_dim), ldq, rows, smem[stage], wave, lane);
+    ld.issue_repeated((const uint8_t*)((const T*)p.dout + at * p.ld_do + (int64_t)h * p.head_dim), ld_do, rows, smem[stage] + TILE, wave, lane);
     if (wave < 2) {
-      const float* const st = (wave ? p.stat_d : p.stat_l) + ((int64_t)b * p.heads + h) * p.q_len + t0;
-      load_lds4(make_rsrc(st, 4 * min(rows, KT)), (uint8_t*)stats[stage][wave], lane * 4);
+      const float* const st = (wave ? p.stat_d : p.stat_l) + (((int64_t)b * p.heads + h) * per_head + tile) * KT;
+      load_lds4(make_rsrc(st, 4 * KT), (uint8_t*)stats[stage][wave], lane * 4);
     }
     if (++tile == per_head) {
       tile = 0;
       ++g;
     }
   };
-  int now = tile;
   if (count > 0) issue(0);
 
   frag kf[KK], vf[KK];
@@ -208,19 +209,20 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 1) void k_cross_dkv(CrossBwd p) {
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
     __syncthreads();
-    const int here = p.q_len - now * KT;             // tokens of this tile on
-    now = now + 1 == per_head ? 0 : now + 1;
     if (i + 1 < count) issue((i + 1) & 1);
     if (!busy) continue;
     const uint8_t *qs = smem[i & 1], *ds = qs + TILE;
     const float *sl = stats[i & 1][0], *sd = stats[i & 1][1];
-#pragma unroll
+    // (32 tokens at a time: both blocks at once would not fit the registers beside dk and dv of wide heads)
+#pragma unroll 1
     for (int blk = 0; blk < 2; ++blk) {
+      forget(ra.base);
+      forget(rx.base);
       f32x16 s, dp;
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) s = Mfma<T>::run(ra.read(qs, 32 * blk, kk, hi), kf[kk], kk ? s : f32x16{});
+      for (int kk = 0; kk < KK; ++kk) s = Mfma<T>::run(ra.read(qs, 32 * blk, kk), kf[kk], kk ? s : f32x16{});
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) dp = Mfma<T>::run(ra.read(ds, 32 * blk, kk, hi), vf[kk], kk ? dp : f32x16{});
+      for (int kk = 0; kk < KK; ++kk) dp = Mfma<T>::run(ra.read(ds, 32 * blk, kk), vf[kk], kk ? dp : f32x16{});
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         const f32x4 L = *reinterpret_cast<const f32x4*>(sl + 32 * blk + 8 * r4 + 4 * hi);
@@ -231,12 +233,6 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 1) void k_cross_dkv(CrossBwd p) {
           s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.c, -L[e]));
           dp[r] = s[r] * fmaf(dp[r], P_UNIT<T>, -D[e]);
         }
-      }
-      // (rows past the last token are zeros, which make NaN of an infinite k)
-      if (here < KT) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (32 * blk + 8 * (r >> 2) + 4 * hi + (r & 3) >= here) s[r] = dp[r] = 0.f;
       }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -333,7 +329,7 @@ BwdSpace bwd_space(const CrossShape& c) {
   const int64_t q_rows = (int64_t)c.batch * c.q_len, kv_rows = (int64_t)c.batch * c.kv_len;
   BwdSpace w{cross_dq_parts(c.batch, c.heads, c.q_len, c.kv_len),
              cross_dkv_parts(c.batch, c.heads, c.kv_heads, c.head_dim, c.q_len, c.kv_len), 0, 0, 0};
-  w.stats = (q_rows * c.heads + 3) / 4 * 4;
+  w.stats = (int64_t)c.batch * c.heads * ((c.q_len + KT - 1) / KT * KT);
   w.dq = w.q_parts > 1 ? w.q_parts * q_rows * c.heads * c.head_dim : 0;
   w.dkv = w.kv_parts > 1 ? w.kv_parts * 2 * kv_rows * c.kv_heads * c.head_dim : 0;
   return w;
