@@ -77,7 +77,8 @@ struct TileLoads {
 };
 
 // Keeps the compiler from holding every address that it forms from x: they are formed again where they are used.
-__device__ __forceinline__ void forget(uint32_t& x) { asm volatile("" : "+v"(x)); }
+template <typename I>
+__device__ __forceinline__ void forget(I& x) { asm volatile("" : "+v"(x)); }
 
 // Fragments along rows: rows row0 + lane % 32, elements 16 kk + 8 (lane / 32) + 0..7.
 template <typename T, int HDP>
@@ -147,32 +148,83 @@ __device__ __forceinline__ float pair_max(float v) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// A lane's column of a transposed result (ND blocks of 32 elements) times f, as
-// row `row` of a matrix: 16 bytes a lane, the halves of the wave exchanging
-// quarters of each 16 elements.  `valid`: whether the column is there.
+// Elements 16 g + 8 (lane / 32) ... + 7 of a lane's column of a transposed result's
+// block of 32, times f: the halves of the wave exchange quarters of each 16.
+template <typename T>
+__device__ __forceinline__ u32x4 eight_of(const f32x16& acc, int g, float f) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  t4 a, b;          // elements 16 g + 4 (lane / 32) ... and eight further on
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    a[e] = (T)(acc[8 * g + e] * f);
+    b[e] = (T)(acc[8 * g + 4 + e] * f);
+  }
+  const u32x2 ua = __builtin_bit_cast(u32x2, a), ub = __builtin_bit_cast(u32x2, b);
+  // the low half takes both halves' a, the high half both halves' b
+  const auto r0 = __builtin_amdgcn_permlane32_swap(ua[0], ub[0], false, false);
+  const auto r1 = __builtin_amdgcn_permlane32_swap(ua[1], ub[1], false, false);
+  return u32x4{r0[0], r1[0], r0[1], r1[1]};
+}
+
+// 32 rows of a matrix [rows, elements] through 32 RB bytes of LDS that a wave has
+// to itself, so that 16 lanes (8 at 128 bytes a row) load or store a row's
+// consecutive bytes: straight between memory and a lane's column each load meets
+// a quarter of 32 rows' lines, and the address unit takes longer than the products
+// (16384 tokens, 32 heads of 128, 512 states: 183 us, through LDS 145).
+template <int HDP>
+struct WaveRows {
+  static constexpr int BYTES = 32 * Rows<HDP>::RB;
+  typedef TileLoads<HDP, 32, 1> Loads;
+  // rows past the last (rows <= 0: all) are zeros
+  static __device__ __forceinline__ void load(const void* base, uint32_t ld_bytes, int head_dim, int rows, uint8_t* at, int lane) {
+    Loads l;
+    l.init(ld_bytes, head_dim, 0, lane);
+    l.issue((const uint8_t*)base, ld_bytes, rows, at, 0);
+  }
+  // a lane's column of it, once it has landed
+  template <typename T>
+  static __device__ __forceinline__ void read(const uint8_t* at, const AlongRows<T, HDP>& r, typename Mfma<T>::frag (&f)[Rows<HDP>::KK]) {
+#pragma unroll
+    for (int kk = 0; kk < Rows<HDP>::KK; ++kk) f[kk] = r.read(at, 0, kk);
+  }
+  // The columns of a transposed result (ND blocks of 32 elements) times f as rows
+  // of 16-bit values, `rows` of them.
+  template <typename T>
+  static __device__ __forceinline__ void store(T* base, int64_t ld, int head_dim, int rows, const f32x16 (&acc)[Rows<HDP>::ND], float f, uint8_t* at,
+                                               int lane) {
+    constexpr int RB = Rows<HDP>::RB, SLOTS = RB / 16;
+    const int c32 = lane & 31, hi = lane >> 5;
+#pragma unroll
+    for (int d = 0; d < Rows<HDP>::ND; ++d)
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+        *reinterpret_cast<u32x4*>(at + c32 * RB + (((d * 4 + g * 2 + hi) ^ Rows<HDP>::swz(c32)) << 4)) = eight_of<T>(acc[d], g, f);
+    // (the wave's own writes: LDS takes a wave's accesses in order)
+    const int slot = lane % SLOTS;
+#pragma unroll
+    for (int c = 0; c < 32 * SLOTS / 64; ++c) {
+      const int row = c * (64 / SLOTS) + lane / SLOTS;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(at + row * RB + ((slot ^ Rows<HDP>::swz(row)) << 4));
+      if (row < rows && slot * 8 < head_dim) *reinterpret_cast<u32x4*>(base + row * ld + slot * 8) = v;
+    }
+  }
+};
+
+// A lane's column of a transposed result times f, as 16-bit values at `row`, 16
+// bytes a lane.  `valid`: whether the column is there.
 template <typename T, int ND>
 __device__ __forceinline__ void store_column(T* row, int head_dim, const f32x16 (&acc)[ND], float f, int hi, bool valid) {
-  typedef T t4 __attribute__((ext_vector_type(4)));
 #pragma unroll
   for (int d = 0; d < ND; ++d)
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      t4 a, b;        // elements 16 g + 4 hi ... and 16 g + 8 + 4 hi ... of the block
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        a[e] = (T)(acc[d][8 * g + e] * f);
-        b[e] = (T)(acc[d][8 * g + 4 + e] * f);
-      }
-      const u32x2 ua = __builtin_bit_cast(u32x2, a), ub = __builtin_bit_cast(u32x2, b);
-      // the low half takes both halves' a (8 elements), the high half both halves' b
-      const auto r0 = __builtin_amdgcn_permlane32_swap(ua[0], ub[0], false, false);
-      const auto r1 = __builtin_amdgcn_permlane32_swap(ua[1], ub[1], false, false);
-      const u32x4 o = {r0[0], r1[0], r0[1], r1[1]};
+      const u32x4 o = eight_of<T>(acc[d], g, f);
       const int e = d * 32 + g * 16 + hi * 8;
       if (valid && e < head_dim) *reinterpret_cast<u32x4*>(row + e) = o;
     }
 }
-// The same in fp32.
+// A lane's column of a transposed result times f, as fp32 values at `row`.
+// `valid`: whether the column is there.
 template <int ND>
 __device__ __forceinline__ void store_column_f32(float* row, int head_dim, const f32x16 (&acc)[ND], float f, int hi, bool valid) {
 #pragma unroll

@@ -23,7 +23,7 @@ namespace xema {
 
 namespace {
 
-constexpr int KT = 64;                 // states per tile
+constexpr int KT = 32;                 // states per tile
 constexpr int CROSS_WAVES = 4;
 constexpr float PMAX = 4096.f;         // (fp16 P stays finite; 2^12 beside sums in fp32 loses nothing)
 constexpr float LOWEST = -1e30f;       // a reference below every score, so that -infinity less it stays one
@@ -97,43 +97,42 @@ struct Column {
 // Scores of states at or past `left` become -infinity: block b's register r is state 32 b + 8 (r / 4) + 4 hi + r % 4.
 template <int NB>
 __device__ __forceinline__ void mask_from(f32x16 (&s)[NB], int left, int hi) {
+  const int mine = left - 4 * hi;      // (against constants, which take no registers)
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r)
-      if (32 * b + 8 * (r >> 2) + 4 * hi + (r & 3) >= left) s[b][r] = -INFINITY;
+      if (32 * b + 8 * (r >> 2) + (r & 3) >= mine) s[b][r] = -INFINITY;
 }
 
-// What a lane's column leaves: o and lse, or its part of them.  `row` is the
-// column's among all (batch, head, token); o_at the address of its output.
-template <typename T, int ND>
-__device__ __forceinline__ void finish(const CrossParams& p, const Column<ND>& col, float l, int64_t row, T* o_at, int part, int hi, bool valid) {
-  if (p.parts > 1) {
-    const int64_t at = part * p.rows + row;
-    store_column_f32<ND>(p.part_o + at * p.head_dim, p.head_dim, col.o, 1.f, hi, valid);
-    if (valid && !hi) p.part_ml[at] = float2{col.m, l};
-    return;
-  }
-  store_column<T, ND>(o_at, p.head_dim, col.o, l == 0.f ? 0.f : 1.f / l, hi, valid);
-  // (v_log_f32 is log2)
-  if (p.lse && valid && !hi) p.lse[row] = l == 0.f ? -INFINITY : (col.m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-}
+// ln of the sum, of which l is what 2^m leaves (v_log_f32 is log2); -infinity for none.
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f; }
 
-template <typename T, int HDP, int QB>
-__global__ __launch_bounds__(CROSS_WAVES * 64, 2) void k_cross(CrossParams p) {
+template <typename T, int HDP>
+__global__ __launch_bounds__(CROSS_WAVES * 64, HDP <= 64 ? 4 : 3) void k_cross(CrossParams p) {
   typedef Rows<HDP> R;
   typedef typename Mfma<T>::frag frag;
   constexpr int KK = R::KK, ND = R::ND, TILE = KT * R::RB;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2 * TILE];
+  // two stages of K and V, and one tile more: the waves' rows of queries and of
+  // outputs pass through that and the stage that holds no tile then
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[3][2 * TILE];
+  static_assert(CROSS_WAVES * WaveRows<HDP>::BYTES == 4 * TILE, "rows of four waves");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c32 = lane & 31, hi = lane >> 5;
-  // workgroup -> (batch, head, part, block of queries)
+  // workgroup -> (head, batch, part, block of queries): an XCD's range holds all
+  // sequences of its heads, whose lengths may differ
   const int t = xcd_order((int)blockIdx.x, (int)gridDim.x);
-  const int block = t % p.blocks, part = t / p.blocks % p.parts, bh = t / p.blocks / p.parts;
-  const int b = bh / p.heads, h = bh - b * p.heads, kvh = h / (p.heads / p.kv_heads);
+  const int block = t % p.blocks, part = t / p.blocks % p.parts, hb = t / p.blocks / p.parts;
+  const int h = hb / p.batch, b = hb - h * p.batch, kvh = h / (p.heads / p.kv_heads);
   const int n = states_of(p.kv_lens, b, p.kv_len), tiles = (n + KT - 1) / KT;
   int first, count;
   part_of(tiles, part, p.parts, &first, &count);
+  auto rows_at = [&](int free) { return smem[wave < 2 ? 2 : free] + (wave & 1) * WaveRows<HDP>::BYTES; };
+
+  // this wave's queries: q0 .. q0 + 31, of which `left_q` are there
+  const int q0 = (block * CROSS_WAVES + wave) * 32, left_q = p.q_len - q0;
+  const int64_t tok0 = (int64_t)b * p.q_len + q0;
+  WaveRows<HDP>::load((const T*)p.q + tok0 * p.ldq + (int64_t)h * p.head_dim, (uint32_t)p.ldq * 2, p.head_dim, left_q, rows_at(1), lane);
 
   const int64_t kv_row = (int64_t)b * p.kv_len + (int64_t)first * KT;
   const uint8_t* kb = (const uint8_t*)((const T*)p.k + kv_row * p.ldk + kvh * p.head_dim);
@@ -152,65 +151,60 @@ __global__ __launch_bounds__(CROSS_WAVES * 64, 2) void k_cross(CrossParams p) {
   };
   if (count > 0) issue(0);
 
-  // (queries past the last repeat it and are not stored)
-  const int q0 = (block * CROSS_WAVES + wave) * QB * 32;
-  const T* const qh = (const T*)p.q + (int64_t)b * p.q_len * p.ldq + (int64_t)h * p.head_dim;
-  frag qf[QB][KK];
-  Column<ND> col[QB];
-#pragma unroll
-  for (int c = 0; c < QB; ++c) {
-    load_column<T, HDP>(qh + (int64_t)min(q0 + 32 * c + c32, p.q_len - 1) * p.ldq, p.head_dim, hi, qf[c]);
-    col[c].init();
-  }
   AlongRows<T, HDP> rk;
   AcrossRows<T, HDP> rv;
   rk.init(lane);
   rv.init(lane);
-
-  for (int i = 0; i < count; ++i) {
+  frag qf[KK];
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+  asm volatile("" ::: "memory");
+  WaveRows<HDP>::template read<T>(rows_at(1), rk, qf);
+  Column<ND> col;
+  col.init();
+  // (stages by name, so that a fragment's address is a register and an immediate)
+  auto tile = [&](int i, auto stage) {
+    constexpr int ST = decltype(stage)::value;
     // tile i has landed (this wave's part: vmcnt; the others': the barrier), and
-    // every wave has read tile i - 1, whose stage tile i + 1 takes
+    // every wave has read tile i - 1 (or its queries), whose stage tile i + 1 takes
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
     __syncthreads();
-    if (i + 1 < count) issue((i + 1) & 1);
-    const uint8_t *ks = smem[i & 1], *vs = ks + TILE;
-    f32x16 s[QB][2];
+    if (i + 1 < count) issue(ST ^ 1);
+    const uint8_t *ks = smem[ST], *vs = ks + TILE;
+    if constexpr (ND == 4) {        // (all of a wide head's addresses beside its sums would not fit the registers)
+      forget(rk.base);
+      forget(rv.base);
+    }
+    f32x16 s[1];
 #pragma unroll
-    for (int kb2 = 0; kb2 < 2; ++kb2)
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        const frag f = rk.read(ks, 32 * kb2, kk);
-#pragma unroll
-        for (int c = 0; c < QB; ++c) s[c][kb2] = Mfma<T>::run(f, qf[c][kk], kk ? s[c][kb2] : f32x16{});
-      }
+    for (int kk = 0; kk < KK; ++kk) s[0] = Mfma<T>::run(rk.read(ks, 0, kk), qf[kk], kk ? s[0] : f32x16{});
     const int here = n - (first + i) * KT;
+    if (here < KT) mask_from<1>(s, here, hi);
+    col.template weigh<1>(s, p.c, i == 0);
 #pragma unroll
-    for (int c = 0; c < QB; ++c) {
-      if (here < KT) mask_from<2>(s[c], here, hi);
-      col[c].template weigh<2>(s[c], p.c, i == 0);
+    for (int u = 0; u < 2; ++u) {
+      const frag pf = pack8<T>(s[0], u);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) col.o[d] = Mfma<T>::run(rv.read(vs, 16 * u, d), pf, col.o[d]);
     }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      frag pf[QB];
-#pragma unroll
-      for (int c = 0; c < QB; ++c) pf[c] = pack8<T>(s[c][u >> 1], u & 1);
-#pragma unroll
-      for (int d = 0; d < ND; ++d) {
-        const frag f = rv.read(vs, 16 * u, d);
-#pragma unroll
-        for (int c = 0; c < QB; ++c) col[c].o[d] = Mfma<T>::run(f, pf[c], col[c].o[d]);
-      }
-    }
+  };
+  for (int i = 0; i < count; i += 2) {
+    tile(i, std::integral_constant<int, 0>());
+    if (i + 1 < count) tile(i + 1, std::integral_constant<int, 1>());
   }
-#pragma unroll
-  for (int c = 0; c < QB; ++c) {
-    const int q = q0 + 32 * c + c32;
-    const bool valid = q < p.q_len;
-    const int64_t token = valid ? q : 0;
-    finish<T, ND>(p, col[c], pair_sum(col[c].l), ((int64_t)b * p.heads + h) * p.q_len + token,
-                  (T*)p.o + ((int64_t)b * p.q_len + token) * p.ldo + (int64_t)h * p.head_dim, part, hi, valid);
+  const float l = pair_sum(col.l);
+  const bool valid = c32 < left_q;
+  const int64_t row = ((int64_t)b * p.heads + h) * p.q_len + q0 + (valid ? c32 : 0);
+  if (p.parts > 1) {
+    const int64_t at = part * p.rows + row;
+    store_column_f32<ND>(p.part_o + at * p.head_dim, p.head_dim, col.o, 1.f, hi, valid);
+    if (valid && !hi) p.part_ml[at] = float2{col.m, l};
+    return;
   }
+  // (the stage that the last tile is not in)
+  WaveRows<HDP>::template store<T>((T*)p.o + tok0 * p.ldo + (int64_t)h * p.head_dim, p.ldo, p.head_dim, left_q, col.o, l == 0.f ? 0.f : 1.f / l,
+                                   rows_at(count & 1), lane);
+  if (p.lse && valid && !hi) p.lse[row] = lse_of(col.m, l);
 }
 
 constexpr int FT = 32;                 // states per tile of a wave of k_cross_few
@@ -328,7 +322,7 @@ __global__ __launch_bounds__(CROSS_WAVES * 64) void k_cross_few(CrossParams p) {
   }
   if (threadIdx.x & 7) return;
   if (p.parts > 1) p.part_ml[prow] = float2{m, sum};
-  else if (p.lse) p.lse[row] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  else if (p.lse) p.lse[row] = lse_of(m, sum);
 }
 
 // The parts of a (batch, head, token)'s sums, joined in order: 16 threads a row, eight columns each.
@@ -345,7 +339,7 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p) {
   const int64_t bh = row / p.q_len, token = row - bh * p.q_len, b = bh / p.heads, h = bh - b * p.heads;
   const float f = sum == 0.f ? 0.f : 1.f / sum;
   const int e = ((int)threadIdx.x & 15) * 8;
-  if (e == 0 && p.lse) p.lse[row] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+  if (e == 0 && p.lse) p.lse[row] = lse_of(m, sum);
   if (e >= p.head_dim) return;
   f32x4 v[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll 4
@@ -364,11 +358,10 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p) {
 
 template <typename T, int HDP>
 hipError_t run_cross(CrossParams p, const CrossPick& pick, hipStream_t s) {
-  constexpr int QB = HDP <= 64 ? 2 : 1;
   p.blocks = pick.blocks;
   const unsigned wgs = (unsigned)((int64_t)p.batch * (pick.few ? p.kv_heads : p.heads) * pick.blocks * pick.parts);
   if (pick.few) hipLaunchKernelGGL((k_cross_few<T, HDP>), dim3(wgs), dim3(CROSS_WAVES * 64), 0, s, p);
-  else hipLaunchKernelGGL((k_cross<T, HDP, QB>), dim3(wgs), dim3(CROSS_WAVES * 64), 0, s, p);
+  else hipLaunchKernelGGL((k_cross<T, HDP>), dim3(wgs), dim3(CROSS_WAVES * 64), 0, s, p);
   return hipGetLastError();
 }
 

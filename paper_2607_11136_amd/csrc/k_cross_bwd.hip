@@ -42,62 +42,93 @@ struct CrossBwd {
   float c, scale;                      // scale * log2(e), scale
 };
 
+constexpr int QKT = 32;                // states per tile of k_cross_dq
+
 template <typename T, int HDP>
 __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
   typedef Rows<HDP> R;
   typedef typename Mfma<T>::frag frag;
-  constexpr int KK = R::KK, ND = R::ND, TILE = KT * R::RB;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2 * TILE];
+  constexpr int KK = R::KK, ND = R::ND, TILE = QKT * R::RB, SLOTS = R::RB / 16, PER = 64 / SLOTS;
+  // two stages of K and V; the waves' rows of q pass through stage 1 and a third
+  // part, those of dout, and of dq in the end, through two more
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[5][2 * TILE];
+  static_assert(BWD_WAVES * WaveRows<HDP>::BYTES == 4 * TILE, "rows of four waves");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c32 = lane & 31, hi = lane >> 5;
   const int blocks = (p.q_len + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES);
   const int t = xcd_order((int)blockIdx.x, (int)gridDim.x);
-  const int block = t % blocks, part = t / blocks % p.q_parts, bh = t / blocks / p.q_parts;
-  const int b = bh / p.heads, h = bh - b * p.heads, kvh = h / (p.heads / p.kv_heads);
-  const int n = states_of(p.kv_lens, b, p.kv_len), tiles = (n + KT - 1) / KT;
+  // (an XCD's range holds all sequences of its heads, whose lengths may differ)
+  const int block = t % blocks, part = t / blocks % p.q_parts, hb = t / blocks / p.q_parts;
+  const int h = hb / p.batch, b = hb - h * p.batch, kvh = h / (p.heads / p.kv_heads);
+  const int n = states_of(p.kv_lens, b, p.kv_len), tiles = (n + QKT - 1) / QKT;
   int first, count;
   part_of(tiles, part, p.q_parts, &first, &count);
   if (!p.dq) count = 0;
 
-  const int64_t kv_row = (int64_t)b * p.kv_len + (int64_t)first * KT;
+  // this wave's tokens: q0 .. q0 + 31, of which `left_q` are there
+  const int q0 = (block * BWD_WAVES + wave) * 32, left_q = p.q_len - q0;
+  const int64_t tok0 = (int64_t)b * p.q_len + q0, at = (int64_t)h * p.head_dim;
+  uint8_t* const q_rows = smem[wave < 2 ? 2 : 1] + (wave & 1) * WaveRows<HDP>::BYTES;
+  uint8_t* const d_out_rows = smem[3 + wave / 2] + (wave & 1) * WaveRows<HDP>::BYTES;
+  WaveRows<HDP>::load((const T*)p.dout + tok0 * p.ld_do + at, (uint32_t)p.ld_do * 2, p.head_dim, left_q, d_out_rows, lane);
+  WaveRows<HDP>::load((const T*)p.q + tok0 * p.ldq + at, (uint32_t)p.ldq * 2, p.head_dim, left_q, q_rows, lane);
+  // (o is met row by row: SLOTS lanes a row, eight elements each)
+  const int slot = lane % SLOTS;
+  frag o[32 / PER];
+#pragma unroll
+  for (int c = 0; c < 32 / PER; ++c) {
+    const int r = c * PER + lane / SLOTS;
+    o[c] = frag{};
+    if (r < left_q && slot * 8 < p.head_dim) o[c] = *reinterpret_cast<const frag*>((const T*)p.o + (tok0 + r) * p.ldo + at + slot * 8);
+  }
+
+  const int64_t kv_row = (int64_t)b * p.kv_len + (int64_t)first * QKT;
   const uint8_t* kb = (const uint8_t*)((const T*)p.k + kv_row * p.ldk + kvh * p.head_dim);
   const uint8_t* vb = (const uint8_t*)((const T*)p.v + kv_row * p.ldv + kvh * p.head_dim);
   const uint32_t ldk = (uint32_t)p.ldk * 2, ldv = (uint32_t)p.ldv * 2;
-  TileLoads<HDP, KT, BWD_WAVES> lk, lv;
+  TileLoads<HDP, QKT, BWD_WAVES> lk, lv;
   lk.init(ldk, p.head_dim, wave, lane);
   lv.init(ldv, p.head_dim, wave, lane);
-  int left = n - first * KT;
+  int left = n - first * QKT;
   auto issue = [&](int stage) {
     lk.issue(kb, ldk, left, smem[stage], wave);
     lv.issue(vb, ldv, left, smem[stage] + TILE, wave);
-    kb += (int64_t)KT * ldk;
-    vb += (int64_t)KT * ldv;
-    left -= KT;
+    kb += (int64_t)QKT * ldk;
+    vb += (int64_t)QKT * ldv;
+    left -= QKT;
   };
   if (count > 0) issue(0);
 
-  const int q = (block * BWD_WAVES + wave) * 32 + c32;
-  const bool valid = q < p.q_len;
-  const int64_t token = min(q, p.q_len - 1), tok_row = (int64_t)b * p.q_len + token, row = ((int64_t)b * p.heads + h) * p.q_len + token;
-  const int64_t at = (int64_t)h * p.head_dim;
-  frag qf[KK], df[KK];
-  load_column<T, HDP>((const T*)p.q + tok_row * p.ldq + at, p.head_dim, hi, qf);
-  load_column<T, HDP>((const T*)p.dout + tok_row * p.ld_do + at, p.head_dim, hi, df);
-  float D = 0.f;
-  {
-    frag of[KK];
-    load_column<T, HDP>((const T*)p.o + tok_row * p.ldo + at, p.head_dim, hi, of);
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) D = fmaf((float)df[kk][e], (float)of[kk][e], D);
-  }
-  D = pair_sum(D);
-  const float lse = p.lse[row];
+  const int q = q0 + c32;
+  const bool valid = c32 < left_q;
+  const float lse = valid ? p.lse[((int64_t)b * p.heads + h) * p.q_len + q] : -INFINITY;
   const float L = lse == -INFINITY ? INFINITY : lse * LOG2E_F;
+  AlongRows<T, HDP> ra;
+  AcrossRows<T, HDP> rx;
+  ra.init(lane);
+  rx.init(lane);
+  frag qf[KK], df[KK];
+  __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+  asm volatile("" ::: "memory");
+  WaveRows<HDP>::template read<T>(q_rows, ra, qf);
+  WaveRows<HDP>::template read<T>(d_out_rows, ra, df);
+#pragma unroll
+  for (int c = 0; c < 32 / PER; ++c) {
+    const int r = c * PER + lane / SLOTS;
+    const frag d = *reinterpret_cast<const frag*>(d_out_rows + r * R::RB + ((slot ^ R::swz(r)) << 4));
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf((float)d[e], (float)o[c][e], sum);
+#pragma unroll
+    for (int x = 1; x < SLOTS; x *= 2) sum += __shfl_xor(sum, x, 64);
+    // (in place of the rows of q, which are read: LDS takes a wave's accesses in order)
+    if (slot == 0) reinterpret_cast<float*>(q_rows)[r] = sum;
+  }
+  asm volatile("" ::: "memory");
+  const float D = reinterpret_cast<const float*>(q_rows)[c32];
   const int padded = (p.q_len + KT - 1) / KT * KT;
   if (part == 0 && q < padded && !hi) {
-    const int64_t st = (int64_t)bh * padded + q;
+    const int64_t st = ((int64_t)b * p.heads + h) * padded + q;
     p.stat_l[st] = valid ? L - P_EXP<T> : INFINITY;
     p.stat_d[st] = valid ? D * P_UNIT<T> : 0.f;
   }
@@ -108,43 +139,43 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
   for (int d = 0; d < ND; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[d][r] = 0.f;
-  AlongRows<T, HDP> ra;
-  AcrossRows<T, HDP> rx;
-  ra.init(lane);
-  rx.init(lane);
-  for (int i = 0; i < count; ++i) {
+  // (stages by name, so that a fragment's address is a register and an immediate)
+  auto tile = [&](int i, auto stage) {
+    constexpr int ST = decltype(stage)::value;
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
     __syncthreads();
-    if (i + 1 < count) issue((i + 1) & 1);
-    const uint8_t *ks = smem[i & 1], *vs = ks + TILE;
-    const int here = n - (first + i) * KT;
+    if (i + 1 < count) issue(ST ^ 1);
+    const uint8_t *ks = smem[ST], *vs = ks + TILE;
+    const int here = n - (first + i) * QKT;
+    f32x16 s, dp;
 #pragma unroll
-    for (int blk = 0; blk < 2; ++blk) {
-      f32x16 s, dp;
+    for (int kk = 0; kk < KK; ++kk) s = Mfma<T>::run(ra.read(ks, 0, kk), qf[kk], kk ? s : f32x16{});
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) s = Mfma<T>::run(ra.read(ks, 32 * blk, kk), qf[kk], kk ? s : f32x16{});
+    for (int kk = 0; kk < KK; ++kk) dp = Mfma<T>::run(ra.read(vs, 0, kk), df[kk], kk ? dp : f32x16{});
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) dp = Mfma<T>::run(ra.read(vs, 32 * blk, kk), df[kk], kk ? dp : f32x16{});
+    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.c, -L)) * (dp[r] - D);
+    if (here < QKT) {
+      const int mine = here - 4 * hi;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.c, -L)) * (dp[r] - D);
-      if (here < KT) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (32 * blk + 8 * (r >> 2) + 4 * hi + (r & 3) >= here) s[r] = 0.f;
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const frag f = pack8<T>(s, u);
-#pragma unroll
-        for (int d = 0; d < ND; ++d) acc[d] = Mfma<T>::run(rx.read(ks, 32 * blk + 16 * u, d), f, acc[d]);
-      }
+      for (int r = 0; r < 16; ++r)
+        if (8 * (r >> 2) + (r & 3) >= mine) s[r] = 0.f;
     }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const frag f = pack8<T>(s, u);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) acc[d] = Mfma<T>::run(rx.read(ks, 16 * u, d), f, acc[d]);
+    }
+  };
+  for (int i = 0; i < count; i += 2) {
+    tile(i, std::integral_constant<int, 0>());
+    if (i + 1 < count) tile(i + 1, std::integral_constant<int, 1>());
   }
   if (p.q_parts > 1)
-    store_column_f32<ND>(p.dq_parts + (part * (int64_t)p.batch * p.q_len + tok_row) * p.heads * p.head_dim + at, p.head_dim, acc, p.scale, hi, valid);
+    store_column_f32<ND>(p.dq_parts + (part * (int64_t)p.batch * p.q_len + tok0 + c32) * p.heads * p.head_dim + at, p.head_dim, acc, p.scale, hi, valid);
   else
-    store_column<T, ND>((T*)p.dq + tok_row * p.ld_dq + at, p.head_dim, acc, p.scale, hi, valid);
+    WaveRows<HDP>::template store<T>((T*)p.dq + tok0 * p.ld_dq + at, p.ld_dq, p.head_dim, left_q, acc, p.scale, d_out_rows, lane);
 }
 
 template <typename T, int HDP>
@@ -158,8 +189,8 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dkv(CrossBwd p) {
   const int c32 = lane & 31, hi = lane >> 5;
   const int blocks = (p.kv_len + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES);
   const int t = xcd_order((int)blockIdx.x, (int)gridDim.x);
-  const int block = t % blocks, part = t / blocks % p.kv_parts, bk = t / blocks / p.kv_parts;
-  const int b = bk / p.kv_heads, kvh = bk - b * p.kv_heads, group = p.heads / p.kv_heads;
+  const int block = t % blocks, part = t / blocks % p.kv_parts, kb = t / blocks / p.kv_parts;
+  const int kvh = kb / p.batch, b = kb - kvh * p.batch, group = p.heads / p.kv_heads;
   const int n = states_of(p.kv_lens, b, p.kv_len);
   const int state0 = (block * BWD_WAVES + wave) * 32, state = state0 + c32;
   // tiles: those of the first head's tokens, the second's, ...

@@ -244,7 +244,7 @@ inline CrossPick pick_cross(int batch, int heads, int kv_heads, int head_dim, in
     pick.parts = (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 64}));
     return pick;
   }
-  const int per = head_dim <= 64 ? 256 : 128;
+  const int per = 128;
   pick.blocks = (q_len + per - 1) / per;
   const int64_t wgs = (int64_t)batch * heads * pick.blocks, tiles = ((int64_t)kv_len + 63) / 64;
   pick.parts = (int)std::max<int64_t>(1, std::min<int64_t>({2 * RULE_CUS / wgs, tiles / 4, 16}));
