@@ -113,36 +113,60 @@ void layernorm_x(const xema_layernorm_args& a, hipStream_t s) {
   }
 }
 
-// Eight elements of a type known at run time (the same for a whole launch).
-struct AnyRaw8 {
-  u32x4 v[2];
-  __device__ __forceinline__ void load(const void* p, int dtype, int64_t at) {
-    if (dtype == XEMA_F32) {
-      v[0] = reinterpret_cast<const u32x4*>((const float*)p + at)[0];
-      v[1] = reinterpret_cast<const u32x4*>((const float*)p + at)[1];
-    } else {
-      v[0] = *reinterpret_cast<const u32x4*>((const uint16_t*)p + at);
-    }
-  }
-  __device__ __forceinline__ void add_to(int dtype, float f[8]) const {
-    float d[8];
-    if (dtype == XEMA_F32) unpack8(Raw8<float>{{v[0], v[1]}}, d);
-    else if (dtype == XEMA_BF16) unpack8(Raw8<bf16>{{v[0]}}, d);
-    else unpack8(Raw8<f16>{{v[0]}}, d);
+// store8 with one branch, the 16-bit types by a choice of values.  (With two, hipcc
+// of ROCm 7.2 lost the gradient's running sums on the path to one of the stores.)
+__device__ __forceinline__ void put8(void* p, int dtype, int64_t at, const float f[8]) {
+  typedef bf16 b8 __attribute__((ext_vector_type(8)));
+  if (dtype == XEMA_F32) {
+    store8_as<float>(p, at, f);
+  } else {
+    b8 b;
+    f16x8 h;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] += d[e];
+    for (int e = 0; e < 8; ++e) {
+      b[e] = (bf16)f[e];
+      h[e] = (f16)f[e];
+    }
+    const u32x4 vb = __builtin_bit_cast(u32x4, b), vh = __builtin_bit_cast(u32x4, h);
+    u32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = dtype == XEMA_BF16 ? vb[e] : vh[e];
+    *reinterpret_cast<u32x4*>((uint16_t*)p + at) = v;
   }
-};
+}
 
-// The gradient.  Workgroup b takes the rows b, b + grid, ... (WPR = 4) or the
-// groups of four rows b, b + grid, ... (WPR = 1), holds its part of dgamma and
-// dbeta in registers over them and writes it once.  A row's s, dy and dsum are
-// loaded while the row before is computed.
-template <typename XT, typename DT, int NV>
+// Sum over each 16 lanes, by rotations, and over all 64 (the same in all, in a fixed order).
+__device__ __forceinline__ float lane_sum16(float v) {
+  auto turned = [](float x, auto ror) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), 0x120 + decltype(ror)::value, 0xf, 0xf, false));
+  };
+  v += turned(v, std::integral_constant<int, 8>());
+  v += turned(v, std::integral_constant<int, 4>());
+  v += turned(v, std::integral_constant<int, 2>());
+  return v + turned(v, std::integral_constant<int, 1>());
+}
+__device__ __forceinline__ float lane_sum(float v) {
+  v = lane_sum16(v);
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+
+// The gradient.  A workgroup has G groups of WPR waves, a row each at a time;
+// group i of them all takes the rows i, i + all groups, ..., holds its part of
+// dgamma and dbeta in registers over them, and the groups' parts are added in the
+// end and written once.  A row's s, dy and dsum are loaded while the row before is
+// computed.  Each wave takes its sums about its own mean, so that one exchange
+// joins them: for a wave of n elements with mean m, the row's mean is the
+// weighted mean M, its squares about M those about m and n (m - M)^2, and
+// sum g (s - M) = sum g (s - m) + (m - M) sum g.  ST void: no dsum.
+template <typename XT, typename DT, typename ST, int NV>
 struct LnBwdRow {
+  typedef std::conditional_t<std::is_void_v<ST>, bf16, ST> S;
   Raw8<XT> x[NV];
   Raw8<DT> d[NV];
-  AnyRaw8 ds[NV];
+  Raw8<S> ds[std::is_void_v<ST> ? 1 : NV];
   template <int STRIDE>
   __device__ __forceinline__ void load(const xema_layernorm_bwd_args& a, int64_t r, int in_row) {
 #pragma unroll
@@ -151,31 +175,59 @@ struct LnBwdRow {
       if (c < a.dim) {
         x[v] = load_raw8((const XT*)a.s + r * a.ld_s + c);
         d[v] = load_raw8((const DT*)a.dy + r * a.ld_dy + c);
-        if (a.dsum) ds[v].load(a.dsum, a.dsum_dtype, r * a.ld_dsum + c);
+        if constexpr (!std::is_void_v<ST>) ds[v] = load_raw8((const ST*)a.dsum + r * a.ld_dsum + c);
       }
     }
   }
 };
 
-template <typename XT, typename DT, int NV, int WPR>
-__global__ __launch_bounds__(LN_WAVES * 64) void k_layernorm_bwd(xema_layernorm_bwd_args a, float* __restrict__ partial) {
-  constexpr int STRIDE = 512 * WPR;
-  __shared__ float red[4][LN_WAVES];
-  __shared__ float fold[WPR == 1 ? LN_WAVES : 1][WPR == 1 ? NV * 512 : 1];
-  const int wave = threadIdx.x >> 6, in_row = WPR == 1 ? threadIdx.x & 63 : threadIdx.x;
+template <typename XT, typename DT, typename ST, int NV, int WPR, int G>
+__global__ __launch_bounds__(G * WPR * 64) void k_layernorm_bwd(xema_layernorm_bwd_args a, float* __restrict__ partial) {
+  constexpr int STRIDE = 512 * WPR, WAVES = G * WPR;
+  __shared__ __attribute__((aligned(16))) float red[2][WAVES][4];
+  __shared__ float fold[G > 1 ? G : 1][G > 1 ? NV * STRIDE : 1];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave / WPR, in_row = threadIdx.x - group * WPR * 64;
   const float n = (float)a.dim;
   float dg[NV][8], db[NV][8];
 #pragma unroll
   for (int v = 0; v < NV; ++v)
 #pragma unroll
     for (int e = 0; e < 8; ++e) dg[v][e] = db[v][e] = 0.f;
-  const int64_t first = WPR == 1 ? (int64_t)blockIdx.x * LN_WAVES + wave : (int64_t)blockIdx.x;
-  const int64_t step = (int64_t)gridDim.x * (WPR == 1 ? LN_WAVES : 1);
-  LnBwdRow<XT, DT, NV> next;
-  if (first < a.rows) next.template load<STRIDE>(a, first, in_row);
-  for (int64_t r = first; r < a.rows; r += step) {
-    const LnBwdRow<XT, DT, NV> row = next;
-    if (r + step < a.rows) next.template load<STRIDE>(a, r + step, in_row);
+  // gamma in registers over all rows, as they allow
+  constexpr bool KEEP = NV == 1;
+  float kept[8];
+  if constexpr (KEEP) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) kept[e] = 1.f;
+    if (a.gamma && in_row * 8 < a.dim) unpack8(load_raw8((const bf16*)a.gamma + in_row * 8), kept);
+  }
+  // g = dy * gamma of a lane's vector at column c
+  auto weigh = [&](int c, const float dy[8], float w[8]) {
+    float gam[8];
+    if (!KEEP && a.gamma) unpack8(load_raw8((const bf16*)a.gamma + c), gam);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = KEEP ? dy[e] * kept[e] : a.gamma ? dy[e] * gam[e] : dy[e];
+  };
+  // elements of a row that wave w of a group has
+  auto share = [&](int w) {
+    int k = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) k += max(0, min(512, a.dim - v * STRIDE - w * 512));
+    return (float)k;
+  };
+  const float mine = WPR == 1 ? n : fmaxf(share(wave % WPR), 1.f), theirs = (int)(threadIdx.x & 15) < WPR ? share(threadIdx.x & 15) : 0.f;
+  // (every wave meets every barrier: a group past the last row takes it again and keeps nothing)
+  const int64_t step = (int64_t)gridDim.x * G, first = (int64_t)blockIdx.x * G + group, turns = (a.rows + step - 1) / step;
+  // rows in flight, as the registers allow
+  constexpr int AHEAD = NV == 1 && WAVES == 8 && sizeof(XT) + sizeof(DT) + sizeof(typename LnBwdRow<XT, DT, ST, NV>::S) <= 8 ? 2 : 1;
+  LnBwdRow<XT, DT, ST, NV> next[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) next[i].template load<STRIDE>(a, first + i * step < a.rows ? first + i * step : a.rows - 1, in_row);
+  auto take = [&](int64_t turn, auto slot) {
+    LnBwdRow<XT, DT, ST, NV>& ahead = next[decltype(slot)::value];
+    const int64_t r = first + turn * step;
+    const LnBwdRow<XT, DT, ST, NV> row = ahead;
+    if (r + AHEAD * step < a.rows) ahead.template load<STRIDE>(a, r + AHEAD * step, in_row);
     float total = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -186,82 +238,86 @@ __global__ __launch_bounds__(LN_WAVES * 64) void k_layernorm_bwd(xema_layernorm_
         for (int e = 0; e < 8; ++e) total += x[e];
       }
     }
-    // (a row's second use of `red` is apart from its first, and the next row's
-    // first comes after every wave has read this one's)
-    const float mean = row_sum<WPR>(total, red[0], wave) / n;
-    float ss = 0.f, sg = 0.f, sgx = 0.f;
+    float mean = lane_sum(total) / mine, ss = 0.f, sg = 0.f, sgx = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = v * STRIDE + in_row * 8;
       if (c < a.dim) {
-        float x[8], g[8], gam[8];
+        float x[8], g[8], w[8];
         unpack8(row.x[v], x);
         unpack8(row.d[v], g);
-        if (a.gamma) unpack8(load_raw8((const bf16*)a.gamma + c), gam);
+        weigh(c, g, w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float d = x[e] - mean, w = a.gamma ? g[e] * gam[e] : g[e];
+          const float d = x[e] - mean;
           ss = fmaf(d, d, ss);
-          sg += w;
-          sgx = fmaf(w, d, sgx);
+          sg += w[e];
+          sgx = fmaf(w[e], d, sgx);
         }
       }
     }
-    ss = wave_sum(ss);
-    sg = wave_sum(sg);
-    sgx = wave_sum(sgx);
+    ss = lane_sum(ss);
+    sg = lane_sum(sg);
+    sgx = lane_sum(sgx);
     if constexpr (WPR > 1) {
-      if ((threadIdx.x & 63) == 0) {
-        red[1][wave] = ss;
-        red[2][wave] = sg;
-        red[3][wave] = sgx;
-      }
-      __syncthreads();
-      ss = sg = sgx = 0.f;
-#pragma unroll
-      for (int w = 0; w < WPR; ++w) {
-        ss += red[1][w];
-        sg += red[2][w];
-        sgx += red[3][w];
-      }
+      float(*const at)[4] = red[turn & 1];
+      if ((threadIdx.x & 63) == 0) *reinterpret_cast<f32x4*>(at[wave]) = f32x4{mean, ss, sg, sgx};
+      __syncthreads();   // (the next row writes the other half)
+      // (lane i of each 16 joins wave i's; one of no elements left zeros)
+      const int i = threadIdx.x & 15;
+      const f32x4 w = i < WPR ? *reinterpret_cast<const f32x4*>(at[group * WPR + i]) : f32x4{0.f, 0.f, 0.f, 0.f};
+      mean = lane_sum16(w[0] * theirs) / n;
+      const float off = theirs > 0.f ? w[0] - mean : 0.f;
+      ss = lane_sum16(fmaf(theirs * off, off, w[1]));
+      sg = lane_sum16(w[2]);
+      sgx = lane_sum16(fmaf(w[2], off, w[3]));
     }
     const float q = 1.0f / sqrtf(ss / n + a.eps);
     const float along = sgx * q / n, level = sg / n;      // mean(g n), mean(g)
+    if (r < a.rows) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int c = v * STRIDE + in_row * 8;
-      if (c < a.dim) {
-        float x[8], g[8], gam[8], o[8];
-        unpack8(row.x[v], x);
-        unpack8(row.d[v], g);
-        if (a.gamma) unpack8(load_raw8((const bf16*)a.gamma + c), gam);
+      for (int v = 0; v < NV; ++v) {
+        const int c = v * STRIDE + in_row * 8;
+        if (c < a.dim) {
+          float x[8], g[8], o[8], ds[8];
+          unpack8(row.x[v], x);
+          unpack8(row.d[v], g);
+          weigh(c, g, o);
+          if constexpr (!std::is_void_v<ST>) unpack8(row.ds[v], ds);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float norm = (x[e] - mean) * q;
-          dg[v][e] = fmaf(g[e], norm, dg[v][e]);
-          db[v][e] += g[e];
-          o[e] = q * ((a.gamma ? g[e] * gam[e] : g[e]) - level - norm * along);
+          for (int e = 0; e < 8; ++e) {
+            const float norm = (x[e] - mean) * q;
+            dg[v][e] = fmaf(g[e], norm, dg[v][e]);
+            db[v][e] += g[e];
+            const float t = fmaf(-along, norm, o[e] - level);
+            o[e] = std::is_void_v<ST> ? q * t : fmaf(q, t, ds[e]);
+          }
+          put8(a.dx, a.dx_dtype, r * a.ld_dx + c, o);
         }
-        if (a.dsum) row.ds[v].add_to(a.dsum_dtype, o);
-        store8(a.dx, a.dx_dtype, r * a.ld_dx + c, o);
       }
+    }
+  };
+  for (int64_t turn = 0; turn < turns; turn += AHEAD) {
+    take(turn, std::integral_constant<int, 0>());
+    if constexpr (AHEAD > 1) {
+      if (turn + 1 < turns) take(turn + 1, std::integral_constant<int, 1>());
     }
   }
   if (!partial) return;
   float* const out = partial + (int64_t)blockIdx.x * 2 * a.dim;
-  if constexpr (WPR == 1) {
+  if constexpr (G > 1) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       if (h) __syncthreads();
 #pragma unroll
       for (int v = 0; v < NV; ++v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) fold[wave][v * 512 + in_row * 8 + e] = h ? db[v][e] : dg[v][e];
+        for (int e = 0; e < 8; ++e) fold[group][v * STRIDE + in_row * 8 + e] = h ? db[v][e] : dg[v][e];
       __syncthreads();
-      for (int c = threadIdx.x; c < a.dim; c += LN_WAVES * 64) {
+      for (int c = threadIdx.x; c < a.dim; c += WAVES * 64) {
         float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < LN_WAVES; ++w) s += fold[w][c];
+        for (int w = 0; w < G; ++w) s += fold[w][c];
         out[(int64_t)h * a.dim + c] = s;
       }
     }
@@ -300,26 +356,41 @@ __global__ __launch_bounds__(1024) void k_layernorm_sums(const float* __restrict
   if (out) out[c < dim ? c : c - dim] = s;
 }
 
-template <typename XT, typename DT, int WPR>
-void layernorm_bwd_nv(const xema_layernorm_bwd_args& a, float* partial, hipStream_t s) {
-  const dim3 grid((unsigned)layernorm_bwd_partials(a.rows)), block(LN_WAVES * 64);
-  const int nv = (a.dim + 512 * WPR - 1) / (512 * WPR);
-  if (nv <= 1) hipLaunchKernelGGL((k_layernorm_bwd<XT, DT, 1, WPR>), grid, block, 0, s, a, partial);
-  else if (nv <= 2) hipLaunchKernelGGL((k_layernorm_bwd<XT, DT, 2, WPR>), grid, block, 0, s, a, partial);
-  else if (nv <= 4) hipLaunchKernelGGL((k_layernorm_bwd<XT, DT, 4, WPR>), grid, block, 0, s, a, partial);
-  else if constexpr (WPR > 1) hipLaunchKernelGGL((k_layernorm_bwd<XT, DT, 8, WPR>), grid, block, 0, s, a, partial);
+// Sixteen waves, eight elements a lane, a row to as many waves as it needs: a
+// workgroup fills a CU, so that the parts of dgamma and dbeta are few.  Returns
+// those parts.
+template <typename XT, typename DT, typename ST, int NV, int WPR, int G>
+int layernorm_bwd_run(const xema_layernorm_bwd_args& a, float* partial, hipStream_t s) {
+  const int parts = (int)std::min<int64_t>(layernorm_bwd_partials(a.rows), (a.rows + G - 1) / G);
+  hipLaunchKernelGGL((k_layernorm_bwd<XT, DT, ST, NV, WPR, G>), dim3(parts), dim3(G * WPR * 64), 0, s, a, partial);
+  return parts;
+}
+template <typename XT, typename DT, typename ST>
+int layernorm_bwd_t(const xema_layernorm_bwd_args& a, float* partial, hipStream_t s) {
+  if (a.dim <= 512) return layernorm_bwd_run<XT, DT, ST, 1, 1, 8>(a, partial, s);
+  if (a.dim <= 1024) return layernorm_bwd_run<XT, DT, ST, 1, 2, 4>(a, partial, s);
+  if (a.dim <= 2048) return layernorm_bwd_run<XT, DT, ST, 1, 4, 2>(a, partial, s);
+  if (a.dim <= 4096) return layernorm_bwd_run<XT, DT, ST, 1, 8, 1>(a, partial, s);
+  if (a.dim <= 8192) return layernorm_bwd_run<XT, DT, ST, 1, 16, 1>(a, partial, s);
+  // (more a lane, in eight waves: sixteen have too few registers)
+  return layernorm_bwd_run<XT, DT, ST, 4, 8, 1>(a, partial, s);
 }
 template <typename XT, typename DT>
-void layernorm_bwd_t(const xema_layernorm_bwd_args& a, float* partial, hipStream_t s) {
-  if (a.dim <= 2048) layernorm_bwd_nv<XT, DT, 1>(a, partial, s);
-  else layernorm_bwd_nv<XT, DT, LN_WAVES>(a, partial, s);
+int layernorm_bwd_d(const xema_layernorm_bwd_args& a, float* partial, hipStream_t s) {
+  if (!a.dsum) return layernorm_bwd_t<XT, DT, void>(a, partial, s);
+  switch (a.dsum_dtype) {
+    case XEMA_BF16: return layernorm_bwd_t<XT, DT, bf16>(a, partial, s);
+    case XEMA_F16: return layernorm_bwd_t<XT, DT, f16>(a, partial, s);
+    default: return layernorm_bwd_t<XT, DT, float>(a, partial, s);
+  }
 }
+// Returns the parts of dgamma and dbeta that it leaves.
 template <typename XT>
-void layernorm_bwd_x(const xema_layernorm_bwd_args& a, float* partial, hipStream_t s) {
+int layernorm_bwd_x(const xema_layernorm_bwd_args& a, float* partial, hipStream_t s) {
   switch (a.dy_dtype) {
-    case XEMA_BF16: return layernorm_bwd_t<XT, bf16>(a, partial, s);
-    case XEMA_F16: return layernorm_bwd_t<XT, f16>(a, partial, s);
-    default: return layernorm_bwd_t<XT, float>(a, partial, s);
+    case XEMA_BF16: return layernorm_bwd_d<XT, bf16>(a, partial, s);
+    case XEMA_F16: return layernorm_bwd_d<XT, f16>(a, partial, s);
+    default: return layernorm_bwd_d<XT, float>(a, partial, s);
   }
 }
 
@@ -334,18 +405,17 @@ hipError_t launch_layernorm(const xema_layernorm_args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-int64_t layernorm_bwd_partials(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(1024, (rows + 3) / 4)); }
+int64_t layernorm_bwd_partials(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(512, rows)); }
 
 hipError_t launch_layernorm_bwd(const xema_layernorm_bwd_args& a, hipStream_t s) {
   const bool sums = a.dgamma || a.dbeta;
   float* partial = sums ? (float*)a.workspace : nullptr;
   int parts = 0;
   if (a.rows > 0) {
-    parts = (int)layernorm_bwd_partials(a.rows);
     switch (a.s_dtype) {
-      case XEMA_BF16: layernorm_bwd_x<bf16>(a, partial, s); break;
-      case XEMA_F16: layernorm_bwd_x<f16>(a, partial, s); break;
-      default: layernorm_bwd_x<float>(a, partial, s); break;
+      case XEMA_BF16: parts = layernorm_bwd_x<bf16>(a, partial, s); break;
+      case XEMA_F16: parts = layernorm_bwd_x<f16>(a, partial, s); break;
+      default: parts = layernorm_bwd_x<float>(a, partial, s); break;
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -67,6 +67,34 @@ def test_gradient(rows, dim, st, dt, at, ot):
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(kept, (dx, dgamma, dbeta)))
 
 
+@pytest.mark.parametrize("dim", [264, 520, 1032, 2056, 4104, 8200])
+def test_every_type_at_every_width_of_waves(dim):
+    """All types of every argument, for each number of waves that a row takes."""
+    rows, types = 19, (BF16, F16, F32)
+    g = gen(dim)
+    gamma, beta = normal(g, (dim,), 0.3, mean=1.0), normal(g, (dim,), 0.3)
+    s, dy, dsum = ({t: normal(g, (rows, dim), std, t, mean) for t in types} for std, mean in ((2.0, -0.7), (0.5, 0.1), (0.3, 0.0)))
+    for st in types:
+        for dt in types:
+            for at in (None, *types):
+                want = R.layernorm_bwd(s[st], dy[dt], dsum[at] if at else None, gamma, 1e-5)
+                for ot in types:
+                    dx, dg, db = empty(rows, dim, 0, ot), torch.full((dim,), 7.0, device=DEV), torch.full((dim,), 7.0, device=DEV)
+                    run_bwd(s[st], dy[dt], dsum[at] if at else None, gamma, 1e-5, dx, dg, db, dim)
+                    R.within(dx, want["dx"][0], R.rounded(*want["dx"], ot), ("dx", st, dt, at, ot))
+                    R.within(dg, *want["dgamma"], ("dgamma", st, dt, at, ot))
+                    R.within(db, *want["dbeta"], ("dbeta", st, dt, at, ot))
+            for yt in types:
+                for sumt in (None, *types):
+                    y, total = empty(rows, dim, 0, yt), empty(rows, dim, 0, sumt) if sumt else None
+                    for r in (None, dy[dt]):
+                        run(s[st], r, gamma, beta, 1e-5, y, dim, total)
+                        want_s, want, err = R.layernorm(s[st], r, gamma, beta, 1e-5)
+                        R.within(y, want, R.rounded(want, err, yt), ("y", st, dt, yt))
+                        if sumt:
+                            R.within(total, want_s, R.rounded(want_s, R.U * want_s.abs(), sumt), ("sum", st, dt, sumt))
+
+
 def test_gradient_against_differences():
     """The formula's own gradient in 64 bits meets central differences of sum(dy * y) + sum(dsum * s)."""
     g = gen(5)
