@@ -208,16 +208,17 @@ __global__ __launch_bounds__(CROSS_WAVES * 64, HDP <= 64 ? 4 : 3) void k_cross(C
 }
 
 constexpr int FT = 32;                 // states per tile of a wave of k_cross_few
+constexpr int FEW_WAVES = 2;
 
 template <typename T, int HDP>
-__global__ __launch_bounds__(CROSS_WAVES * 64) void k_cross_few(CrossParams p) {
+__global__ __launch_bounds__(FEW_WAVES * 64) void k_cross_few(CrossParams p) {
   typedef Rows<HDP> R;
   typedef typename Mfma<T>::frag frag;
   constexpr int KK = R::KK, ND = R::ND, TILE = FT * R::RB, STAGE = 2 * TILE, LOADS = 2 * TileLoads<HDP, FT, 1>::LOADS;
   constexpr int ROW = HDP + 4;                   // fp32 of a column where the waves' sums meet (padded against bank conflicts)
-  constexpr int LDS = CROSS_WAVES * (2 * STAGE > 32 * ROW * 4 ? 2 * STAGE : 32 * ROW * 4);
+  constexpr int LDS = FEW_WAVES * (2 * STAGE > 32 * ROW * 4 ? 2 * STAGE : 32 * ROW * 4);
   __shared__ __attribute__((aligned(1024))) uint8_t smem[LDS];
-  __shared__ float2 ml[CROSS_WAVES][32];
+  __shared__ float2 ml[FEW_WAVES][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c32 = lane & 31, hi = lane >> 5;
   // workgroup -> (batch, state head, block of queries, part)
@@ -225,10 +226,18 @@ __global__ __launch_bounds__(CROSS_WAVES * 64) void k_cross_few(CrossParams p) {
   const int part = t % p.parts, block = t / p.parts % p.blocks, bk = t / p.parts / p.blocks;
   const int b = bk / p.kv_heads, kvh = bk - b * p.kv_heads, group = p.heads / p.kv_heads;
   const int n = states_of(p.kv_lens, b, p.kv_len), tiles = (n + FT - 1) / FT;
-  int first, count;
-  part_of(tiles, part, p.parts, &first, &count);
-  // this wave's tiles: first + wave, first + wave + CROSS_WAVES, ...
-  const int mine = (count - wave + CROSS_WAVES - 1) / CROSS_WAVES;
+  // parts of kv_len, so that a short sequence has few: the rest leave an empty sum
+  const int each = ((p.kv_len + FT - 1) / FT + p.parts - 1) / p.parts, first = part * each, count = min(each, tiles - first);
+  if (count <= 0 && p.parts > 1) {
+    const int r = block * 32 + (int)threadIdx.x, rows = p.q_len * group;
+    if ((int)threadIdx.x < 32 && r < rows) {
+      const int token = r / group, h = kvh * group + r - token * group;
+      p.part_ml[part * p.rows + ((int64_t)b * p.heads + h) * p.q_len + token] = float2{LOWEST, 0.f};
+    }
+    return;
+  }
+  // this wave's tiles: first + wave, first + wave + FEW_WAVES, ...
+  const int mine = max(count - wave + FEW_WAVES - 1, 0) / FEW_WAVES;
 
   uint8_t* const stages = smem + wave * 2 * STAGE;
   const uint32_t ldk = (uint32_t)p.ldk * 2, ldv = (uint32_t)p.ldv * 2;
@@ -240,7 +249,7 @@ __global__ __launch_bounds__(CROSS_WAVES * 64) void k_cross_few(CrossParams p) {
   lv.init(ldv, p.head_dim, 0, lane);
   // (tiles past the wave's last have no states: their loads read nothing)
   auto issue = [&](int i) {
-    const int64_t at = i < mine ? (int64_t)(first + wave + i * CROSS_WAVES) * FT : n;
+    const int64_t at = i < mine ? (int64_t)(first + wave + i * FEW_WAVES) * FT : n;
     uint8_t* const st = stages + (i & 1) * STAGE;
     lk.issue((const uint8_t*)(kh + at * p.ldk), ldk, n - (int)at, st, 0);
     lv.issue((const uint8_t*)(vh + at * p.ldv), ldv, n - (int)at, st + TILE, 0);
@@ -268,7 +277,7 @@ __global__ __launch_bounds__(CROSS_WAVES * 64) void k_cross_few(CrossParams p) {
     f32x16 s[1];
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) s[0] = Mfma<T>::run(rk.read(ks, 0, kk), qf[kk], kk ? s[0] : f32x16{});
-    const int here = n - (first + wave + i * CROSS_WAVES) * FT;
+    const int here = n - (first + wave + i * FEW_WAVES) * FT;
     if (here < FT) mask_from<1>(s, here, hi);
     col.template weigh<1>(s, p.c, i == 0);
 #pragma unroll
@@ -291,25 +300,26 @@ __global__ __launch_bounds__(CROSS_WAVES * 64) void k_cross_few(CrossParams p) {
   float* const sums = (float*)smem;
   float top = LOWEST;
 #pragma unroll
-  for (int w = 0; w < CROSS_WAVES; ++w) top = fmaxf(top, ml[w][c32].x);
+  for (int w = 0; w < FEW_WAVES; ++w) top = fmaxf(top, ml[w][c32].x);
   store_column_f32<ND>(sums + (wave * 32 + c32) * ROW, HDP, col.o, __builtin_amdgcn_exp2f(col.m - top), hi, true);
   __syncthreads();
-  // eight threads a query, four columns each at a time
-  const int q = (int)threadIdx.x / 8, at = block * 32 + q;
+  // THREADS threads a query, four columns each at a time
+  constexpr int THREADS = FEW_WAVES * 2;
+  const int q = (int)threadIdx.x / THREADS, at = block * 32 + q;
   if (at >= rows) return;
   float m = LOWEST, sum = 0.f;
 #pragma unroll
-  for (int w = 0; w < CROSS_WAVES; ++w) m = fmaxf(m, ml[w][q].x);
+  for (int w = 0; w < FEW_WAVES; ++w) m = fmaxf(m, ml[w][q].x);
 #pragma unroll
-  for (int w = 0; w < CROSS_WAVES; ++w) sum += ml[w][q].y * __builtin_amdgcn_exp2f(ml[w][q].x - m);
+  for (int w = 0; w < FEW_WAVES; ++w) sum += ml[w][q].y * __builtin_amdgcn_exp2f(ml[w][q].x - m);
   const int tq = at / group, hq = kvh * group + at - tq * group;
   const int64_t row = ((int64_t)b * p.heads + hq) * p.q_len + tq, prow = part * p.rows + row;
   T* const orow = (T*)p.o + ((int64_t)b * p.q_len + tq) * p.ldo + (int64_t)hq * p.head_dim;
   const float f = p.parts > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
-  for (int e = ((int)threadIdx.x & 7) * 4; e < p.head_dim; e += 32) {
+  for (int e = (int)threadIdx.x % THREADS * 4; e < p.head_dim; e += 4 * THREADS) {
     f32x4 v = *reinterpret_cast<const f32x4*>(sums + q * ROW + e);
 #pragma unroll
-    for (int w = 1; w < CROSS_WAVES; ++w) v += *reinterpret_cast<const f32x4*>(sums + (w * 32 + q) * ROW + e);
+    for (int w = 1; w < FEW_WAVES; ++w) v += *reinterpret_cast<const f32x4*>(sums + (w * 32 + q) * ROW + e);
     if (p.parts > 1) {
       *reinterpret_cast<f32x4*>(p.part_o + prow * p.head_dim + e) = v;
     } else {
@@ -320,47 +330,59 @@ __global__ __launch_bounds__(CROSS_WAVES * 64) void k_cross_few(CrossParams p) {
       *reinterpret_cast<t4*>(orow + e) = o;
     }
   }
-  if (threadIdx.x & 7) return;
+  if (threadIdx.x % THREADS) return;
   if (p.parts > 1) p.part_ml[prow] = float2{m, sum};
   else if (p.lse) p.lse[row] = lse_of(m, sum);
 }
 
-// The parts of a (batch, head, token)'s sums, joined in order: 16 threads a row, eight columns each.
+// The parts of a (batch, head, token)'s sums (up to 64), joined in a fixed order: a
+// workgroup a row, a lane a part's maximum and sum, then sixteen threads a part,
+// eight columns each, sixteen parts at a time.
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
 template <typename T>
 __global__ __launch_bounds__(256) void k_cross_join(CrossParams p) {
-  const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
-  if (row >= p.rows) return;
-  float m = LOWEST, sum = 0.f;
-  for (int i = 0; i < p.parts; ++i) m = fmaxf(m, p.part_ml[i * p.rows + row].x);
-  for (int i = 0; i < p.parts; ++i) {
-    const float2 ml = p.part_ml[i * p.rows + row];
-    sum += ml.y * __builtin_amdgcn_exp2f(ml.x - m);
-  }
-  const int64_t bh = row / p.q_len, token = row - bh * p.q_len, b = bh / p.heads, h = bh - b * p.heads;
-  const float f = sum == 0.f ? 0.f : 1.f / sum;
-  const int e = ((int)threadIdx.x & 15) * 8;
-  if (e == 0 && p.lse) p.lse[row] = lse_of(m, sum);
-  if (e >= p.head_dim) return;
+  __shared__ __attribute__((aligned(16))) float sums[16][128];
+  const int64_t row = blockIdx.x;
+  const int lane = threadIdx.x & 63, e = ((int)threadIdx.x & 15) * 8, first = (int)threadIdx.x / 16;
+  const float2 ml = lane < p.parts ? p.part_ml[lane * p.rows + row] : float2{LOWEST, 0.f};
+  const float m = wave_max(ml.x), w = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - m), sum = wave_sum(ml.y * w);
   f32x4 v[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-#pragma unroll 4
-  for (int i = 0; i < p.parts; ++i) {
-    const float w = __builtin_amdgcn_exp2f(p.part_ml[i * p.rows + row].x - m);
-    const f32x4* const at = reinterpret_cast<const f32x4*>(p.part_o + (i * p.rows + row) * p.head_dim + e);
+  for (int i0 = 0; i0 < p.parts; i0 += 16) {
+    const int i = i0 + first;
+    const float f = __shfl(w, i & 63, 64);
+    // (a part of no weight may not have been written)
+    if (i < p.parts && f != 0.f && e < p.head_dim) {
+      const f32x4* const at = reinterpret_cast<const f32x4*>(p.part_o + (i * p.rows + row) * p.head_dim + e);
 #pragma unroll
-    for (int x = 0; x < 2; ++x) v[x] += at[x] * w;
+      for (int x = 0; x < 2; ++x) v[x] += at[x] * f;
+    }
   }
-  typedef T t8 __attribute__((ext_vector_type(8)));
-  t8 o;
 #pragma unroll
-  for (int x = 0; x < 8; ++x) o[x] = (T)(v[x / 4][x % 4] * f);
-  *reinterpret_cast<t8*>((T*)p.o + (b * p.q_len + token) * p.ldo + h * p.head_dim + e) = o;
+  for (int x = 0; x < 2; ++x) *reinterpret_cast<f32x4*>(&sums[first][e + 4 * x]) = v[x];
+  __syncthreads();
+  if (threadIdx.x == 0 && p.lse) p.lse[row] = lse_of(m, sum);
+  const int c = (int)threadIdx.x * 2;
+  if (c >= p.head_dim) return;
+  float o[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) o[x] += sums[i][c + x];
+  const int64_t bh = row / p.q_len, token = row - bh * p.q_len, b = bh / p.heads, h = bh - b * p.heads;
+  typedef T t2 __attribute__((ext_vector_type(2)));
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
+  *reinterpret_cast<t2*>((T*)p.o + (b * p.q_len + token) * p.ldo + h * p.head_dim + c) = t2{(T)(o[0] * f), (T)(o[1] * f)};
 }
 
 template <typename T, int HDP>
 hipError_t run_cross(CrossParams p, const CrossPick& pick, hipStream_t s) {
   p.blocks = pick.blocks;
   const unsigned wgs = (unsigned)((int64_t)p.batch * (pick.few ? p.kv_heads : p.heads) * pick.blocks * pick.parts);
-  if (pick.few) hipLaunchKernelGGL((k_cross_few<T, HDP>), dim3(wgs), dim3(CROSS_WAVES * 64), 0, s, p);
+  if (pick.few) hipLaunchKernelGGL((k_cross_few<T, HDP>), dim3(wgs), dim3(FEW_WAVES * 64), 0, s, p);
   else hipLaunchKernelGGL((k_cross<T, HDP>), dim3(wgs), dim3(CROSS_WAVES * 64), 0, s, p);
   return hipGetLastError();
 }
@@ -373,7 +395,7 @@ hipError_t cross_t(const CrossParams& p, const CrossPick& pick, hipStream_t s) {
   else if (p.head_dim <= 96) e = run_cross<T, 96>(p, pick, s);
   else e = run_cross<T, 128>(p, pick, s);
   if (e != hipSuccess || p.parts == 1) return e;
-  hipLaunchKernelGGL((k_cross_join<T>), dim3((unsigned)((p.rows + 15) / 16)), dim3(256), 0, s, p);
+  hipLaunchKernelGGL((k_cross_join<T>), dim3((unsigned)p.rows), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

@@ -105,11 +105,16 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_linear(LinearParams p) {
         for (int e = 0; e < 4; ++e) v[j][e] = activate<false>(v[j][e], p.act, nullptr);
       }
       if (p.resid && in) add4(p.resid, p.resid_dtype, m * p.ld_resid + col, v[j]);
-      if constexpr (sizeof(YT) == 4) {
-        if (in) *reinterpret_cast<f32x4*>((float*)p.y + m * p.ldy + col) = f32x4{v[j][0], v[j][1], v[j][2], v[j][3]};
-      }
     }
-    if constexpr (sizeof(YT) == 2) store_row<YT, S::NJ>((YT*)p.y + (valid ? m : 0) * p.ldy, nw, p.out_dim, v, l4, valid);
+    if constexpr (sizeof(YT) == 4) {
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j) {
+        const int col = nw + 16 * j + 4 * l4;
+        if (valid && col < p.out_dim) *reinterpret_cast<f32x4*>((float*)p.y + m * p.ldy + col) = f32x4{v[j][0], v[j][1], v[j][2], v[j][3]};
+      }
+    } else {
+      store_row<YT, S::NJ>((YT*)p.y + (valid ? m : 0) * p.ldy, nw, p.out_dim, v, l4, valid);
+    }
   }
 }
 
@@ -192,7 +197,20 @@ hipError_t linear_t(const LinearParams& p, hipStream_t s) {
     return run_linear_few<T, YT, 4, 2, 1>(p, s);
   }
   if (few.cols16 == 4) return few.rows16 == 1 ? run_linear_few<T, YT, 1, 4, 1>(p, s) : run_linear_few<T, YT, 2, 4, 1>(p, s);
-  return with_tile(pick_tile(p.rows, p.out_dim, (p.dim * 2 + KB - 1) / KB), [&](auto shape) { return run_linear<T, YT, decltype(shape)>(p, s); });
+  const FfnRows pick = pick_rows(p.rows, p.out_dim, (p.dim * 2 + KB - 1) / KB);
+  LinearParams rest = p;
+  if (pick.rows) {
+    LinearParams first = p;
+    first.rows = pick.rows;
+    const hipError_t e = run_linear<T, YT, Tile256x256>(first, s);
+    if (e != hipSuccess) return e;
+    rest.rows -= pick.rows;
+    rest.x = (const T*)p.x + pick.rows * p.ldx;
+    rest.y = (YT*)p.y + pick.rows * p.ldy;
+    if (p.resid) rest.resid = (const uint8_t*)p.resid + pick.rows * p.ld_resid * (p.resid_dtype == XEMA_F32 ? 4 : 2);
+    if (p.pre) rest.pre = (uint8_t*)p.pre + pick.rows * p.out_dim / 4 * Z_GROUP;
+  }
+  return with_tile(pick.rest, [&](auto shape) { return run_linear<T, YT, decltype(shape)>(rest, s); });
 }
 template <typename T>
 hipError_t linear_y(const LinearParams& p, int y_dtype, hipStream_t s) {

@@ -152,6 +152,24 @@ inline FfnTile pick_tile(int64_t m, int64_t n, int64_t steps) {
   return (FfnTile)best;
 }
 
+// Rows of a product in two launches: the first `rows` in tiles of 256 x 256, as many
+// whole rounds of them as there are, and the rest in a tile that finishes soonest
+// (a second launch costs 3 us).  Every tile sums in the same order, so the values
+// do not depend on it.
+struct FfnRows { int64_t rows; FfnTile rest; };
+inline FfnRows pick_rows(int64_t m, int64_t n, int64_t steps) {
+  FfnRows best{0, pick_tile(m, n, steps)};
+  double least = ffn_tile_us(kFfnCost[best.rest], m, n, steps);
+  const int64_t whole = m / 256;
+  for (int64_t k = whole; k > 0 && k > whole - 48; --k) {
+    if (k * 256 == m) continue;
+    const FfnTile t = pick_tile(m - k * 256, n, steps);
+    const double us = ffn_tile_us(kFfnCost[FFN_256x256], k * 256, n, steps) + 3.0 + ffn_tile_us(kFfnCost[t], m - k * 256, n, steps);
+    if (us < least) { best = {k * 256, t}; least = us; }
+  }
+  return best;
+}
+
 // A product whose k may be split: `parts` sums over consecutive steps, kept in
 // fp32 and added by a launch of their own (3 us, and the sums' bytes at about 7
 // TB/s there and back, for most stay in the caches).  For small results of long k
@@ -233,6 +251,7 @@ inline ReducePick pick_reduce(int64_t rows, int rank) {
 // few: the kernel of single tokens, whose blocks are 32 queries of all heads that
 // share a state's head; otherwise blocks of a head's queries, 256 to a workgroup
 // at head dims to 64 and 128 past that.  parts: of the states.
+constexpr int FEW_WGS = 2 * RULE_CUS;
 struct CrossPick { bool few; int blocks, parts; };
 inline CrossPick pick_cross(int batch, int heads, int kv_heads, int head_dim, int q_len, int kv_len) {
   const int64_t rows = (int64_t)q_len * (heads / kv_heads);
@@ -240,8 +259,7 @@ inline CrossPick pick_cross(int batch, int heads, int kv_heads, int head_dim, in
   if (pick.few) {
     pick.blocks = (int)((rows + 31) / 32);
     const int64_t wgs = (int64_t)batch * kv_heads * pick.blocks, most = ((int64_t)kv_len + 255) / 256;
-    const int64_t want = (RULE_CUS * (head_dim <= 64 ? 2 : 1) + wgs - 1) / wgs;
-    pick.parts = (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 64}));
+    pick.parts = (int)std::max<int64_t>(1, std::min<int64_t>({(FEW_WGS + wgs - 1) / wgs, most, 64}));
     return pick;
   }
   const int per = 128;
