@@ -237,6 +237,23 @@ __device__ __forceinline__ void store_column_f32(float* row, int head_dim, const
     }
 }
 
+// Division by a number that the host knows, in scalar instructions: the product
+// with floor(2^32 / d) is the quotient or one less (n below 2^31).
+struct Divisor {
+  uint32_t d, m;
+  Divisor() = default;
+  explicit Divisor(int64_t by) : d((uint32_t)by), m(by == 1 ? 0xffffffffu : (uint32_t)(((uint64_t)1 << 32) / (uint64_t)by)) {}
+  __device__ __forceinline__ int divide(int n, int* rest) const {
+    uint32_t q = __umulhi((uint32_t)n, m), r = (uint32_t)n - q * d;
+    if (r >= d) {
+      ++q;
+      r -= d;
+    }
+    *rest = (int)r;
+    return (int)q;
+  }
+};
+
 // Workgroup wg of `total` in an order that gives each XCD (wg % 8) a contiguous
 // range, so that workgroups that share operands share an L2.
 __device__ __forceinline__ int xcd_order(int wg, int total) {

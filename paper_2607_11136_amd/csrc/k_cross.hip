@@ -38,6 +38,7 @@ struct CrossParams {
   int64_t ldq, ldk, ldv, ldo;
   int64_t rows;                        // batch * heads * q_len
   int batch, heads, kv_heads, head_dim, q_len, kv_len, parts, blocks;     // blocks of queries of a head
+  Divisor by_blocks, by_parts, by_batch, by_kv_heads, by_group;
   float c;                             // scale * log2(e)
 };
 
@@ -122,8 +123,8 @@ __global__ __launch_bounds__(CROSS_WAVES * 64, HDP <= 64 ? 4 : 3) void k_cross(C
   // workgroup -> (head, batch, part, block of queries): an XCD's range holds all
   // sequences of its heads, whose lengths may differ
   const int t = xcd_order((int)blockIdx.x, (int)gridDim.x);
-  const int block = t % p.blocks, part = t / p.blocks % p.parts, hb = t / p.blocks / p.parts;
-  const int h = hb / p.batch, b = hb - h * p.batch, kvh = h / (p.heads / p.kv_heads);
+  int block, part, b, rest;
+  const int h = p.by_batch.divide(p.by_parts.divide(p.by_blocks.divide(t, &block), &part), &b), kvh = p.by_group.divide(h, &rest);
   const int n = states_of(p.kv_lens, b, p.kv_len), tiles = (n + KT - 1) / KT;
   int first, count;
   part_of(tiles, part, p.parts, &first, &count);
@@ -223,15 +224,16 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_cross_few(CrossParams p) {
   const int c32 = lane & 31, hi = lane >> 5;
   // workgroup -> (batch, state head, block of queries, part)
   const int t = (int)blockIdx.x;
-  const int part = t % p.parts, block = t / p.parts % p.blocks, bk = t / p.parts / p.blocks;
-  const int b = bk / p.kv_heads, kvh = bk - b * p.kv_heads, group = p.heads / p.kv_heads;
+  int part, block, kvh;
+  const int b = p.by_kv_heads.divide(p.by_blocks.divide(p.by_parts.divide(t, &part), &block), &kvh), group = (int)p.by_group.d;
   const int n = states_of(p.kv_lens, b, p.kv_len), tiles = (n + FT - 1) / FT;
   // parts of kv_len, so that a short sequence has few: the rest leave an empty sum
   const int each = ((p.kv_len + FT - 1) / FT + p.parts - 1) / p.parts, first = part * each, count = min(each, tiles - first);
   if (count <= 0 && p.parts > 1) {
     const int r = block * 32 + (int)threadIdx.x, rows = p.q_len * group;
     if ((int)threadIdx.x < 32 && r < rows) {
-      const int token = r / group, h = kvh * group + r - token * group;
+      int g;
+      const int token = p.by_group.divide(r, &g), h = kvh * group + g;
       p.part_ml[part * p.rows + ((int64_t)b * p.heads + h) * p.q_len + token] = float2{LOWEST, 0.f};
     }
     return;
@@ -259,7 +261,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_cross_few(CrossParams p) {
 
   // query r of the block: token r / group of the head kvh * group + r % group
   const int r0 = block * 32 + c32, rows = p.q_len * group;
-  const int rq = min(r0, rows - 1), token = rq / group, h = kvh * group + rq - token * group;
+  int g;
+  const int token = p.by_group.divide(min(r0, rows - 1), &g), h = kvh * group + g;
   frag qf[KK];
   load_column<T, HDP>((const T*)p.q + ((int64_t)b * p.q_len + token) * p.ldq + (int64_t)h * p.head_dim, p.head_dim, hi, qf);
   Column<ND> col;
@@ -312,7 +315,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_cross_few(CrossParams p) {
   for (int w = 0; w < FEW_WAVES; ++w) m = fmaxf(m, ml[w][q].x);
 #pragma unroll
   for (int w = 0; w < FEW_WAVES; ++w) sum += ml[w][q].y * __builtin_amdgcn_exp2f(ml[w][q].x - m);
-  const int tq = at / group, hq = kvh * group + at - tq * group;
+  const int tq = p.by_group.divide(at, &g), hq = kvh * group + g;
   const int64_t row = ((int64_t)b * p.heads + hq) * p.q_len + tq, prow = part * p.rows + row;
   T* const orow = (T*)p.o + ((int64_t)b * p.q_len + tq) * p.ldo + (int64_t)hq * p.head_dim;
   const float f = p.parts > 1 ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
@@ -381,6 +384,7 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p) {
 template <typename T, int HDP>
 hipError_t run_cross(CrossParams p, const CrossPick& pick, hipStream_t s) {
   p.blocks = pick.blocks;
+  p.by_blocks = Divisor(pick.blocks);
   const unsigned wgs = (unsigned)((int64_t)p.batch * (pick.few ? p.kv_heads : p.heads) * pick.blocks * pick.parts);
   if (pick.few) hipLaunchKernelGGL((k_cross_few<T, HDP>), dim3(wgs), dim3(FEW_WAVES * 64), 0, s, p);
   else hipLaunchKernelGGL((k_cross<T, HDP>), dim3(wgs), dim3(CROSS_WAVES * 64), 0, s, p);
@@ -415,7 +419,7 @@ hipError_t launch_cross_attn(const xema_cross_attn_args& a, hipStream_t s) {
   float* const part_o = (float*)a.workspace;
   const CrossParams p{a.q, a.k, a.v, a.o, a.lse, a.kv_lens, part_o, (float2*)(part_o + pick.parts * rows * a.head_dim),
                       a.ldq, a.ldk, a.ldv, a.ldo, rows, a.batch, a.heads, a.kv_heads, a.head_dim, a.q_len, a.kv_len, pick.parts, 0,
-                      a.scale * LOG2E_F};
+                      Divisor(1), Divisor(pick.parts), Divisor(a.batch), Divisor(a.kv_heads), Divisor(a.heads / a.kv_heads), a.scale * LOG2E_F};
   return a.dtype == XEMA_BF16 ? cross_t<bf16>(p, pick, s) : cross_t<f16>(p, pick, s);
 }
 

@@ -39,6 +39,7 @@ struct CrossBwd {
   float* dkv_parts;                    // [parts][dk, dv][batch * kv_len][kv_heads * head_dim]
   int64_t ldq, ldk, ldv, ldo, ld_do, ld_dq, ld_dk, ld_dv;
   int batch, heads, kv_heads, head_dim, q_len, kv_len, q_parts, kv_parts;
+  Divisor by_q_blocks, by_q_parts, by_kv_blocks, by_kv_parts, by_batch, by_group, by_tiles;
   float c, scale;                      // scale * log2(e), scale
 };
 
@@ -55,11 +56,10 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
   static_assert(BWD_WAVES * WaveRows<HDP>::BYTES == 4 * TILE, "rows of four waves");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c32 = lane & 31, hi = lane >> 5;
-  const int blocks = (p.q_len + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES);
   const int t = xcd_order((int)blockIdx.x, (int)gridDim.x);
   // (an XCD's range holds all sequences of its heads, whose lengths may differ)
-  const int block = t % blocks, part = t / blocks % p.q_parts, hb = t / blocks / p.q_parts;
-  const int h = hb / p.batch, b = hb - h * p.batch, kvh = h / (p.heads / p.kv_heads);
+  int block, part, b, rest;
+  const int h = p.by_batch.divide(p.by_q_parts.divide(p.by_q_blocks.divide(t, &block), &part), &b), kvh = p.by_group.divide(h, &rest);
   const int n = states_of(p.kv_lens, b, p.kv_len), tiles = (n + QKT - 1) / QKT;
   int first, count;
   part_of(tiles, part, p.q_parts, &first, &count);
@@ -187,10 +187,9 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dkv(CrossBwd p) {
   __shared__ __attribute__((aligned(16))) float stats[2][2][KT];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c32 = lane & 31, hi = lane >> 5;
-  const int blocks = (p.kv_len + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES);
   const int t = xcd_order((int)blockIdx.x, (int)gridDim.x);
-  const int block = t % blocks, part = t / blocks % p.kv_parts, kb = t / blocks / p.kv_parts;
-  const int kvh = kb / p.batch, b = kb - kvh * p.batch, group = p.heads / p.kv_heads;
+  int block, part, b;
+  const int kvh = p.by_batch.divide(p.by_kv_parts.divide(p.by_kv_blocks.divide(t, &block), &part), &b), group = (int)p.by_group.d;
   const int n = states_of(p.kv_lens, b, p.kv_len);
   const int state0 = (block * BWD_WAVES + wave) * 32, state = state0 + c32;
   // tiles: those of the first head's tokens, the second's, ...
@@ -203,7 +202,7 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dkv(CrossBwd p) {
   TileLoads<HDP, KT, BWD_WAVES> lq, ld;
   lq.init(ldq, p.head_dim, wave, lane);
   ld.init(ld_do, p.head_dim, wave, lane);
-  int g = per_head ? __builtin_amdgcn_readfirstlane(first / per_head) : 0, tile = first - g * per_head;      // of the next tile to load
+  int tile, g = p.by_tiles.divide(first, &tile);        // of the next tile to load
   auto issue = [&](int stage) {
     const int h = kvh * group + g, t0 = tile * KT, rows = p.q_len - t0;
     const int64_t at = (int64_t)b * p.q_len + t0;
@@ -376,9 +375,11 @@ int64_t cross_attn_bwd_workspace(const CrossShape& c) {
 hipError_t launch_cross_attn_bwd(const xema_cross_attn_bwd_args& a, hipStream_t s) {
   const BwdSpace w = bwd_space({a.batch, a.heads, a.kv_heads, a.head_dim, a.q_len, a.kv_len});
   float* const ws = (float*)a.workspace;
+  auto blocks = [](int n) { return n > 0 ? (n + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES) : 1; };
   const CrossBwd p{a.q, a.k, a.v, a.o, a.dout, a.lse, a.kv_lens, a.dq, a.dk, a.dv, ws, ws + w.stats, ws + 2 * w.stats, ws + 2 * w.stats + w.dq,
                    a.ldq, a.ldk, a.ldv, a.ldo, a.ld_do, a.ld_dq, a.ld_dk, a.ld_dv, a.batch, a.heads, a.kv_heads, a.head_dim, a.q_len, a.kv_len,
-                   w.q_parts, w.kv_parts, a.scale * LOG2E_F, a.scale};
+                   w.q_parts, w.kv_parts, Divisor(blocks(a.q_len)), Divisor(w.q_parts), Divisor(blocks(a.kv_len)), Divisor(w.kv_parts), Divisor(a.batch),
+                   Divisor(a.heads / a.kv_heads), Divisor(a.q_len > 0 ? (a.q_len + KT - 1) / KT : 1), a.scale * LOG2E_F, a.scale};
   return a.dtype == XEMA_BF16 ? cross_bwd_t<bf16>(p, s) : cross_bwd_t<f16>(p, s);
 }
 
