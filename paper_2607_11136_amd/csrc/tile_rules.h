@@ -280,7 +280,7 @@ inline int cross_dkv_parts(int batch, int heads, int kv_heads, int head_dim, int
   const int64_t wgs = (int64_t)batch * kv_heads * ((kv_len + 127) / 128), tiles = (int64_t)heads / kv_heads * ((q_len + 63) / 64);
   const int64_t sums = 2 * (int64_t)batch * kv_len * kv_heads * head_dim;
   const int64_t slots = (head_dim <= 64 ? 3 : 2) * RULE_CUS;
-  return wgs ? (int)std::max<int64_t>(1, std::min<int64_t>({slots / wgs, tiles / 4, 32, ((int64_t)1 << 26) / sums})) : 1;
+  return wgs ? (int)std::max<int64_t>(1, std::min<int64_t>({slots / wgs, tiles / 2, 32, ((int64_t)1 << 26) / sums})) : 1;
 }
 
 // ---------------------------------------------------------------------------
