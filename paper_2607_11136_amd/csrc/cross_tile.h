@@ -63,22 +63,45 @@ struct TileLoads {
 #pragma unroll
     for (int c = 0; c < LOADS; ++c) load_lds16(r, st + (wave * LOADS + c) * 1024, off[c], 0);
   }
-  // The same, rows past the last (rows >= 1) repeating it.
-  __device__ __forceinline__ void issue_repeated(const uint8_t* base, uint32_t ld_bytes, int rows, uint8_t* st, int wave, int lane) const {
-    if (rows >= N) return issue(base, ld_bytes, N, st, wave);
-    TileLoads last;
-#pragma unroll
-    for (int c = 0; c < LOADS; ++c) {
-      const int row = (wave * LOADS + c) * RPL + lane / (RB / 16);
-      last.off[c] = off[c] == OUT_OF_RANGE ? OUT_OF_RANGE : off[c] - (uint32_t)max(row - (rows - 1), 0) * ld_bytes;
-    }
-    last.issue(base, ld_bytes, rows, st, wave);
-  }
 };
 
 // Keeps the compiler from holding every address that it forms from x: they are formed again where they are used.
 template <typename I>
 __device__ __forceinline__ void forget(I& x) { asm volatile("" : "+v"(x)); }
+
+// The lane, formed anew: no register holds it until here.
+__device__ __forceinline__ int lane_again() {
+  uint32_t all = ~0u;
+  asm volatile("" : "+s"(all));
+  return (int)__builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0));
+}
+
+// The same loads with rows past the last (rows >= 1) repeating it.  In rows of
+// 256 bytes their offsets are formed at each tile: beside the sums of wide heads,
+// offsets kept over the loop spill.
+template <int HDP, int N, int NW>
+struct RepeatedLoads {
+  static constexpr int RB = Rows<HDP>::RB, RPL = 1024 / RB, LOADS = N / RPL / NW;
+  static_assert(LOADS * RPL * NW == N && LOADS == (RB == 128 ? 2 : 4), "a load's rows move the swizzle by a constant");
+  static __device__ __forceinline__ void issue(const uint8_t* base, uint32_t ld_bytes, int head_dim, int rows, uint8_t* st, int wave) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(base, (int64_t)min(rows, N) * ld_bytes);
+    const int lane = RB == 128 ? (int)(threadIdx.x & 63) : lane_again();
+    const int row0 = wave * LOADS * RPL + lane / (RB / 16), slot0 = (lane % (RB / 16)) ^ Rows<HDP>::swz(lane / (RB / 16));
+    uint32_t off[LOADS];
+    if (rows >= N) {
+#pragma unroll
+      for (int c = 0; c < LOADS; ++c) off[c] = row0 * ld_bytes + c * RPL * ld_bytes;
+    } else {
+#pragma unroll
+      for (int c = 0; c < LOADS; ++c) off[c] = min(row0 + c * RPL, rows - 1) * ld_bytes;
+    }
+#pragma unroll
+    for (int c = 0; c < LOADS; ++c) {
+      const int slot = slot0 ^ (RB == 128 ? c << 1 : c);
+      load_lds16(r, st + (wave * LOADS + c) * 1024, slot * 8 < head_dim ? off[c] + slot * 16 : OUT_OF_RANGE, 0);
+    }
+  }
+};
 
 // Fragments along rows: rows row0 + lane % 32, elements 16 kk + 8 (lane / 32) + 0..7.
 template <typename T, int HDP>

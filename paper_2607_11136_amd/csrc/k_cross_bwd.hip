@@ -199,16 +199,14 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dkv(CrossBwd p) {
   if (block * BWD_WAVES * 32 >= n) count = 0;       // (no states here: zeros)
 
   const uint32_t ldq = (uint32_t)p.ldq * 2, ld_do = (uint32_t)p.ld_do * 2;
-  TileLoads<HDP, KT, BWD_WAVES> lq, ld;
-  lq.init(ldq, p.head_dim, wave, lane);
-  ld.init(ld_do, p.head_dim, wave, lane);
+  typedef RepeatedLoads<HDP, KT, BWD_WAVES> Loads;
   int tile, g = p.by_tiles.divide(first, &tile);        // of the next tile to load
   auto issue = [&](int stage) {
     const int h = kvh * group + g, t0 = tile * KT, rows = p.q_len - t0;
     const int64_t at = (int64_t)b * p.q_len + t0;
     // (tokens past the last repeat it, and weigh 0 by their lse: rows of zeros would make NaN of an infinite k)
-    lq.issue_repeated((const uint8_t*)((const T*)p.q + at * p.ldq + (int64_t)h * p.head_dim), ldq, rows, smem[stage], wave, lane);
-    ld.issue_repeated((const uint8_t*)((const T*)p.dout + at * p.ld_do + (int64_t)h * p.head_dim), ld_do, rows, smem[stage] + TILE, wave, lane);
+    Loads::issue((const uint8_t*)((const T*)p.q + at * p.ldq + (int64_t)h * p.head_dim), ldq, p.head_dim, rows, smem[stage], wave);
+    Loads::issue((const uint8_t*)((const T*)p.dout + at * p.ld_do + (int64_t)h * p.head_dim), ld_do, p.head_dim, rows, smem[stage] + TILE, wave);
     if (wave < 2) {
       const float* const st = (wave ? p.stat_d : p.stat_l) + (((int64_t)b * p.heads + h) * per_head + tile) * KT;
       load_lds4(make_rsrc(st, 4 * KT), (uint8_t*)stats[stage][wave], lane * 4);
@@ -275,21 +273,23 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dkv(CrossBwd p) {
       }
     }
   }
-  if (state >= n) {
+  const int again = lane_again(), half = again >> 5, mine = state0 + (again & 31);
+  if (mine >= n) {
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.f;
   }
-  const bool valid = state < p.kv_len;
+  const bool valid = mine < p.kv_len;
+  const int64_t row = (int64_t)b * p.kv_len + mine;
   if (p.kv_parts > 1) {
     const int64_t width = (int64_t)p.kv_heads * p.head_dim, one = (int64_t)p.batch * p.kv_len * width;
-    float* const out = p.dkv_parts + part * 2 * one + kv_row * width + at;
-    store_column_f32<ND>(out, p.head_dim, dk, p.scale, hi, valid);
-    store_column_f32<ND>(out + one, p.head_dim, dv, P_UNIT<T>, hi, valid);
+    float* const out = p.dkv_parts + part * 2 * one + row * width + at;
+    store_column_f32<ND>(out, p.head_dim, dk, p.scale, half, valid);
+    store_column_f32<ND>(out + one, p.head_dim, dv, P_UNIT<T>, half, valid);
   } else {
-    store_column<T, ND>((T*)p.dk + kv_row * p.ld_dk + at, p.head_dim, dk, p.scale, hi, valid);
-    store_column<T, ND>((T*)p.dv + kv_row * p.ld_dv + at, p.head_dim, dv, P_UNIT<T>, hi, valid);
+    store_column<T, ND>((T*)p.dk + row * p.ld_dk + at, p.head_dim, dk, p.scale, half, valid);
+    store_column<T, ND>((T*)p.dv + row * p.ld_dv + at, p.head_dim, dv, P_UNIT<T>, half, valid);
   }
 }
 
