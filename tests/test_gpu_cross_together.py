@@ -191,9 +191,9 @@ def norm_bwd(rows):
     return [s, dy, gamma], [dx, dgamma, dbeta], [ws], lambda st: X.xema_op_layernorm_bwd(a, st)
 
 
-def linear(rows, out):
+def linear(rows, out, dim=264):
     g = gen(3)
-    x, w, r = normal(g, (rows, 264)), normal(g, (out, 264), 0.06), normal(g, (rows, out))
+    x, w, r = normal(g, (rows, dim)), normal(g, (out, dim), 0.06), normal(g, (rows, out))
     y = empty(rows, out, 0, BF16)
     return [x, w, r], [y], [], lambda st: run_linear(x, w, None, 1, y, r, None, st)
 
@@ -213,7 +213,7 @@ CASES = {
     "single tokens": lambda: attention(130, 4, 2, 64, 1, 40), "single tokens in parts": lambda: attention(2, 8, 2, 128, 1, 3000),
     "attention gradient": lambda: attention_gradient(8, 40, 40, 64, 90, 40), "attention gradient in parts": lambda: attention_gradient(1, 3, 3, 72, 129, 1000),
     "norm": lambda: norm(300), "norm gradient": lambda: norm_bwd(3000), "linear, few rows": lambda: linear(7, 520), "linear": lambda: linear(700, 520),
-    "linear, two launches": lambda: linear(9000, 8200), "linear gradient, one launch of products": lambda: linear_bwd(65, 136, 200),
+    "linear, two launches": lambda: linear(9000, 2056, 520), "linear gradient, one launch of products": lambda: linear_bwd(65, 136, 200),
     "two launches": lambda: linear_bwd(3000, 1032, 4104), "split dx": lambda: linear_bwd(70, 136, 8200), "split dw": lambda: linear_bwd(4500, 64, 72),
 }
 

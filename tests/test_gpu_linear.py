@@ -13,10 +13,11 @@ pytestmark = pytest.mark.gpu
 # rows, dim, out_dim: every few-row kernel and every tile (tests/test_cross_rules.py)
 SIZES = [(1, 8, 8), (1, 4096, 136), (17, 264, 72), (33, 520, 4096), (64, 72, 1000), (5, 136, 4104), (20, 264, 8192), (40, 72, 6000), (50, 136, 4608),
          (3, 264, 8200), (30, 72, 12008), (65, 40, 8), (100, 264, 392), (700, 136, 520), (300, 136, 8200), (1100, 72, 3000), (2600, 520, 2056),
-         (6000, 64, 4104), (130, 2056, 72)]
+         (6000, 64, 4104), (130, 2056, 72), (9000, 264, 8200), (9000, 520, 2056), (2600, 520, 8200)]
 # whole and split k of either product, one launch and two
 BWD_SIZES = [(1, 8, 8), (7, 72, 136), (65, 136, 200), (333, 512, 1368), (70, 136, 8200), (4500, 64, 72), (1614, 1240, 2400), (3000, 1032, 4104),
-             (257, 8200, 136), (16, 2056, 2056), (2100, 264, 264), (9000, 136, 1032)]
+             (257, 8200, 136), (16, 2056, 2056), (2100, 264, 264), (9000, 136, 1032), (1000, 136, 264), (2048, 136, 264), (8200, 520, 264),
+             (1000, 2056, 264), (8200, 136, 2056), (1000, 4104, 264), (2048, 4104, 264), (8200, 2056, 264), (8200, 136, 8200), (8200, 264, 4104)]
 
 
 def run(x, w, bias, act, y, resid=None, pre=None, stream=None):
