@@ -381,6 +381,43 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p) {
   *reinterpret_cast<t2*>((T*)p.o + (b * p.q_len + token) * p.ldo + h * p.head_dim + c) = t2{(T)(o[0] * f), (T)(o[1] * f)};
 }
 
+// The same for many rows: LANES threads a row, eight columns each, part by part.
+template <typename T, int LANES>
+__global__ __launch_bounds__(256) void k_cross_join_rows(CrossParams p) {
+  const int64_t row = (int64_t)blockIdx.x * (256 / LANES) + (int)threadIdx.x / LANES;
+  const int e = (int)threadIdx.x % LANES * 8;
+  if (row >= p.rows || e >= p.head_dim) return;
+  float m = LOWEST;
+#pragma unroll 4
+  for (int i = 0; i < p.parts; ++i) m = fmaxf(m, p.part_ml[i * p.rows + row].x);
+  f32x4 v[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+  float sum = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < p.parts; ++i) {
+    const float2 ml = p.part_ml[i * p.rows + row];
+    const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+    if (f == 0.f) continue;      // (a part of no weight may not have been written)
+    sum = fmaf(ml.y, f, sum);
+    const f32x4* const at = reinterpret_cast<const f32x4*>(p.part_o + (i * p.rows + row) * p.head_dim + e);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) v[x] += at[x] * f;
+  }
+  if (e == 0 && p.lse) p.lse[row] = lse_of(m, sum);
+  const int64_t bh = row / p.q_len, token = row - bh * p.q_len, b = bh / p.heads, h = bh - b * p.heads;
+  typedef T t8 __attribute__((ext_vector_type(8)));
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
+  t8 o;
+#pragma unroll
+  for (int x = 0; x < 8; ++x) o[x] = (T)(v[x / 4][x % 4] * f);
+  *reinterpret_cast<t8*>((T*)p.o + (b * p.q_len + token) * p.ldo + h * p.head_dim + e) = o;
+}
+
+template <typename T, int LANES>
+hipError_t run_join_rows(const CrossParams& p, hipStream_t s) {
+  hipLaunchKernelGGL((k_cross_join_rows<T, LANES>), dim3((unsigned)((p.rows * LANES + 255) / 256)), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
 template <typename T, int HDP>
 hipError_t run_cross(CrossParams p, const CrossPick& pick, hipStream_t s) {
   p.blocks = pick.blocks;
@@ -391,6 +428,11 @@ hipError_t run_cross(CrossParams p, const CrossPick& pick, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Rows up to which a workgroup joins one (us of the call with k_cross_join and
+// k_cross_join_rows: 128 rows in 16 parts 47 and 54; 512 in 4 either 47; 8192 in 2
+// 21 and 14).
+constexpr int64_t JOIN_ROWS = 1024;
+
 template <typename T>
 hipError_t cross_t(const CrossParams& p, const CrossPick& pick, hipStream_t s) {
   hipError_t e;
@@ -399,6 +441,7 @@ hipError_t cross_t(const CrossParams& p, const CrossPick& pick, hipStream_t s) {
   else if (p.head_dim <= 96) e = run_cross<T, 96>(p, pick, s);
   else e = run_cross<T, 128>(p, pick, s);
   if (e != hipSuccess || p.parts == 1) return e;
+  if (p.rows > JOIN_ROWS) return p.head_dim <= 64 ? run_join_rows<T, 8>(p, s) : run_join_rows<T, 16>(p, s);
   hipLaunchKernelGGL((k_cross_join<T>), dim3((unsigned)p.rows), dim3(256), 0, s, p);
   return hipGetLastError();
 }

@@ -248,33 +248,48 @@ inline ReducePick pick_reduce(int64_t rows, int rank) {
 // ---------------------------------------------------------------------------
 // Attention to an encoder's states (k_cross.hip, k_cross_bwd.hip)
 // ---------------------------------------------------------------------------
-// few: the kernel of single tokens, whose blocks are 32 queries of all heads that
-// share a state's head; otherwise blocks of a head's queries, 256 to a workgroup
-// at head dims to 64 and 128 past that.  parts: of the states.
+// few: the kernel of single tokens, whose blocks are 32 rows (tokens of all heads
+// that share a state's head); otherwise blocks of 128 of a head's queries.  us, few
+// and not: 64 rows, 4 sequences of 4096 states, 8 state heads of 128, 24 and 40;
+// 96 rows 49 and 40; with fewer states (1024, 512, 77) they are within 15%.
+//
+// parts: of the states, for calls of few workgroups, which k_cross_join adds up.
+// Single tokens: one round of two workgroups a CU (us, at 512 and 1024 workgroups:
+// 8 sequences of 4096 states 33 and 39, 64 of 1024 52 and 58), no part below 128
+// states, and none at all where the half of the CUs has work and the states are so
+// few that the join costs more (256 sequences' heads of 64, 512 states: whole 9.2,
+// two parts 10.8).  Otherwise parts of 256 states or more, from 1024 states on (us,
+// whole and in the parts picked: 2 x 500 tokens, 8 heads of 128, 512 states 13.4
+// and 17.0; 1000 tokens, 8 heads of 64, 1024 states 18.1 and 15.3; 256 tokens, 4
+// heads of 128, 4096 states 80 and 18).
 constexpr int FEW_WGS = 2 * RULE_CUS;
 struct CrossPick { bool few; int blocks, parts; };
+// Of the states, for `wgs` workgroups of 128 queries: the forward pass, and dq.
+inline int cross_parts(int64_t wgs, int kv_len) {
+  if (wgs == 0 || kv_len < 1024) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({2 * RULE_CUS / wgs, kv_len / 256, 16}));
+}
 inline CrossPick pick_cross(int batch, int heads, int kv_heads, int head_dim, int q_len, int kv_len) {
   const int64_t rows = (int64_t)q_len * (heads / kv_heads);
-  CrossPick pick{rows <= 64, 0, 1};
-  if (pick.few) {
-    pick.blocks = (int)((rows + 31) / 32);
-    const int64_t wgs = (int64_t)batch * kv_heads * pick.blocks, most = ((int64_t)kv_len + 255) / 256;
-    pick.parts = (int)std::max<int64_t>(1, std::min<int64_t>({(FEW_WGS + wgs - 1) / wgs, most, 64}));
-    return pick;
+  if (rows > 64) {
+    const int blocks = (q_len + 127) / 128;
+    return {false, blocks, cross_parts((int64_t)batch * heads * blocks, kv_len)};
   }
-  const int per = 128;
-  pick.blocks = (q_len + per - 1) / per;
-  const int64_t wgs = (int64_t)batch * heads * pick.blocks, tiles = ((int64_t)kv_len + 63) / 64;
-  pick.parts = (int)std::max<int64_t>(1, std::min<int64_t>({2 * RULE_CUS / wgs, tiles / 4, 16}));
-  return pick;
+  const int blocks = (int)((rows + 31) / 32);
+  const int64_t wgs = (int64_t)batch * kv_heads * blocks;
+  const int64_t most = wgs >= RULE_CUS / 2 && kv_len <= 768 ? 1 : ((int64_t)kv_len + 127) / 128;
+  return {true, blocks, wgs ? (int)std::max<int64_t>(1, std::min<int64_t>({(FEW_WGS + wgs - 1) / wgs, most, 64})) : 1};
 }
 
-// The gradient: parts of the states for dq (workgroups of 128 queries of a head),
-// and of the tokens of all heads that share a state's head for dk and dv
-// (workgroups of 128 states).
+// The gradient.  dq: as the forward pass (us, whole and in parts: 512 states 17.9
+// and 19.5, 1024 states 19.8 and 15.6, 4096 states 100 and 21).  dk and dv: parts of
+// the tokens of all heads that share a state's head, for workgroups of 128 states;
+// as many as the CUs hold (two each, three at head dims to 64), of two tiles of 64
+// tokens or more, their sums within 256 MiB (us of dk and dv, whole and in the parts
+// picked: 4608 tokens, 32 heads of 128, 512 states 194 and 96; 2 x 577 tokens, 4
+// heads of 64 for 16, 120 states 82 and 19; 4 x 1024, 12 heads of 72, 77 states 33 and 18).
 inline int cross_dq_parts(int batch, int heads, int q_len, int kv_len) {
-  const int64_t wgs = (int64_t)batch * heads * ((q_len + 127) / 128), tiles = ((int64_t)kv_len + 63) / 64;
-  return wgs ? (int)std::max<int64_t>(1, std::min<int64_t>({2 * RULE_CUS / wgs, tiles / 4, 16})) : 1;
+  return cross_parts((int64_t)batch * heads * ((q_len + 127) / 128), kv_len);
 }
 inline int cross_dkv_parts(int batch, int heads, int kv_heads, int head_dim, int q_len, int kv_len) {
   const int64_t wgs = (int64_t)batch * kv_heads * ((kv_len + 127) / 128), tiles = (int64_t)heads / kv_heads * ((q_len + 63) / 64);

@@ -81,11 +81,12 @@ SIZES = [
     (2, 2, 1, 128, 500, 300, [300, 128]), (1, 3, 3, 24, 129, 1000, None), (2, 8, 1, 128, 70, 515, [400, 515]), (4, 2, 2, 64, 1030, 31, [31, 5, 0, 32]),
     (1, 16, 4, 56, 16, 700, [-3]), (1, 2, 2, 120, 600, 1100, [2000]), (8, 40, 40, 64, 90, 40, None),
     (1, 2, 2, 64, 300, 900, None), (1, 2, 2, 88, 200, 1000, None), (1, 2, 1, 32, 700, 100, None),
+    (1, 2, 2, 64, 300, 1025, [1000]), (1, 2, 2, 88, 200, 1300, None), (1, 3, 3, 32, 129, 1200, [1100]), (1, 2, 2, 120, 200, 2100, None),
 ]
 TOKENS = [
     (1, 1, 1, 128, 1, 1, None), (3, 8, 1, 128, 1, 5000, [5000, 1, 0]), (2, 4, 4, 64, 1, 3001, [3001, 64]), (1, 32, 8, 128, 1, 9000, None),
     (2, 6, 3, 72, 5, 1027, [1000, 33]), (4, 16, 2, 96, 4, 513, [0, 512, 513, 31]), (2, 64, 1, 32, 1, 2000, [2000, 1999]), (130, 4, 2, 64, 1, 40, None),
-    (2, 8, 2, 88, 3, 250, [250, 7]),
+    (2, 8, 2, 88, 3, 250, [250, 7]), (2, 8, 2, 96, 3, 100, [100, 7]),
 ]
 
 
