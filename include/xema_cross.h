@@ -157,7 +157,8 @@ XEMA_API int xema_op_linear_bwd(const xema_linear_bwd_args* args, void* stream);
  * q and o [batch * q_len, heads * head_dim], k and v [batch * kv_len, kv_heads *
  * head_dim] have type `dtype` (XEMA_BF16 or XEMA_F16); row b q_len + i is token
  * i of sequence b, and head h is columns h head_dim ... .  q_len and kv_len may
- * be 0, as may batch; head_dim is a multiple of 8 up to 128; scale is finite.
+ * be 0, as may batch; head_dim is a multiple of 8 up to 128; scale is finite
+ * and above 0.
  * kv_lens int32 [batch] (4-byte aligned), on the device, NULL: kv_len for all;
  * values are taken between 0 and kv_len.  Rows of k and v behind a sequence's
  * last state are not read for their values: NaN there does not reach o.  A

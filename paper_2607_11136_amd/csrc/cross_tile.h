@@ -192,8 +192,8 @@ __device__ __forceinline__ u32x4 eight_of(const f32x16& acc, int g, float f) {
 // 32 rows of a matrix [rows, elements] through 32 RB bytes of LDS that a wave has
 // to itself, so that 16 lanes (8 at 128 bytes a row) load or store a row's
 // consecutive bytes: straight between memory and a lane's column each load meets
-// a quarter of 32 rows' lines, and the address unit takes longer than the products
-// (16384 tokens, 32 heads of 128, 512 states: 183 us, through LDS 145).
+// 32 rows' lines (18432 tokens, 32 heads of 128, 64 states: 75 us, through LDS 65;
+// with 512 states, where the products take longer, 205 either way).
 template <int HDP>
 struct WaveRows {
   static constexpr int BYTES = 32 * Rows<HDP>::RB;
