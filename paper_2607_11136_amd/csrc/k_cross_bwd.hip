@@ -50,18 +50,38 @@ struct CrossBwd {
 
 constexpr int QKT = 32;                // states per tile of k_cross_dq
 
+// What both passes form has the same bits in either.
+// lse in log2 units, +infinity for a token of no states (its weights are then zeros).
+__device__ __forceinline__ float log2_lse(float lse) {
+  float l = lse * LOG2E_F;
+  asm("" : "+v"(l));                   // (rounded here, not fused with what it is added to)
+  return lse == -INFINITY ? INFINITY : l;
+}
+// A 16-byte slot's share of D; slots are added in pairs, their pairs in pairs, ...
+template <typename F>
+__device__ __forceinline__ float slot_dot(const F& d, const F& o) {
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum = fmaf((float)d[e], (float)o[e], sum);
+  return sum;
+}
+
+// Two stages of K and V; the waves' rows of q pass through stage 1 and a third
+// part, those of dout, and of dq in the end, through two more.
+template <int HDP>
+constexpr int DQ_LDS = 5 * 2 * QKT * Rows<HDP>::RB;
+
+// Workgroup wg of `wgs`.
 template <typename T, int HDP>
-__global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
+__device__ __forceinline__ void cross_dq(const CrossBwd& p, int wg, int wgs, uint8_t* lds) {
   typedef Rows<HDP> R;
   typedef typename Mfma<T>::frag frag;
   constexpr int KK = R::KK, ND = R::ND, TILE = QKT * R::RB, SLOTS = R::RB / 16, PER = 64 / SLOTS;
-  // two stages of K and V; the waves' rows of q pass through stage 1 and a third
-  // part, those of dout, and of dq in the end, through two more
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[5][2 * TILE];
+  const auto smem = reinterpret_cast<uint8_t(*)[2 * TILE]>(lds);
   static_assert(BWD_WAVES * WaveRows<HDP>::BYTES == 4 * TILE, "rows of four waves");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c32 = lane & 31, hi = lane >> 5;
-  const int t = xcd_order((int)blockIdx.x, (int)gridDim.x);
+  const int t = xcd_order(wg, wgs);
   // (an XCD's range holds all sequences of its heads, whose lengths may differ)
   int block, part, b, rest;
   const int h = p.by_batch.divide(p.by_q_parts.divide(p.by_q_blocks.divide(t, &block), &part), &b), kvh = p.by_group.divide(h, &rest);
@@ -107,7 +127,7 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
   const int q = q0 + c32;
   const bool valid = c32 < left_q;
   const float lse = valid ? p.lse[((int64_t)b * p.heads + h) * p.q_len + q] : -INFINITY;
-  const float L = lse == -INFINITY ? INFINITY : lse * LOG2E_F;
+  const float L = log2_lse(lse);
   AlongRows<T, HDP> ra;
   AcrossRows<T, HDP> rx;
   ra.init(lane);
@@ -121,9 +141,7 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
   for (int c = 0; c < 32 / PER; ++c) {
     const int r = c * PER + lane / SLOTS;
     const frag d = *reinterpret_cast<const frag*>(d_out_rows + r * R::RB + ((slot ^ R::swz(r)) << 4));
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fmaf((float)d[e], (float)o[c][e], sum);
+    float sum = slot_dot(d, o[c]);
 #pragma unroll
     for (int x = 1; x < SLOTS; x *= 2) sum += __shfl_xor(sum, x, 64);
     // (in place of the rows of q, which are read: LDS takes a wave's accesses in order)
@@ -132,7 +150,7 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
   asm volatile("" ::: "memory");
   const float D = reinterpret_cast<const float*>(q_rows)[c32];
   const int padded = (p.q_len + KT - 1) / KT * KT;
-  if (part == 0 && q < padded && !hi) {
+  if (p.stat_l && part == 0 && q < padded && !hi) {
     const int64_t st = ((int64_t)b * p.heads + h) * padded + q;
     p.stat_l[st] = valid ? L - P_EXP<T> : INFINITY;
     p.stat_d[st] = valid ? D * P_UNIT<T> : 0.f;
@@ -183,16 +201,21 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
     WaveRows<HDP>::template store<T>((T*)p.dq + tok0 * p.ld_dq + at, p.ld_dq, p.head_dim, left_q, acc, p.scale, d_out_rows, lane);
 }
 
-template <typename T, int HDP>
-__global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dkv(CrossBwd p) {
+// Two stages of q, dout, and lse and D of their tokens.
+template <int HDP>
+constexpr int DKV_LDS = 2 * (2 * KT * Rows<HDP>::RB + 2 * KT * 4);
+
+// Workgroup wg of `wgs`.  OWN: lse and D are taken from their sources here, not from dq's pass.
+template <typename T, int HDP, bool OWN>
+__device__ __forceinline__ void cross_dkv(const CrossBwd& p, int wg, int wgs, uint8_t* lds) {
   typedef Rows<HDP> R;
   typedef typename Mfma<T>::frag frag;
   constexpr int KK = R::KK, ND = R::ND, TILE = KT * R::RB;
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[2][2 * TILE];
-  __shared__ __attribute__((aligned(16))) float stats[2][2][KT];
+  const auto smem = reinterpret_cast<uint8_t(*)[2 * TILE]>(lds);
+  const auto stats = reinterpret_cast<float(*)[2][KT]>(lds + 4 * TILE);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c32 = lane & 31, hi = lane >> 5;
-  const int t = xcd_order((int)blockIdx.x, (int)gridDim.x);
+  const int t = xcd_order(wg, wgs);
   int block, part, b;
   const int kvh = p.by_batch.divide(p.by_kv_parts.divide(p.by_kv_blocks.divide(t, &block), &part), &b), group = (int)p.by_group.d;
   const int n = states_of(p.kv_lens, b, p.kv_len);
@@ -212,7 +235,7 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dkv(CrossBwd p) {
     // (tokens past the last repeat it, and weigh 0 by their lse: rows of zeros would make NaN of an infinite k)
     Loads::issue((const uint8_t*)((const T*)p.q + at * p.ldq + (int64_t)h * p.head_dim), ldq, p.head_dim, rows, smem[stage], wave);
     Loads::issue((const uint8_t*)((const T*)p.dout + at * p.ld_do + (int64_t)h * p.head_dim), ld_do, p.head_dim, rows, smem[stage] + TILE, wave);
-    if (wave < 2) {
+    if (!OWN && wave < 2) {
       const float* const st = (wave ? p.stat_d : p.stat_l) + (((int64_t)b * p.heads + h) * per_head + tile) * KT;
       load_lds4(make_rsrc(st, 4 * KT), (uint8_t*)stats[stage][wave], lane * 4);
     }
@@ -240,7 +263,40 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dkv(CrossBwd p) {
   const bool busy = state0 < n;
   for (int i = 0; i < count; ++i) {
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    if constexpr (OWN) {
+      // four threads a token: 16-byte slots quarter, quarter + 4, ... of its rows of o and dout
+      const int th = wave * 64 + lane_again(), r = th >> 2, quarter = th & 3;
+      int at_tile;
+      const int h = kvh * group + p.by_tiles.divide(first + i, &at_tile), token = at_tile * KT + r;
+      const bool there = token < p.q_len;
+      const int64_t row = (int64_t)b * p.q_len + token;
+      frag o[ND];
+      float lse = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < ND; ++j) {
+        const int slot = quarter + 4 * j;
+        o[j] = frag{};
+        if (there && slot * 8 < p.head_dim) o[j] = *reinterpret_cast<const frag*>((const T*)p.o + row * p.ldo + (int64_t)h * p.head_dim + slot * 8);
+      }
+      if (there) lse = p.lse[((int64_t)b * p.heads + h) * p.q_len + token];
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      __syncthreads();
+      const uint8_t* const rows = smem[i & 1] + TILE + r * R::RB;
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < ND; ++j) {
+        sum[j] = slot_dot(*reinterpret_cast<const frag*>(rows + (((quarter + 4 * j) ^ R::swz(r)) << 4)), o[j]);
+        sum[j] += __shfl_xor(sum[j], 1, 64);
+        sum[j] += __shfl_xor(sum[j], 2, 64);
+      }
+      const float D = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      if (quarter == 0) {
+        stats[i & 1][0][r] = log2_lse(lse) - P_EXP<T>;
+        stats[i & 1][1][r] = there ? D * P_UNIT<T> : 0.f;
+      }
+    } else {
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+    }
     __syncthreads();
     if (i + 1 < count) issue((i + 1) & 1);
     if (!busy) continue;
@@ -298,6 +354,28 @@ __global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dkv(CrossBwd p) {
   }
 }
 
+template <typename T, int HDP>
+__global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dq(CrossBwd p) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[DQ_LDS<HDP>];
+  cross_dq<T, HDP>(p, (int)blockIdx.x, (int)gridDim.x, lds);
+}
+
+template <typename T, int HDP>
+__global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_dkv(CrossBwd p) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[DKV_LDS<HDP>];
+  cross_dkv<T, HDP, false>(p, (int)blockIdx.x, (int)gridDim.x, lds);
+}
+
+// Both of a call that leaves CUs idle either way, side by side: kv_wgs workgroups for dk and dv, the rest for dq.
+template <typename T, int HDP>
+__global__ __launch_bounds__(BWD_WAVES * 64, 2) void k_cross_both(CrossBwd p, int kv_wgs) {
+  static_assert(DKV_LDS<HDP> <= DQ_LDS<HDP>);
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[DQ_LDS<HDP>];
+  const int wg = (int)blockIdx.x;
+  if (wg < kv_wgs) cross_dkv<T, HDP, true>(p, wg, kv_wgs, lds);
+  else cross_dq<T, HDP>(p, wg - kv_wgs, (int)gridDim.x - kv_wgs, lds);
+}
+
 // Outputs from their parts, in order: matrix blockIdx.y of up to two, n elements
 // in rows of `width`; part i of it lies i `stride` past its first.
 template <typename T>
@@ -318,55 +396,55 @@ __global__ __launch_bounds__(256) void k_cross_sums(const float* __restrict__ su
   *reinterpret_cast<t4*>((second ? out1 : out0) + r * (second ? ld1 : ld0) + (at - r * width)) = o;
 }
 
+// The sums of `parts` parts to one matrix, or to two.
+template <typename T>
+hipError_t run_cross_sums(const float* sums, int parts, int64_t rows, int width, T* out0, T* out1, int64_t ld0, int64_t ld1, hipStream_t s) {
+  const int64_t n = rows * width;
+  const int outs = out1 ? 2 : 1;
+  hipLaunchKernelGGL((k_cross_sums<T>), dim3((unsigned)((n / 4 + 255) / 256), outs), dim3(256), 0, s, sums, parts, outs * n, n, width, out0, out1, ld0, ld1);
+  return hipGetLastError();
+}
+
 template <typename T, int HDP>
-hipError_t run_cross_bwd(const CrossBwd& p, hipStream_t s) {
+hipError_t run_cross_bwd(CrossBwd p, bool both, hipStream_t s) {
   const int64_t q_wgs = (int64_t)p.batch * p.heads * ((p.q_len + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES)) * p.q_parts;
   const int64_t kv_wgs = (int64_t)p.batch * p.kv_heads * ((p.kv_len + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES)) * p.kv_parts;
-  hipError_t e = hipSuccess;
-  if (q_wgs) {
-    hipLaunchKernelGGL((k_cross_dq<T, HDP>), dim3((unsigned)q_wgs), dim3(BWD_WAVES * 64), 0, s, p);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (p.dq && p.q_parts > 1) {
-      const int width = p.heads * p.head_dim;
-      const int64_t n = (int64_t)p.batch * p.q_len * width;
-      hipLaunchKernelGGL((k_cross_sums<T>), dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, s, p.dq_parts, p.q_parts, n, n, width, (T*)p.dq, (T*)p.dq,
-                         p.ld_dq, p.ld_dq);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
+  const dim3 block(BWD_WAVES * 64);
+  if (both && p.dq && p.dk && q_wgs && kv_wgs) {
+    p.stat_l = p.stat_d = nullptr;
+    hipLaunchKernelGGL((k_cross_both<T, HDP>), dim3((unsigned)(q_wgs + kv_wgs)), block, 0, s, p, (int)kv_wgs);
+  } else {
+    if (q_wgs) hipLaunchKernelGGL((k_cross_dq<T, HDP>), dim3((unsigned)q_wgs), block, 0, s, p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (p.dk && kv_wgs) hipLaunchKernelGGL((k_cross_dkv<T, HDP>), dim3((unsigned)kv_wgs), block, 0, s, p);
   }
-  if (p.dk && kv_wgs) {
-    hipLaunchKernelGGL((k_cross_dkv<T, HDP>), dim3((unsigned)kv_wgs), dim3(BWD_WAVES * 64), 0, s, p);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (p.kv_parts > 1) {
-      const int width = p.kv_heads * p.head_dim;
-      const int64_t n = (int64_t)p.batch * p.kv_len * width;
-      hipLaunchKernelGGL((k_cross_sums<T>), dim3((unsigned)((n / 4 + 255) / 256), 2), dim3(256), 0, s, p.dkv_parts, p.kv_parts, 2 * n, n, width, (T*)p.dk,
-                         (T*)p.dv, p.ld_dk, p.ld_dv);
-      e = hipGetLastError();
-    }
-  }
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && p.dq && q_wgs && p.q_parts > 1)
+    e = run_cross_sums<T>(p.dq_parts, p.q_parts, (int64_t)p.batch * p.q_len, p.heads * p.head_dim, (T*)p.dq, nullptr, p.ld_dq, 0, s);
+  if (e == hipSuccess && p.dk && kv_wgs && p.kv_parts > 1)
+    e = run_cross_sums<T>(p.dkv_parts, p.kv_parts, (int64_t)p.batch * p.kv_len, p.kv_heads * p.head_dim, (T*)p.dk, (T*)p.dv, p.ld_dk, p.ld_dv, s);
   return e;
 }
 
 template <typename T>
-hipError_t cross_bwd_t(const CrossBwd& p, hipStream_t s) {
-  if (p.head_dim <= 32) return run_cross_bwd<T, 32>(p, s);
-  if (p.head_dim <= 64) return run_cross_bwd<T, 64>(p, s);
-  return p.head_dim <= 96 ? run_cross_bwd<T, 96>(p, s) : run_cross_bwd<T, 128>(p, s);
+hipError_t cross_bwd_t(const CrossBwd& p, bool both, hipStream_t s) {
+  if (p.head_dim <= 32) return run_cross_bwd<T, 32>(p, both, s);
+  if (p.head_dim <= 64) return run_cross_bwd<T, 64>(p, both, s);
+  return p.head_dim <= 96 ? run_cross_bwd<T, 96>(p, both, s) : run_cross_bwd<T, 128>(p, both, s);
 }
 
 // The workspace, in floats: lse and D, then the parts of dq, then those of dk and dv.
 struct BwdSpace {
-  int q_parts, kv_parts;
+  CrossBwdPick pick;
   int64_t stats, dq, dkv;
 };
 BwdSpace bwd_space(const CrossShape& c) {
   const int64_t q_rows = (int64_t)c.batch * c.q_len, kv_rows = (int64_t)c.batch * c.kv_len;
-  BwdSpace w{cross_dq_parts(c.batch, c.heads, c.q_len, c.kv_len),
-             cross_dkv_parts(c.batch, c.heads, c.kv_heads, c.head_dim, c.q_len, c.kv_len), 0, 0, 0};
+  BwdSpace w{pick_cross_bwd(c.batch, c.heads, c.kv_heads, c.head_dim, c.q_len, c.kv_len), 0, 0, 0};
   w.stats = (int64_t)c.batch * c.heads * ((c.q_len + KT - 1) / KT * KT);
-  w.dq = w.q_parts > 1 ? w.q_parts * q_rows * c.heads * c.head_dim : 0;
-  w.dkv = w.kv_parts > 1 ? w.kv_parts * 2 * kv_rows * c.kv_heads * c.head_dim : 0;
+  w.dq = w.pick.q_parts > 1 ? w.pick.q_parts * q_rows * c.heads * c.head_dim : 0;
+  w.dkv = w.pick.kv_parts > 1 ? w.pick.kv_parts * 2 * kv_rows * c.kv_heads * c.head_dim : 0;
   return w;
 }
 
@@ -383,9 +461,9 @@ hipError_t launch_cross_attn_bwd(const xema_cross_attn_bwd_args& a, hipStream_t 
   auto blocks = [](int n) { return n > 0 ? (n + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES) : 1; };
   const CrossBwd p{a.q, a.k, a.v, a.o, a.dout, a.lse, a.kv_lens, a.dq, a.dk, a.dv, ws, ws + w.stats, ws + 2 * w.stats, ws + 2 * w.stats + w.dq,
                    a.ldq, a.ldk, a.ldv, a.ldo, a.ld_do, a.ld_dq, a.ld_dk, a.ld_dv, a.batch, a.heads, a.kv_heads, a.head_dim, a.q_len, a.kv_len,
-                   w.q_parts, w.kv_parts, Divisor(blocks(a.q_len)), Divisor(w.q_parts), Divisor(blocks(a.kv_len)), Divisor(w.kv_parts), Divisor(a.batch),
+                   w.pick.q_parts, w.pick.kv_parts, Divisor(blocks(a.q_len)), Divisor(w.pick.q_parts), Divisor(blocks(a.kv_len)), Divisor(w.pick.kv_parts), Divisor(a.batch),
                    Divisor(a.heads / a.kv_heads), Divisor(a.q_len > 0 ? (a.q_len + KT - 1) / KT : 1), a.scale * LOG2E_F, a.scale};
-  return a.dtype == XEMA_BF16 ? cross_bwd_t<bf16>(p, s) : cross_bwd_t<f16>(p, s);
+  return a.dtype == XEMA_BF16 ? cross_bwd_t<bf16>(p, w.pick.both, s) : cross_bwd_t<f16>(p, w.pick.both, s);
 }
 
 }  // namespace xema

@@ -288,14 +288,18 @@ inline CrossPick pick_cross(int batch, int heads, int kv_heads, int head_dim, in
 // tokens or more, their sums within 256 MiB (us of dk and dv, whole and in the parts
 // picked: 4608 tokens, 32 heads of 128, 512 states 194 and 96; 2 x 577 tokens, 4
 // heads of 64 for 16, 120 states 82 and 19; 4 x 1024, 12 heads of 72, 77 states 33 and 18).
-inline int cross_dq_parts(int batch, int heads, int q_len, int kv_len) {
-  return cross_parts((int64_t)batch * heads * ((q_len + 127) / 128), kv_len);
-}
-inline int cross_dkv_parts(int batch, int heads, int kv_heads, int head_dim, int q_len, int kv_len) {
+//
+// both: one launch, for calls whose dq leaves half of the CUs' places to dk and dv.
+struct CrossBwdPick { int q_parts, kv_parts; bool both; };
+inline CrossBwdPick pick_cross_bwd(int batch, int heads, int kv_heads, int head_dim, int q_len, int kv_len) {
+  const int64_t q_wgs = (int64_t)batch * heads * ((q_len + 127) / 128);
+  const int q_parts = cross_parts(q_wgs, kv_len);
   const int64_t wgs = (int64_t)batch * kv_heads * ((kv_len + 127) / 128), tiles = (int64_t)heads / kv_heads * ((q_len + 63) / 64);
-  const int64_t sums = 2 * (int64_t)batch * kv_len * kv_heads * head_dim;
-  const int64_t slots = (head_dim <= 64 ? 3 : 2) * RULE_CUS;
-  return wgs ? (int)std::max<int64_t>(1, std::min<int64_t>({slots / wgs, tiles / 2, 32, ((int64_t)1 << 26) / sums})) : 1;
+  if (!wgs) return {q_parts, 1, false};
+  const int64_t sums = 2 * (int64_t)batch * kv_len * kv_heads * head_dim, left = 2 * RULE_CUS - q_wgs * q_parts;
+  const bool both = left >= RULE_CUS && left >= wgs;
+  const int64_t slots = both ? left : (head_dim <= 64 ? 3 : 2) * RULE_CUS;
+  return {q_parts, (int)std::max<int64_t>(1, std::min<int64_t>({slots / wgs, tiles / 2, 32, ((int64_t)1 << 26) / sums})), both};
 }
 
 // ---------------------------------------------------------------------------

@@ -23,14 +23,16 @@ int cross(int batch, int heads, int kv_heads, int head_dim, int q_len, int kv_le
   *parts = p.parts;
   return p.few;
 }
-int dq(int batch, int heads, int q_len, int kv_len) { return cross_dq_parts(batch, heads, q_len, kv_len); }
 int rows(long long m, long long n, long long steps, long long* first) {
   const FfnRows p = pick_rows(m, n, steps);
   *first = p.rows;
   return p.rest;
 }
-int dkv(int batch, int heads, int kv_heads, int head_dim, int q_len, int kv_len) {
-  return cross_dkv_parts(batch, heads, kv_heads, head_dim, q_len, kv_len);
+int bwd(int batch, int heads, int kv_heads, int head_dim, int q_len, int kv_len, int* q_parts, int* kv_parts) {
+  const CrossBwdPick p = pick_cross_bwd(batch, heads, kv_heads, head_dim, q_len, kv_len);
+  *q_parts = p.q_parts;
+  *kv_parts = p.kv_parts;
+  return p.both;
 }
 }
 """
@@ -50,6 +52,12 @@ def cross(b, h, kh, d, q, kv):
     blocks, parts = ctypes.c_int(), ctypes.c_int()
     few = lib().cross(b, h, kh, d, q, kv, ctypes.byref(blocks), ctypes.byref(parts))
     return bool(few), blocks.value, parts.value
+
+
+def bwd(b, h, kh, d, q, kv):
+    q_parts, kv_parts = ctypes.c_int(), ctypes.c_int()
+    both = lib().bwd(b, h, kh, d, q, kv, ctypes.byref(q_parts), ctypes.byref(kv_parts))
+    return bool(both), q_parts.value, kv_parts.value
 
 
 def rows(m, n, steps):
@@ -100,8 +108,9 @@ def test_attention_sizes_reach_every_kernel_whole_and_in_parts():
     assert found >= {(w, few, False) for w in (1, 2, 3, 4) for few in (False, True)}
     assert found >= {(w, True, True) for w in (1, 2, 3, 4)} | {(w, False, True) for w in (1, 2, 3, 4)}
     sizes = [s[:6] for s in A.SIZES + A.TOKENS[1:6]]
-    assert {(width(d), lib().dq(b, h, q, kv) > 1) for b, h, kh, d, q, kv in sizes} == {(w, p) for w in (1, 2, 3, 4) for p in (False, True)}
-    assert {(width(d), lib().dkv(b, h, kh, d, q, kv) > 1) for b, h, kh, d, q, kv in sizes} == {(w, p) for w in (1, 2, 3, 4) for p in (False, True)}
+    found = {(width(s[3]), *bwd(*s)) for s in sizes}
+    assert {(w, both, parts > 1) for w, both, parts, _ in found} >= {(w, True, p) for w in (1, 2, 3, 4) for p in (False, True)}
+    assert {(w, both, parts > 1) for w, both, _, parts in found} >= {(w, b, p) for w in (1, 2, 3, 4) for b in (False, True) for p in (False, True)}
 
 
 def test_parts_stay_in_bounds():
@@ -117,7 +126,7 @@ def test_parts_stay_in_bounds():
         assert (blocks - 1) * per < q * (group if few else 1) <= blocks * per
         if parts > 1:      # the sums of all parts stay within 512 MiB
             assert parts * b * h * q * (4 * d + 8) < 1 << 29
-        n = lib().dq(b, h, q, kv)
-        assert 1 <= n <= 16 and (n == 1 or n * b * h * q * d * 4 < 1 << 29)
-        n = lib().dkv(b, h, kh, d, q, kv)
-        assert 1 <= n <= 32 and (n == 1 or n * 2 * b * kv * kh * d <= 1 << 26)
+        both, dq, dkv = bwd(b, h, kh, d, q, kv)
+        assert 1 <= dq <= 16 and (dq == 1 or dq * b * h * q * d * 4 < 1 << 29)
+        assert 1 <= dkv <= 32 and (dkv == 1 or dkv * 2 * b * kv * kh * d <= 1 << 26)
+        assert not both or b * h * -(-q // 128) * dq + b * kh * -(-kv // 128) * dkv <= 512
