@@ -11,6 +11,9 @@
 // encoder has few states beside the tokens: the tokens are split over workgroups,
 // whose sums k_cross_sums adds in order.
 //
+// k_cross_both: the two in one launch, side by side, for calls too small to fill the
+// CUs with either; dk and dv then form D themselves.
+//
 // 18432 tokens, 32 heads of 128: dq 130 us with 64 states, 272 with 512 (850
 // TFLOP/s), 810 with 2048 (1140); dk and dv 104, 321 (960) and 1115 (1110).  One
 // pass for all three would form five products in place of seven, but has no place

@@ -289,7 +289,11 @@ inline CrossPick pick_cross(int batch, int heads, int kv_heads, int head_dim, in
 // picked: 4608 tokens, 32 heads of 128, 512 states 194 and 96; 2 x 577 tokens, 4
 // heads of 64 for 16, 120 states 82 and 19; 4 x 1024, 12 heads of 72, 77 states 33 and 18).
 //
-// both: one launch, for calls whose dq leaves half of the CUs' places to dk and dv.
+// both: one launch, where dq leaves dk and dv a quarter of the CUs' places or more,
+// for two parts of theirs if they have as many (us, in turn and in one launch: 3 x 577
+// tokens, 16 heads of 72 on 4, 120 states 26.5 and 21.5; 2048 tokens, 16 heads of 128, 512
+// states 63 and 51; 20 heads of 64, 256 states 38 and 32; 24 heads of 128, 512
+// states, whose dk and dv would be whole, 81 and 125).
 struct CrossBwdPick { int q_parts, kv_parts; bool both; };
 inline CrossBwdPick pick_cross_bwd(int batch, int heads, int kv_heads, int head_dim, int q_len, int kv_len) {
   const int64_t q_wgs = (int64_t)batch * heads * ((q_len + 127) / 128);
@@ -297,7 +301,7 @@ inline CrossBwdPick pick_cross_bwd(int batch, int heads, int kv_heads, int head_
   const int64_t wgs = (int64_t)batch * kv_heads * ((kv_len + 127) / 128), tiles = (int64_t)heads / kv_heads * ((q_len + 63) / 64);
   if (!wgs) return {q_parts, 1, false};
   const int64_t sums = 2 * (int64_t)batch * kv_len * kv_heads * head_dim, left = 2 * RULE_CUS - q_wgs * q_parts;
-  const bool both = left >= RULE_CUS && left >= wgs;
+  const bool both = left >= RULE_CUS / 2 && left >= (tiles >= 4 ? 2 : 1) * wgs;
   const int64_t slots = both ? left : (head_dim <= 64 ? 3 : 2) * RULE_CUS;
   return {q_parts, (int)std::max<int64_t>(1, std::min<int64_t>({slots / wgs, tiles / 2, 32, ((int64_t)1 << 26) / sums})), both};
 }

@@ -82,8 +82,8 @@ SIZES = [
     (1, 16, 4, 56, 16, 700, [-3]), (1, 2, 2, 120, 600, 1100, [2000]), (8, 40, 40, 64, 90, 40, None),
     (1, 2, 2, 64, 300, 900, None), (1, 2, 2, 88, 200, 1000, None), (1, 2, 1, 32, 700, 100, None),
     (1, 2, 2, 64, 300, 1025, [1000]), (1, 2, 2, 88, 200, 1300, None), (1, 3, 3, 32, 129, 1200, [1100]), (1, 2, 2, 120, 200, 2100, None),
-    (8, 33, 33, 32, 40, 20, None), (3, 90, 30, 32, 70, 20, [20, 3, 0]), (3, 90, 30, 56, 70, 20, [7, 20, 20]), (8, 33, 33, 72, 40, 20, None),
-    (3, 90, 30, 96, 70, 20, [0, 20, 11]),
+    (8, 33, 33, 32, 40, 20, None), (4, 99, 33, 32, 70, 20, [20, 3, 0, 9]), (4, 99, 33, 56, 70, 20, [7, 20, 20, 1]), (8, 33, 33, 72, 40, 20, None),
+    (4, 99, 33, 96, 70, 20, [0, 20, 11, 20]),
 ]
 TOKENS = [
     (1, 1, 1, 128, 1, 1, None), (3, 8, 1, 128, 1, 5000, [5000, 1, 0]), (2, 4, 4, 64, 1, 3001, [3001, 64]), (1, 32, 8, 128, 1, 9000, None),
