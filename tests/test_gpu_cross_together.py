@@ -211,7 +211,7 @@ def linear_bwd(rows, dim, out):
 CASES = {
     "attention": lambda: attention(1, 4, 4, 64, 700, 300), "attention in parts": lambda: attention(1, 2, 2, 128, 200, 2000),
     "single tokens": lambda: attention(130, 4, 2, 64, 1, 40), "single tokens in parts": lambda: attention(2, 8, 2, 128, 1, 3000),
-    "attention gradient": lambda: attention_gradient(8, 40, 40, 64, 90, 40), "attention gradient in parts": lambda: attention_gradient(1, 3, 3, 72, 129, 1000),
+    "attention gradient": lambda: attention_gradient(8, 40, 40, 64, 90, 40), "attention gradient in parts": lambda: attention_gradient(1, 3, 3, 72, 300, 1100),
     "norm": lambda: norm(300), "norm gradient": lambda: norm_bwd(3000), "linear, few rows": lambda: linear(7, 520), "linear": lambda: linear(700, 520),
     "linear, two launches": lambda: linear(9000, 2056, 520), "linear gradient, one launch of products": lambda: linear_bwd(65, 136, 200),
     "two launches": lambda: linear_bwd(3000, 1032, 4104), "split dx": lambda: linear_bwd(70, 136, 8200), "split dw": lambda: linear_bwd(4500, 64, 72),
