@@ -163,7 +163,8 @@ XEMA_API int xema_op_linear_bwd(const xema_linear_bwd_args* args, void* stream);
  * values are taken between 0 and kv_len.  Rows of k and v behind a sequence's
  * last state are not read for their values: NaN there does not reach o.  A
  * sequence of no states gives o = 0 and lse = -infinity, and so do tokens whose
- * scores all are -infinity; such scores weigh nothing beside others.
+ * scores all are -infinity; such scores weigh nothing beside others.  Scores are
+ * fp32 and so is scale log2(e) q_i . k_j: past 2^128 they are infinite.
  * lse fp32 [batch, heads, q_len] (may be NULL; 4-byte aligned) is for the
  * gradient.  p is rounded to `dtype` for its product with v; scores, sums and o
  * are fp32 until the rounding of o (weights below 2^-126 are zeros).

@@ -33,7 +33,10 @@ namespace {
 constexpr int KT = 32;                 // states per tile
 constexpr int CROSS_WAVES = 4;
 constexpr float PMAX = 4096.f;         // (fp16 P stays finite; 2^12 beside sums in fp32 loses nothing)
-constexpr float LOWEST = -1e30f;       // a reference below every score, so that -infinity less it stays one
+constexpr float LOWEST = -0x1.fffffep127f;   // a reference that no finite score is below; -infinity less it stays one
+// References from here on have steps of 2 and more: what their own rounding leaves of
+// c s - m, formed in one step, would be whole factors of 2 in every weight.
+constexpr float COARSE = 0x1p24f;
 
 struct CrossParams {
   const void *q, *k, *v;
@@ -62,12 +65,13 @@ struct Column {
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[d][r] = 0.f;
   }
-  // scores (of NB blocks of 32 states) to weights 2^(c s - m)
+  // scores (of NB blocks of 32 states) to weights 2^(c s - m).  Coarse references
+  // take every tile through the branch, whose c s is rounded as the maximum's is.
   template <int NB>
   __device__ __forceinline__ void weigh(f32x16 (&s)[NB], float c, bool first) {
     f32x16 p[NB];
-    float sum = first ? 0.f : exps<NB>(s, p, c);
-    const bool grow = first || !(pair_max(sum) <= PMAX);
+    float sum = first ? 0.f : exps<NB>(s, p, 1.f, c);
+    const bool grow = first || !(pair_max(sum) <= PMAX) || !(fabsf(m) < COARSE);
     if (__builtin_amdgcn_ballot_w64(grow)) {
       float top = s[0][0] * c;
 #pragma unroll
@@ -82,21 +86,23 @@ struct Column {
       for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[d][r] *= f;
-      sum = exps<NB>(s, p, c);
+      const bool fine = fabsf(m) < COARSE;
+      sum = exps<NB>(s, p, fine ? 1.f : c, fine ? c : 1.f);
     }
     l += sum;
 #pragma unroll
     for (int b = 0; b < NB; ++b) s[b] = p[b];
   }
+  // p = 2^((a s) b - m), a s rounded; returns this lane's sum
   template <int NB>
-  __device__ __forceinline__ float exps(const f32x16 (&s)[NB], f32x16 (&p)[NB], float c) const {
+  __device__ __forceinline__ float exps(const f32x16 (&s)[NB], f32x16 (&p)[NB], float a, float b) const {
     float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+    for (int n = 0; n < NB; ++n)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        p[b][r] = __builtin_amdgcn_exp2f(fmaf(s[b][r], c, -m));
-        part[r & 3] += p[b][r];
+        p[n][r] = __builtin_amdgcn_exp2f(fmaf(a * s[n][r], b, -m));
+        part[r & 3] += p[n][r];
       }
     return (part[0] + part[1]) + (part[2] + part[3]);
   }
