@@ -202,6 +202,9 @@ XEMA_API int xema_op_cross_attn(const xema_cross_attn_args* args, void* stream);
  * in fp32 and rounded to `dtype` once, for the products; in fp16 p is carried as
  * 2^14 p (16 bits down to p = 2^-28), and ds below 2^-14 loses bits (off by up to
  * 2^-25): scale the loss as fp16 training does.  D comes from the rounded o.
+ * p comes from lse, whose rounding takes it off by a factor of up to e^(|lse| / 2^22)
+ * (2^-8, bf16's half step, at |lse| = 2^14); a token whose |lse| is 2^22 or more has
+ * no gradient: its lse tells no weights, and p = 0.
  * The workspace (256-byte aligned) has at least
  * xema_cross_attn_bwd_workspace_bytes bytes.  Limits as above.              */
 typedef struct {

@@ -42,7 +42,7 @@ struct CrossBwd {
   const float* lse;
   const int32_t* kv_lens;
   void *dq, *dk, *dv;
-  float *stat_l, *stat_d;              // [batch, heads, q_len rounded up to KT]: lse in log2 units less P_EXP (+infinity: no states, no token), P_UNIT D
+  float *stat_l, *stat_d;              // [batch, heads, q_len rounded up to KT]: lse in log2 units less P_EXP (+infinity: no weights, no token), P_UNIT D
   float* dq_parts;                     // [parts][batch * q_len][heads * head_dim]
   float* dkv_parts;                    // [parts][dk, dv][batch * kv_len][kv_heads * head_dim]
   int64_t ldq, ldk, ldv, ldo, ld_do, ld_dq, ld_dk, ld_dv;
@@ -54,11 +54,16 @@ struct CrossBwd {
 constexpr int QKT = 32;                // states per tile of k_cross_dq
 
 // What both passes form has the same bits in either.
-// lse in log2 units, +infinity for a token of no states (its weights are then zeros).
+// lse in log2 units, +infinity for a token of no states and for one whose lse is too
+// coarse (their weights are then zeros).  lse has the roundings of scale log2(e) times
+// a score, of a sum and of two products, up to 4 half steps: from 2^22 on e^(s - lse)
+// would be off by a factor of e or more, and soon 2^14 p past fp16's range.  (Weights
+// held at 1 at most, in place of this, cost an instruction each: up to 5% of a pass.)
+constexpr float LSE_END = 0x1p22f;
 __device__ __forceinline__ float log2_lse(float lse) {
   float l = lse * LOG2E_F;
   asm("" : "+v"(l));                   // (rounded here, not fused with what it is added to)
-  return lse == -INFINITY ? INFINITY : l;
+  return fabsf(lse) >= LSE_END ? INFINITY : l;
 }
 // A 16-byte slot's share of D; slots are added in pairs, their pairs in pairs, ...
 template <typename F>

@@ -52,3 +52,48 @@ def test_finite_scores_of_any_size(size, dtype, base):
         lse = c.lse[i].double()
         want = s + torch.full_like(lse, len(v)).log()
         R.within(lse, want, 6 * R.U * want.abs() + (n + 100) * 2 * R.U, "lse")
+
+
+# the kernels of the gradient: one launch and two, dq whole and in parts, dk and dv too, every width of heads
+GRADIENTS = [(2, 4, 2, 64, 130, 200, [200, 77]), (1, 2, 2, 96, 100, 2100, [2050]), (8, 33, 33, 32, 40, 20, None), (8, 33, 33, 72, 40, 20, None),
+             (1, 2, 2, 128, 3000, 20, None), (1, 16, 1, 128, 1100, 150, None), (1, 4, 2, 128, 2, 3000, [2500]), (4, 32, 32, 128, 300, 100, [100, 9, 50, 0])]
+
+
+@pytest.mark.parametrize("size", GRADIENTS, ids=str)
+@pytest.mark.parametrize("dtype,base", [(t, s * b) for s in (1, -1) for t, b in ((BF16, 1e8), (BF16, 1e10), (BF16, 1e30), (BF16, 1e36), (F16, 1e8),
+                                                                                 (F16, 1e9))], ids=str)
+def test_tokens_whose_lse_tells_no_weights_have_no_gradient(size, dtype, base):
+    """Every third token has scores of +-base, with an lse past 2^22: the gradients are those of the other tokens alone."""
+    c = Call(*size[:6], dtype, size[6], seed=12)
+    b, h, kh, d, q_len, n = c.sizes
+    root = 1.0 if dtype == BF16 else 2.0 ** 15           # (fp16: both factors share the score)
+    c.k[:, 0:c.nk:d] = base / root
+    c.q[:, 0:c.nq:d] = 0
+    coarse = torch.arange(b * q_len, device=DEV) % 3 == 1
+    c.q[coarse, 0:c.nq:d] = root
+    c.forward()
+    lse = c.lse.transpose(1, 2).reshape(b * q_len, h).abs()
+    # (infinite where a sequence has no states)
+    assert bool((lse[coarse] > 2.0 ** 22).all()) and bool(((lse < 100) | torch.isinf(lse))[~coarse].all())
+    c.backward()
+    assert bool((c.dq[coarse, :c.nq] == 0).all())
+    # (the reference meets the other tokens alone: no dout, and scores and an lse that leave p = 0 here)
+    c.q[coarse, :c.nq] = 0
+    c.do[coarse] = 0
+    c.lse[:] = torch.where(coarse.view(b, 1, q_len).expand(b, h, q_len), 1e4, c.lse)
+    c.check_backward()
+
+
+@pytest.mark.parametrize("size", GRADIENTS, ids=str)
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_gradient_of_scores_of_tens_of_thousands(size, dtype):
+    """p comes from lse: the bound takes 4 half steps of it."""
+    c = Call(*size[:6], dtype, size[6], seed=13)
+    d = c.sizes[3]
+    c.k[:, 0:c.nk:d] = 1000
+    c.q[:, 0:c.nq:d] = torch.linspace(-500, 500, c.q.shape[0], device=DEV).to(dtype)[:, None]
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
+    assert float(c.lse.abs().max()) > 4e4
