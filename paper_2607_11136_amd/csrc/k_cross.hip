@@ -366,12 +366,13 @@ __global__ __launch_bounds__(256) void k_cross_join(CrossParams p) {
   const int lane = threadIdx.x & 63, e = ((int)threadIdx.x & 15) * 8, first = (int)threadIdx.x / 16;
   const float2 ml = lane < p.parts ? p.part_ml[lane * p.rows + row] : float2{LOWEST, 0.f};
   const float m = wave_max(ml.x), w = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - m), sum = wave_sum(ml.y * w);
+  // (a part of no sum may not have been written; one whose sum weighs nothing here may hold a NaN)
+  const uint64_t written = __builtin_amdgcn_ballot_w64(ml.y != 0.f);
   f32x4 v[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
   for (int i0 = 0; i0 < p.parts; i0 += 16) {
     const int i = i0 + first;
     const float f = __shfl(w, i & 63, 64);
-    // (a part of no weight may not have been written)
-    if (i < p.parts && f != 0.f && e < p.head_dim) {
+    if (i < p.parts && (written >> i & 1) && e < p.head_dim) {
       const f32x4* const at = reinterpret_cast<const f32x4*>(p.part_o + (i * p.rows + row) * p.head_dim + e);
 #pragma unroll
       for (int x = 0; x < 2; ++x) v[x] += at[x] * f;
@@ -408,8 +409,8 @@ __global__ __launch_bounds__(256) void k_cross_join_rows(CrossParams p) {
 #pragma unroll 4
   for (int i = 0; i < p.parts; ++i) {
     const float2 ml = p.part_ml[i * p.rows + row];
-    const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
-    if (f == 0.f) continue;      // (a part of no weight may not have been written)
+    if (ml.y == 0.f) continue;      // (a part of no sum may not have been written; one whose sum weighs nothing here may hold a NaN)
+    const float f = __builtin_amdgcn_exp2f(ml.x - m);
     sum = fmaf(ml.y, f, sum);
     const f32x4* const at = reinterpret_cast<const f32x4*>(p.part_o + (i * p.rows + row) * p.head_dim + e);
 #pragma unroll

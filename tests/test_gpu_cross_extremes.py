@@ -97,3 +97,26 @@ def test_gradient_of_scores_of_tens_of_thousands(size, dtype):
     c.backward()
     c.check_backward()
     assert float(c.lse.abs().max()) > 4e4
+
+
+# with the states of the first part, where there are parts
+@pytest.mark.parametrize("size,first", list(zip(KERNELS, (64, 288, 288, 288, 1, 128))), ids=str)
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_nan_of_any_state_is_met(size, first, dtype):
+    """Every sequence's first states, a whole part of them, have NaN as keys, or as the values of states that weigh nothing in
+    fp32: it is not lost where the parts are joined."""
+    c = Call(*size[:6], dtype, size[6], seed=14)
+    b, h, kh, d, q_len, n = c.sizes
+    bad = (torch.arange(n, device=DEV) < first).repeat(b)
+    keep = c.kv.clone()
+    c.kv[bad, :c.nk] = float("nan")
+    c.forward()
+    assert bool(torch.isnan(c.o[:, :c.nq]).all()) and bool(torch.isnan(c.lse).all())
+    c.kv.copy_(keep)
+    c.q[:, 0:c.nq:d] = 100
+    c.k[bad, 0:c.nk:d] = -100           # a weight of e^-883 at most beside the others
+    c.v[bad, 1:c.nk:d] = float("nan")
+    c.forward()
+    o = c.o[:, :c.nq].view(-1, h, d)
+    assert bool(torch.isnan(o[:, :, 1]).all()) and bool(torch.isfinite(torch.cat((o[:, :, :1], o[:, :, 2:]), 2)).all())
+    assert bool(torch.isfinite(c.lse).all())
