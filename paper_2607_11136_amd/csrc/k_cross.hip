@@ -442,11 +442,6 @@ hipError_t run_cross(CrossParams p, const CrossPick& pick, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Rows up to which a workgroup joins one (us of the call with k_cross_join and
-// k_cross_join_rows: 128 rows in 16 parts 47 and 54; 512 in 4 either 47; 8192 in 2
-// 21 and 14).
-constexpr int64_t JOIN_ROWS = 1024;
-
 template <typename T>
 hipError_t cross_t(const CrossParams& p, const CrossPick& pick, hipStream_t s) {
   hipError_t e;
@@ -455,7 +450,10 @@ hipError_t cross_t(const CrossParams& p, const CrossPick& pick, hipStream_t s) {
   else if (p.head_dim <= 96) e = run_cross<T, 96>(p, pick, s);
   else e = run_cross<T, 128>(p, pick, s);
   if (e != hipSuccess || p.parts == 1) return e;
-  if (p.rows > JOIN_ROWS) return p.head_dim <= 64 ? run_join_rows<T, 8>(p, s) : run_join_rows<T, 16>(p, s);
+  switch (pick_join(p.rows, p.head_dim)) {
+    case 8: return run_join_rows<T, 8>(p, s);
+    case 16: return run_join_rows<T, 16>(p, s);
+  }
   hipLaunchKernelGGL((k_cross_join<T>), dim3((unsigned)p.rows), dim3(256), 0, s, p);
   return hipGetLastError();
 }

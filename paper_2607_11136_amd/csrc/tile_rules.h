@@ -281,6 +281,12 @@ inline CrossPick pick_cross(int batch, int heads, int kv_heads, int head_dim, in
   return {true, blocks, wgs ? (int)std::max<int64_t>(1, std::min<int64_t>({(FEW_WGS + wgs - 1) / wgs, most, 64})) : 1};
 }
 
+// Threads that join a row's parts: a workgroup for each of few rows (k_cross_join),
+// otherwise eight columns a thread (k_cross_join_rows).  us of the call with a
+// workgroup a row and with threads a row: 128 rows in 16 parts 47 and 54; 512 in 4
+// either 47; 8192 in 2 21 and 14.
+inline int pick_join(int64_t rows, int head_dim) { return rows <= 1024 ? 256 : head_dim <= 64 ? 8 : 16; }
+
 // The gradient.  dq: as the forward pass (us, whole and in parts: 512 states 17.9
 // and 19.5, 1024 states 19.8 and 15.6, 4096 states 100 and 21).  dk and dv: parts of
 // the tokens of all heads that share a state's head, for workgroups of 128 states;
