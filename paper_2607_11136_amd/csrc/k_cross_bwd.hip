@@ -104,7 +104,7 @@ __device__ __forceinline__ void cross_dq(const CrossBwd& p, int wg, int wgs, uin
   uint8_t* const q_rows = smem[wave < 2 ? 2 : 1] + (wave & 1) * WaveRows<HDP>::BYTES;
   uint8_t* const d_out_rows = smem[3 + wave / 2] + (wave & 1) * WaveRows<HDP>::BYTES;
   WaveRows<HDP>::load((const T*)p.dout + tok0 * p.ld_do + at, (uint32_t)p.ld_do * 2, p.head_dim, left_q, d_out_rows, lane);
-  WaveRows<HDP>::load((const T*)p.q + tok0 * p.ldq + at, (uint32_t)p.ldq * 2, p.head_dim, left_q, q_rows, lane);
+  if (p.dq) WaveRows<HDP>::load((const T*)p.q + tok0 * p.ldq + at, (uint32_t)p.ldq * 2, p.head_dim, left_q, q_rows, lane);
   // (o is met row by row: SLOTS lanes a row, eight elements each)
   const int slot = lane % SLOTS;
   frag o[32 / PER];
@@ -465,13 +465,14 @@ int64_t cross_attn_bwd_workspace(const CrossShape& c) {
 
 hipError_t launch_cross_attn_bwd(const xema_cross_attn_bwd_args& a, hipStream_t s) {
   const BwdSpace w = bwd_space({a.batch, a.heads, a.kv_heads, a.head_dim, a.q_len, a.kv_len});
+  const CrossBwdPick pick = a.dq ? w.pick : without_dq(w.pick);
   float* const ws = (float*)a.workspace;
   auto blocks = [](int n) { return n > 0 ? (n + 32 * BWD_WAVES - 1) / (32 * BWD_WAVES) : 1; };
   const CrossBwd p{a.q, a.k, a.v, a.o, a.dout, a.lse, a.kv_lens, a.dq, a.dk, a.dv, ws, ws + w.stats, ws + 2 * w.stats, ws + 2 * w.stats + w.dq,
                    a.ldq, a.ldk, a.ldv, a.ldo, a.ld_do, a.ld_dq, a.ld_dk, a.ld_dv, a.batch, a.heads, a.kv_heads, a.head_dim, a.q_len, a.kv_len,
-                   w.pick.q_parts, w.pick.kv_parts, Divisor(blocks(a.q_len)), Divisor(w.pick.q_parts), Divisor(blocks(a.kv_len)), Divisor(w.pick.kv_parts), Divisor(a.batch),
-                   Divisor(a.heads / a.kv_heads), Divisor(a.q_len > 0 ? (a.q_len + KT - 1) / KT : 1), a.scale * LOG2E_F, a.scale};
-  return a.dtype == XEMA_BF16 ? cross_bwd_t<bf16>(p, w.pick.both, s) : cross_bwd_t<f16>(p, w.pick.both, s);
+                   pick.q_parts, pick.kv_parts, Divisor(blocks(a.q_len)), Divisor(pick.q_parts), Divisor(blocks(a.kv_len)),
+                   Divisor(pick.kv_parts), Divisor(a.batch), Divisor(a.heads / a.kv_heads), Divisor(a.q_len > 0 ? (a.q_len + KT - 1) / KT : 1), a.scale * LOG2E_F, a.scale};
+  return a.dtype == XEMA_BF16 ? cross_bwd_t<bf16>(p, pick.both, s) : cross_bwd_t<f16>(p, pick.both, s);
 }
 
 }  // namespace xema

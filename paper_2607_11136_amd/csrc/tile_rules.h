@@ -312,6 +312,11 @@ inline CrossBwdPick pick_cross_bwd(int batch, int heads, int kv_heads, int head_
   return {q_parts, (int)std::max<int64_t>(1, std::min<int64_t>({slots / wgs, tiles / 2, 32, ((int64_t)1 << 26) / sums})), both};
 }
 
+// Without dq, its pass leaves lse and D for dk and dv, of every token once and
+// whatever the states: one part, no launch of both.  kv_parts, which the workspace and
+// the bytes of dk and dv go by, stay as they are.
+inline CrossBwdPick without_dq(const CrossBwdPick& p) { return {1, p.kv_parts, false}; }
+
 // ---------------------------------------------------------------------------
 // k_upconv.  A tile is RG R fragments of 16 corners (a corner: the four outputs
 // between four source pixels) and 128 / RG channels.
