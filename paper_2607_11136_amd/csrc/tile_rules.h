@@ -152,10 +152,17 @@ inline FfnTile pick_tile(int64_t m, int64_t n, int64_t steps) {
   return (FfnTile)best;
 }
 
-// Rows of a product in two launches: the first `rows` in tiles of 256 x 256, as many
-// whole rounds of them as there are, and the rest in a tile that finishes soonest
-// (a second launch costs 3 us).  Every tile sums in the same order, so the values
-// do not depend on it.
+// Rows of a product in two launches: the first `rows`, any number of 256-row blocks
+// that leaves less than 48 of them, in tiles of 256 x 256, and the rest in the tile
+// that finishes soonest, where the model has the two take less than one (a second
+// launch costs 3 us).  Most often the rest is what lies past whole rounds of tiles.
+// Every tile sums in the same order, so the values do not depend on it.  129 sizes
+// (1063 to 31706 rows, 536 to 15992 columns, k of 320 to 11264), what two launches
+// take off one's time: where the model gives less than 2%, -6 to 9%, 0.8% in the mean
+// (so small gains are taken too); from 2 to 8%, -3 to 10%, 3.2%; past that 1 to 31%, 13%.
+// us, rows x columns x k, one and two: 4608 x 4096 x 4096 149 and 129, 9216 rows 270
+// and 245; 8192 x 11008 x 4096, 0.6% by the model, 570 and 571; 10793 x 4456 x 512,
+// 0.8%, 64 and 68; 9854 x 15872 x 320, 0.1%, 155 and 141.
 struct FfnRows { int64_t rows; FfnTile rest; };
 inline FfnRows pick_rows(int64_t m, int64_t n, int64_t steps) {
   FfnRows best{0, pick_tile(m, n, steps)};
