@@ -116,8 +116,11 @@ void layernorm_x(const xema_layernorm_args& a, hipStream_t s) {
   }
 }
 
-// store8 with one branch, the 16-bit types by a choice of values.  (With two, hipcc
-// of ROCm 7.2 lost the gradient's running sums on the path to one of the stores.)
+// store8 with one branch, the 16-bit types by a choice of values.  With the three-way
+// switch that store8 becomes, hipcc of ROCm 7.2 makes wrong code here: the IR joins the
+// running sums from all three stores, the machine code enters the fp32 store from the
+// tests of the other types with its copies of four of them undefined (16-bit s and dy,
+// fp32 dx, narrow rows: dbeta wrong in up to half of the columns).
 __device__ __forceinline__ void put8(void* p, int dtype, int64_t at, const float f[8]) {
   typedef bf16 b8 __attribute__((ext_vector_type(8)));
   if (dtype == XEMA_F32) {
