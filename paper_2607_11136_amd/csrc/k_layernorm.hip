@@ -95,8 +95,13 @@ template <typename XT, typename RT, int WPR>
 void layernorm_nv(const xema_layernorm_args& a, hipStream_t s) {
   const dim3 grid((unsigned)(WPR == 1 ? (a.rows + LN_WAVES - 1) / LN_WAVES : a.rows)), block(LN_WAVES * 64);
   const int nv = (a.dim + 512 * WPR - 1) / (512 * WPR);
-  if (nv <= 1) hipLaunchKernelGGL((k_layernorm<XT, RT, 1, WPR>), grid, block, 0, s, a);
-  else if (nv <= 2) hipLaunchKernelGGL((k_layernorm<XT, RT, 2, WPR>), grid, block, 0, s, a);
+  if constexpr (WPR == 1) {      // (rows of four waves have more than 2048 elements)
+    if (nv <= 1) {
+      hipLaunchKernelGGL((k_layernorm<XT, RT, 1, WPR>), grid, block, 0, s, a);
+      return;
+    }
+  }
+  if (nv <= 2) hipLaunchKernelGGL((k_layernorm<XT, RT, 2, WPR>), grid, block, 0, s, a);
   else if (nv <= 4) hipLaunchKernelGGL((k_layernorm<XT, RT, 4, WPR>), grid, block, 0, s, a);
   else if constexpr (WPR > 1) hipLaunchKernelGGL((k_layernorm<XT, RT, 8, WPR>), grid, block, 0, s, a);
 }
