@@ -153,7 +153,9 @@ __device__ __forceinline__ void load_column(const T* p, int head_dim, int hi, ty
   }
 }
 
-// 8 registers of a result as the operand of the next product
+// 8 registers of a result as the operand of the next product: P and dS are rounded
+// here, to the 16 bits of the other operand (the MFMA takes no wider one; a second
+// product with what the rounding leaves would double their cost).
 template <typename T>
 __device__ __forceinline__ typename Mfma<T>::frag pack8(const f32x16& s, int u) {
   typename Mfma<T>::frag f;

@@ -9,10 +9,12 @@
 // PMAX, and the largest weight is at least 1 against the sum.  Tiles of 32 states
 // leave three workgroups a CU (four at head dims to 64), which hide each other's
 // loads, barriers and exponentials: 2 x 28612 tokens, 32 heads of 128, 512 and 256
-// states 429 to 475 us by the card, 510 with tiles of 64 and two workgroups.
-// 18432 tokens, 32 heads of 128: 64 states 64 us (4.8 TB/s), 512 states 205 (750
-// TFLOP/s), 2048 states 615 (1010); products and exponentials add up, and the
-// card's clock sinks under both.
+// states 415 to 475 us by the card, 510 with tiles of 64 and two workgroups.
+// 18432 tokens, 32 heads of 128: 64 states 63 us (4.8 TB/s), 512 states 201 (770
+// TFLOP/s), 2048 states 590 (1045); MFMAs are busy 13, 46 and 60% of the cycles, at
+// 2.5, 1.95 and 1.7 GHz.  A workgroup's loads of q, products, exponentials and stores
+// of o follow one another, which other workgroups hide in part; the more of it they
+// hide, the lower the card's clock.
 //
 // k_cross_few: single tokens.  The tokens of all heads that share a state's head
 // are one block of up to 32 queries, and the workgroup's waves take tiles of 32

@@ -14,10 +14,12 @@
 // k_cross_both: the two in one launch, side by side, for calls too small to fill the
 // CUs with either; dk and dv then form D themselves.
 //
-// 18432 tokens, 32 heads of 128: dq 130 us with 64 states, 272 with 512 (850
-// TFLOP/s), 810 with 2048 (1140); dk and dv 104, 321 (960) and 1115 (1110).  One
-// pass for all three would form five products in place of seven, but has no place
-// for dq but sums in memory.
+// 18432 tokens, 32 heads of 128: dq 127 us with 64 states, 280 with 512 (830
+// TFLOP/s), 825 with 2048 (1120); dk and dv 95, 305 (1010) and 1065 (1160).  MFMAs are
+// busy 9 and 20% of the cycles with 64 states, 40 and 52% with 512 at 2.0 GHz, 57% with
+// 2048 at 1.8.  One pass for all three would form five products in place of seven.
+// Past the 128 states of a workgroup dq would have to be added up in memory; up to
+// there its waves could add it in LDS, which no kernel here does.
 //
 // Products are formed transposed (cross_tile.h): a column's scores and their
 // gradients feed the last product from their registers.
@@ -65,7 +67,9 @@ __device__ __forceinline__ float log2_lse(float lse) {
   asm("" : "+v"(l));                   // (rounded here, not fused with what it is added to)
   return fabsf(lse) >= LSE_END ? INFINITY : l;
 }
-// A 16-byte slot's share of D; slots are added in pairs, their pairs in pairs, ...
+// A 16-byte slot's share of D; slots are added in pairs, their pairs in pairs, ...  (o
+// is the rounded one, all that the caller keeps: the exact D would take the scores and
+// dp of all states before the first dS.)
 template <typename F>
 __device__ __forceinline__ float slot_dot(const F& d, const F& o) {
   float sum = 0.f;

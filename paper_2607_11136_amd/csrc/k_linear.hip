@@ -225,9 +225,10 @@ hipError_t linear_y(const LinearParams& p, int y_dtype, hipStream_t s) {
   return y_dtype == XEMA_BF16 ? linear_t<T, bf16>(p, s) : y_dtype == XEMA_F16 ? linear_t<T, f16>(p, s) : linear_t<T, float>(p, s);
 }
 
-// dz = dy act'(z), rounded to T (not stored where dz is null), and the column
-// sums of the rounded-free values over each chunk of rows.  A workgroup takes 256
-// columns, 8 a thread, of `chunk` rows, 8 rows at a time.
+// dz = dy act'(z), rounded to T, the type of its products' other operands (not stored
+// where dz is null), and the column sums of the values before that rounding over each
+// chunk of rows.  A workgroup takes 256 columns, 8 a thread, of `chunk` rows, 8 rows
+// at a time.
 template <typename T, typename DT, bool ACT>
 __global__ __launch_bounds__(256) void k_linear_grad(const uint8_t* __restrict__ pre, const DT* __restrict__ dy, int64_t ld_dy, int64_t rows,
                                                      int out_dim, int act, int chunk, T* __restrict__ dz, float* __restrict__ partial) {
@@ -337,6 +338,7 @@ __global__ __launch_bounds__(S::NW * 64, 1) void k_linear_products(LinearBwd p, 
     float v = 0.f;
 #pragma unroll 8
     for (int i = 0; i < p.chunks; ++i) v += p.partial[(int64_t)i * p.out_dim + c];
+    // (bf16 in fp16 calls too, as the bias itself: the library's vectors of weights have one type)
     p.dbias[c] = __builtin_bit_cast(uint16_t, (bf16)v);
     return;
   }
