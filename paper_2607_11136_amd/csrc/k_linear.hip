@@ -1,13 +1,14 @@
 // Linear layer with bias, activation and residual in its epilogue, and its
 // gradient (xema_cross.h), on the tiles of mma_tile.h.
 //
-// Forward: one kernel, bound by its MFMAs, or for few rows by reading the
-// weights; the last rows take a launch of their own where the rule's model has that
-// faster (4608 x 4096 x 4096 with an fp32 residual 145 us, in one launch 163).  9216 x 4096 x 4096: in bf16 245 us, 1260 TFLOP/s; with the fp32
-// residual 306, as its 302 MB come and go while no tile multiplies (loads ahead of
-// the epilogue gained nothing; the rest's tiles ahead of the others in one launch,
-// so that half of the CUs end at unlike times, 5% here and nothing at other sizes).
-// 24 x 4096 x 4096: 12 us, 2.8 TB/s.
+// Forward: one kernel, bound by its MFMAs, or for few rows by reading the weights;
+// the last rows take a launch of their own where the rule's model has that faster
+// (4608 x 4096 x 4096 with an fp32 residual 145 us, in one launch 163).  9216 x
+// 4096 x 4096: in bf16 245 us, 1260 TFLOP/s; with the fp32 residual 306, as its
+// 302 MB come and go while no tile multiplies (loads ahead of the epilogue gained
+// nothing; the rest's tiles ahead of the others in one launch, so that half of the
+// CUs end at unlike times, 5% here and nothing at other sizes). 24 x 4096 x 4096:
+// 12 us, 2.8 TB/s.
 //
 // Gradient: dz first where there is an activation, dy in fp32 or a bias (bound by
 // HBM: both products need it in either order; 8192 x 11008, gelu, 143 us, 4.4
